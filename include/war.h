@@ -16,6 +16,10 @@
  *   war_verify_attn                      tree-masked GQA decode attention over a paged bf16 KV cache
  *   war_accept                           longest root path of the tree that equals the target's tokens
  *   war_commit                           the accepted tokens become context: KV rows, prefix length, tail window
+ *   war_rope_store                       rotary positions of a tree's queries and keys, K/V rows into the paged cache
+ *   war_verify_attn_quant                war_verify_attn over a cache held in 8 bits with a scale per block and head
+ *   war_target                           penalties, biases and grammar masks on the logits: the tokens war_accept compares with
+ *   war_commit_quant                     war_commit for the 8-bit cache
  *
  * Conventions shared by every call
  *   - Pointers named d_* are DEVICE pointers, h_* are HOST pointers.  The caller owns every buffer it
@@ -359,6 +363,150 @@ war_status_t war_commit(const int32_t* d_ids, const int32_t* d_accept_len, const
                         const int32_t* d_bonus, void* d_kpool, void* d_vpool, const int32_t* d_page_table,
                         const war_commit_params_t* params, int32_t* d_prefix_len, int32_t* d_tail,
                         int32_t* d_tail_len, war_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Rotary positions and the write of a tree's K/V rows into the cache (the model's side of verification, which the calls
+ * above leave to the caller: "slot a's K/V are at logical position prefix_len + a").  For request b, slot
+ * j < num_nodes[b], every head and every pair i < rot_dim / 2:
+ *     t      = (prefix_len[b] + depth(j)) * inv_freq[i]           (depth of slot j in its tree: its place in the text)
+ *     c, s   = factor * cos(t), factor * sin(t)
+ *     y[lo]  = x[lo] * c - x[hi] * s        y[hi] = x[hi] * c + x[lo] * s
+ *     (lo, hi) = (i, i + rot_dim / 2), or (2i, 2i + 1) when interleaved = 1; elements from rot_dim on are copied
+ * q goes to d_q_out (bf16 [B, N, Hq, D], rounded once; d_q_out may be d_q if d_q is contiguous), k rotated and v as it is
+ * go to cache position prefix_len[b] + j.  The angle is reduced in 64 bits; the rest is 32-bit arithmetic.
+ * kv_type 0: a bf16 pool, rows rounded once.  kv_type 1 (e4m3) or 2 (e5m2): an 8-bit pool with scales,
+ *     value = code * scale[page, head, (token in page) / scale_block],  scales float32 [num_pages, Hkv, page_size / scale_block]
+ * For every (head, block of scale_block tokens) that receives rows, K and V apart:
+ *     s_old  = the block's scale if it holds a token before prefix_len[b], else 0 (nothing of it is in use)
+ *     s      = max(s_old, smallest power of two with (largest new magnitude) <= most * s), most = 448 or 57344; at least
+ *              2^-100; 1 if all of that is 0
+ *     new codes = round(x / s) to nearest even, saturating; rows of tokens before prefix_len[b] are re-encoded by s_old / s
+ *     if s > s_old (exact for powers of two down to the type's smallest normal number); other rows keep their codes.
+ * A block that receives rows must belong to this request alone (a shared prefix is copied on write, as anywhere).
+ * inf saturates, NaN stays NaN (in the block's other rows neither is felt, but an infinite row makes its block's scale the
+ * largest there is).
+ * Inputs q, k, v: bf16 [B, N, H, D] by strides (request, slot, head, 1), multiples of 8 elements, on 16-byte boundaries
+ * (so the three parts of one projection's rows can be passed as they are).  Pools by strides as in war_attn_params_t: any
+ * with unit stride along d and the others multiples of 16 bytes.  page_size: a multiple of scale_block (8, 16, 32, 64 or
+ * 128); any for bf16.  D == 128, N <= 64, rot_dim even, 0 .. 128; Hq = 0 stores only.
+ * A malformed tree or prefix_len (WAR_ERR_BAD_TREE) or rows beyond max_pages_per_req (WAR_ERR_BAD_PAGE) leave the request
+ * as it was; a page id outside [0, num_pages) records WAR_ERR_BAD_PAGE and its rows are not written.
+ * Rows j >= num_nodes[b] of d_q_out and all other cache rows are left as they are.  One launch, no workspace. */
+#define WAR_KV_BF16 0
+#define WAR_KV_E4M3 1
+#define WAR_KV_E5M2 2
+typedef struct {
+    int32_t B, N, Hq, Hkv, D, page_size, max_pages_per_req;
+    int32_t kv_type, scale_block;                      /* scale_block is ignored for bf16 */
+    int32_t rot_dim, interleaved;
+    float factor;
+    int64_t num_pages;
+    int64_t q_strides[4], k_strides[4], v_strides[4];  /* [request, slot, head, d] in elements */
+    int64_t kpool_strides[4], vpool_strides[4];        /* [page, head, token, d] in elements */
+} war_rope_store_params_t;
+war_status_t war_rope_store(const void* d_q, const void* d_k, const void* d_v, const float* d_inv_freq,
+                            const int32_t* d_page_table, const int32_t* d_prefix_len, const int32_t* d_num_nodes,
+                            const int32_t* d_parent, const war_rope_store_params_t* params, void* d_kpool, void* d_vpool,
+                            float* d_kscale, float* d_vscale, void* d_q_out, war_stream_t stream);
+
+/* The frequencies of war_rope_store, on the host: h_inv_freq[rot_dim / 2] and the factor for cosine and sine.  With
+ * f[i] = base^(-2i / rot_dim), worked out in 64 bits and rounded once:
+ *   PLAIN   f
+ *   LINEAR  f / scale (positions interpolated)
+ *   BASE    base * scale^(rot_dim / (rot_dim - 2)) in place of base (the slowest wave is stretched by `scale`, the fastest
+ *           is kept)
+ *   RAMP    waves that make more than `fast` turns over original_length keep f, those with fewer than `slow` get f / scale,
+ *           between the two pair indices (rounded outwards) the share grows linearly with the index;
+ *           factor = 0.1 ln(scale) + 1
+ *   BANDS   the same choice by turns, with the share linear in the number of turns; factor 1
+ * fast, slow and original_length are read by the last two only; factor is 1 where nothing else is said. */
+#define WAR_ROPE_PLAIN 0
+#define WAR_ROPE_LINEAR 1
+#define WAR_ROPE_BASE 2
+#define WAR_ROPE_RAMP 3
+#define WAR_ROPE_BANDS 4
+typedef struct {
+    int32_t kind, rot_dim;
+    double base, scale, original_length, fast, slow;
+} war_rope_freq_params_t;
+war_status_t war_rope_frequencies(const war_rope_freq_params_t* params, float* h_inv_freq, float* h_factor);
+
+/* ------------------------------------------------------------------------------------------------
+ * Verification attention over a cache held in 8 bits: war_verify_attn with K[c,:] = kscale * kcode[c,:] and
+ * V[c,:] = vscale * vcode[c,:], the scales those of c's block of scale_block tokens and kv head (see war_rope_store; any
+ * scales >= 0 will do here, powers of two or not).  Half the bytes of the bf16 cache, and the codes go to the tensor
+ * cores as they are: q and the softmax weights are each split into two 8-bit parts whose products are summed in 32 bits,
+ * so no precision of the bf16 queries is lost (elements below 2^-9 of a row's largest are held to 2^-18 of it) and the
+ * weights are held to 2^-8, as bf16 would.
+ * Arguments, masks, outputs, untouched rows, workspace rules and limits as in war_verify_attn, and:
+ *   kv_type 1 (e4m3) or 2 (e5m2); scales float32 [num_pages, Hkv, page_size / scale_block], scale_block 8 .. page_size
+ *   pools by strides: unit stride along d, the others multiples of 16 bytes, the base on 16 bytes
+ *   rows and scales of positions at or beyond prefix_len + num_nodes may hold anything, NaN codes included; V rows and
+ *   scales of live positions must be finite (a hidden slot's weight is 0, and 0 * NaN is NaN)
+ *   a query row that holds NaN or infinity gives NaN
+ *   kernel: 0 and 2 as there, 1 = plain CUDA-core kernel
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct {
+    war_attn_params_t attn;                            /* strides in elements (bytes) of the 8-bit pools */
+    int32_t kv_type, scale_block;
+} war_attn_quant_params_t;
+size_t war_verify_attn_quant_workspace_bytes(const war_attn_quant_params_t* params);
+war_status_t war_verify_attn_quant(const void* d_q, const void* d_kpool, const void* d_vpool, const float* d_kscale,
+                                   const float* d_vscale, const int32_t* d_page_table, const int32_t* d_prefix_len,
+                                   const int32_t* d_num_nodes, const int32_t* d_parent, const war_attn_quant_params_t* params,
+                                   void* d_workspace, void* d_out, float* d_lse, war_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * The target's choices (what war_accept compares the drafts with, target_mode 0): the largest logit after every slot, once
+ * penalties, biases and a grammar have been applied.  For request b, slot j < num_nodes[b], token v, in this order and in
+ * 32-bit arithmetic, every operation rounded:
+ *     seen  = v occurs in the context or on slot j's path         made = its occurrences at or behind prompt_len[b] in the
+ *             context, plus those on the path                     (path: the slots from the root's child down to j)
+ *     x     = logits[b, j, v]
+ *     x     = x / repetition[b] if x > 0 else x * repetition[b]   when seen
+ *     x     = x - frequency[b] * made                             x = x - presence[b] when made > 0
+ *     x     = x + bias_val[e]                                     e: the last entry of request b's list with bias_ids[e] = v
+ *     x     = -inf                                                when bit v % 32 of mask word v / 32 is 0
+ *   target[b, j] = the v with the largest x, the lowest one of equals; NaN and -inf are never chosen, and -1 means that
+ *   nothing is left.  Slots j >= num_nodes[b] get -1.
+ *   d_out (may be NULL, may be d_logits with the same strides): the x, rounded to the logits' type; rows j >= num_nodes[b]
+ *   are left as they are.
+ * dtype 0 = bf16, 1 = float32 logits [B, N, V] by strides (request, slot); no alignment beyond the type's own.
+ * Contexts as in war_draft_local: d_ctx tokens back to back, d_ctx_off int64 [B+1] on the device, the root is the last token;
+ * tokens outside [0, V) count nowhere.  prompt_len NULL: 0 for all.  Without repetition, presence and frequency (each may be
+ * NULL: 1, 0, 0) contexts and trees are not read and may be NULL; without ids and parent (both or none) paths do not count.
+ * Bias lists: d_bias_off int64 [B+1], entries behind each other; all three arrays or none; at most 65 534 entries a request.
+ * d_mask: words by strides (request, slot); stride 0 shares a mask.  N <= 64, V <= 262144.
+ * A malformed tree (WAR_ERR_BAD_TREE), or offsets that decrease or hold 2^31 tokens or too many bias entries
+ * (WAR_ERR_INVALID_ARG), give -1 for all of the request's slots and leave its rows of d_out.  One launch, no workspace. */
+typedef struct {
+    const int32_t* d_ctx; const int64_t* d_ctx_off; const int32_t* d_prompt_len;
+    const float* d_repetition; const float* d_presence; const float* d_frequency;       /* [B] each */
+    const int64_t* d_bias_off; const int32_t* d_bias_ids; const float* d_bias_val;
+    const void* d_mask;                                                                 /* 32-bit words */
+} war_target_inputs_t;
+typedef struct {
+    int32_t B, N, V, dtype;
+    int64_t logits_strides[2], out_strides[2], mask_strides[2];
+} war_target_params_t;
+war_status_t war_target(const void* d_logits, const int32_t* d_num_nodes, const int32_t* d_ids, const int32_t* d_parent,
+                        const war_target_inputs_t* inputs, const war_target_params_t* params, int32_t* d_target, void* d_out,
+                        war_stream_t stream);
+
+/* war_commit for the 8-bit cache: the same arguments and bookkeeping, with the scales.  A block that receives rows gets the
+ * largest scale among the blocks its live rows (positions up to prefix_len + accept_len) come from, and live rows that come
+ * from, or stay in, a block with another scale are re-encoded by the ratio of the two, rounded to nearest even; rows of
+ * rejected slots keep their codes (they are dead).  params: war_commit's, strides in elements (bytes) of the 8-bit pools, any
+ * with unit stride along d and the others multiples of 16 bytes.  A request that war_commit would leave as it is is left
+ * as it is here, its KV rows included.  One launch. */
+typedef struct {
+    war_commit_params_t commit;
+    int32_t kv_type, scale_block;
+} war_commit_quant_params_t;
+war_status_t war_commit_quant(const int32_t* d_ids, const int32_t* d_accept_len, const int32_t* d_accept_path,
+                              const int32_t* d_bonus, void* d_kpool, void* d_vpool, float* d_kscale, float* d_vscale,
+                              const int32_t* d_page_table, const war_commit_quant_params_t* params, int32_t* d_prefix_len,
+                              int32_t* d_tail, int32_t* d_tail_len, war_stream_t stream);
 
 /* Diagnostic, no counterpart in the paper: exercises the bounded waits of the attention kernel without the kernel.
  * Every wait inside the tensor-core kernel (on a tile that has not arrived, on a result that is not ready) gives up

@@ -28,6 +28,8 @@ STATUS_NAMES = {0: "WAR_OK", 1: "WAR_ERR_INVALID_ARG", 2: "WAR_ERR_OOM", 3: "WAR
 EXPORTS = ["war_index_build", "war_index_append", "war_index_append_async", "war_index_evict", "war_index_export_bytes", "war_index_export",
            "war_index_import", "war_index_info", "war_index_destroy", "war_draft", "war_draft_scored_workspace_bytes", "war_draft_scored", "war_draft_local", "war_draft_pick",
            "war_verify_attn_workspace_bytes", "war_verify_attn", "war_verify_attn_noalloc", "war_accept", "war_commit", "war_device_status",
+           "war_rope_store", "war_rope_frequencies", "war_verify_attn_quant_workspace_bytes", "war_verify_attn_quant", "war_target",
+           "war_commit_quant",
            "war_selftest_bounded_wait",
            "war_status_string"]
 
@@ -375,3 +377,236 @@ def new_workspace(params: AttnParams, device) -> torch.Tensor:
     if n == 0:
         raise WarError("war_verify_attn_workspace_bytes", 6)
     return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# rotary store, 8-bit cache, target choice
+# ---------------------------------------------------------------------------------------------------------------
+KV_TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.float8_e5m2: 2}
+ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
+
+
+class RopeStoreParams(C.Structure):
+    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+                ("page_size", C.c_int32), ("max_pages_per_req", C.c_int32), ("kv_type", C.c_int32), ("scale_block", C.c_int32),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_float), ("num_pages", C.c_int64),
+                ("q_strides", C.c_int64 * 4), ("k_strides", C.c_int64 * 4), ("v_strides", C.c_int64 * 4),
+                ("kpool_strides", C.c_int64 * 4), ("vpool_strides", C.c_int64 * 4)]
+
+
+class RopeFreqParams(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("rot_dim", C.c_int32), ("base", C.c_double), ("scale", C.c_double),
+                ("original_length", C.c_double), ("fast", C.c_double), ("slow", C.c_double)]
+
+
+class AttnQuantParams(C.Structure):
+    _fields_ = [("attn", AttnParams), ("kv_type", C.c_int32), ("scale_block", C.c_int32)]
+
+
+class TargetInputs(C.Structure):
+    _fields_ = [("d_ctx", C.c_void_p), ("d_ctx_off", C.c_void_p), ("d_prompt_len", C.c_void_p), ("d_repetition", C.c_void_p),
+                ("d_presence", C.c_void_p), ("d_frequency", C.c_void_p), ("d_bias_off", C.c_void_p), ("d_bias_ids", C.c_void_p),
+                ("d_bias_val", C.c_void_p), ("d_mask", C.c_void_p)]
+
+
+class TargetParams(C.Structure):
+    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("logits_strides", C.c_int64 * 2),
+                ("out_strides", C.c_int64 * 2), ("mask_strides", C.c_int64 * 2)]
+
+
+class CommitQuantParams(C.Structure):
+    _fields_ = [("commit", CommitParams), ("kv_type", C.c_int32), ("scale_block", C.c_int32)]
+
+
+_lib.war_rope_store.restype = C.c_int
+_lib.war_rope_store.argtypes = [C.c_void_p] * 8 + [C.POINTER(RopeStoreParams)] + [C.c_void_p] * 6
+_lib.war_rope_frequencies.restype = C.c_int
+_lib.war_rope_frequencies.argtypes = [C.POINTER(RopeFreqParams), C.c_void_p, C.c_void_p]
+_lib.war_verify_attn_quant_workspace_bytes.restype = C.c_size_t
+_lib.war_verify_attn_quant_workspace_bytes.argtypes = [C.POINTER(AttnQuantParams)]
+_lib.war_verify_attn_quant.restype = C.c_int
+_lib.war_verify_attn_quant.argtypes = [C.c_void_p] * 9 + [C.POINTER(AttnQuantParams)] + [C.c_void_p] * 4
+_lib.war_target.restype = C.c_int
+_lib.war_target.argtypes = [C.c_void_p] * 4 + [C.POINTER(TargetInputs), C.POINTER(TargetParams)] + [C.c_void_p] * 3
+_lib.war_commit_quant.restype = C.c_int
+_lib.war_commit_quant.argtypes = [C.c_void_p] * 9 + [C.POINTER(CommitQuantParams)] + [C.c_void_p] * 4
+
+
+def _strided(t: torch.Tensor, ndim: int, *dtypes) -> int:
+    """Address of a device tensor that is passed with its strides."""
+    if not t.is_cuda or t.dim() != ndim:
+        raise ValueError(f"expected a {ndim}-dimensional CUDA tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"expected {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    return t.data_ptr()
+
+
+def _pool_args(k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale, v_scale):
+    """(kv_type, scale_block) of a cache; checks that the two pools and their scales belong together."""
+    kv = KV_TYPES.get(k_pool.dtype)
+    if kv is None or v_pool.dtype != k_pool.dtype or v_pool.shape != k_pool.shape or k_pool.dim() != 4:
+        raise ValueError("pools must be [pages, Hkv, page_size, D] of one shape and one of the types " + ", ".join(map(str, KV_TYPES)))
+    if kv == 0:
+        if k_scale is not None or v_scale is not None:
+            raise ValueError("a bf16 cache has no scales")
+        return kv, 0
+    pages, Hkv, pg, _ = k_pool.shape
+    for t in (k_scale, v_scale):
+        if t is None or t.dim() != 3 or t.shape[:2] != (pages, Hkv) or t.shape[2] < 1 or pg % t.shape[2] or t.shape != k_scale.shape:
+            raise ValueError("scales must be float32 [pages, Hkv, page_size / scale_block], the same for K and V")
+    return kv, pg // k_scale.shape[2]
+
+
+def _shape(t: Optional[torch.Tensor], *want) -> None:
+    if t is not None and tuple(t.shape) != want:
+        raise ValueError(f"expected shape {want}, got {tuple(t.shape)}")
+
+
+def war_rope_frequencies(rot_dim: int, base: float, kind: str = "plain", scale: float = 1.0, original_length: float = 0.0,
+                         fast: float = 32.0, slow: float = 1.0) -> Tuple[torch.Tensor, float]:
+    """(inv_freq float32 [rot_dim / 2] on the host, factor) for war_rope_store; kinds: ROPE_KINDS (see include/war.h)."""
+    out = torch.zeros(rot_dim // 2, dtype=torch.float32)
+    f = C.c_float(1.0)
+    p = RopeFreqParams(ROPE_KINDS[kind], rot_dim, base, scale, original_length, fast, slow)
+    _check("war_rope_frequencies", _lib.war_rope_frequencies(C.byref(p), out.data_ptr(), C.addressof(f)))
+    return out, float(f.value)
+
+
+def war_rope_store(d_q: Optional[torch.Tensor], d_k: torch.Tensor, d_v: torch.Tensor, d_inv_freq: torch.Tensor, page_table: torch.Tensor,
+                   d_prefix_len: torch.Tensor, d_num_nodes: torch.Tensor, d_parent: torch.Tensor, k_pool: torch.Tensor,
+                   v_pool: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor],
+                   d_q_out: Optional[torch.Tensor], interleaved: bool = False, factor: float = 1.0) -> None:
+    """Rotates q (to d_q_out) and k at the slots' places in the text and writes k and v behind prefix_len.  d_q, d_k, d_v:
+    bf16 [B, N, H, D], any strides the library accepts (the parts of one projection, say); rot_dim = 2 * len(d_inv_freq).
+    Pools [pages, Hkv, page_size, D]: bf16 (no scales), or float8_e4m3fn / float8_e5m2 with float32 scales
+    [pages, Hkv, page_size / scale_block]; updated in place.  d_q and d_q_out None: nothing but the store."""
+    B, N, Hkv, D = d_k.shape
+    kv, block = _pool_args(k_pool, v_pool, k_scale, v_scale)
+    _shape(d_v, B, N, Hkv, D)
+    _shape(k_pool, k_pool.shape[0], Hkv, k_pool.shape[2], D)
+    _shape(d_prefix_len, B)
+    _shape(d_num_nodes, B)
+    _shape(d_parent, B, N)
+    if page_table.dim() != 2 or page_table.shape[0] != B or (d_q is None) != (d_q_out is None):
+        raise ValueError("page_table must be [B, max_pages]; d_q and d_q_out come together")
+    p = RopeStoreParams()
+    p.B, p.N, p.Hkv, p.D = B, N, Hkv, D
+    if d_q is not None:
+        _shape(d_q, B, N, d_q.shape[2], D)
+        _shape(d_q_out, B, N, d_q.shape[2], D)
+        p.Hq = d_q.shape[2]
+        for i in range(4):
+            p.q_strides[i] = d_q.stride(i)
+    else:
+        p.Hq, p.q_strides[3] = 0, 1
+    p.page_size, p.max_pages_per_req, p.num_pages = k_pool.shape[2], page_table.shape[1], k_pool.shape[0]
+    p.kv_type, p.scale_block, p.rot_dim, p.interleaved, p.factor = kv, block, 2 * d_inv_freq.numel(), int(interleaved), factor
+    for i in range(4):
+        p.k_strides[i], p.v_strides[i] = d_k.stride(i), d_v.stride(i)
+        p.kpool_strides[i], p.vpool_strides[i] = k_pool.stride(i), v_pool.stride(i)
+    bf16 = torch.bfloat16
+    code = _lib.war_rope_store(None if d_q is None else _strided(d_q, 4, bf16), _strided(d_k, 4, bf16), _strided(d_v, 4, bf16),
+                               _ptr(d_inv_freq, torch.float32), _ptr(page_table, torch.int32), _ptr(d_prefix_len, torch.int32),
+                               _ptr(d_num_nodes, torch.int32), _ptr(d_parent, torch.int32), C.byref(p),
+                               _strided(k_pool, 4, *KV_TYPES), _strided(v_pool, 4, *KV_TYPES), _ptr(k_scale, torch.float32),
+                               _ptr(v_scale, torch.float32), _ptr(d_q_out, bf16), _stream())
+    _check("war_rope_store", code)
+
+
+def attn_quant_params(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                      page_table: torch.Tensor, scale: float, kernel: int = 0) -> AttnQuantParams:
+    kv, block = _pool_args(k_pool, v_pool, k_scale, v_scale)
+    if kv == 0:
+        raise ValueError("pools must hold 8-bit codes; war_verify_attn reads a bf16 cache")
+    if q.shape[3] != k_pool.shape[3] or page_table.dim() != 2 or page_table.shape[0] != q.shape[0]:
+        raise ValueError("q [B, N, Hq, D], pools [pages, Hkv, page_size, D], page_table [B, max_pages]")
+    return AttnQuantParams(attn_params(q, k_pool, v_pool, page_table, scale, kernel), kv, block)
+
+
+def war_verify_attn_quant_workspace_bytes(params: AttnQuantParams) -> int:
+    return int(_lib.war_verify_attn_quant_workspace_bytes(C.byref(params)))
+
+
+def new_quant_workspace(params: AttnQuantParams, device) -> torch.Tensor:
+    """A device buffer of the size war_verify_attn_quant asks for."""
+    n = war_verify_attn_quant_workspace_bytes(params)
+    if n == 0:
+        raise WarError("war_verify_attn_quant_workspace_bytes", 6)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def war_verify_attn_quant(d_q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                          d_page_table: torch.Tensor, d_prefix_len: torch.Tensor, d_num_nodes: torch.Tensor, d_parent: torch.Tensor,
+                          params: AttnQuantParams, d_workspace: torch.Tensor, d_out: torch.Tensor, d_lse: Optional[torch.Tensor]) -> None:
+    """war_verify_attn over a float8_e4m3fn / float8_e5m2 cache; params from attn_quant_params for these tensors."""
+    if d_workspace.numel() * d_workspace.element_size() < war_verify_attn_quant_workspace_bytes(params):
+        raise ValueError("workspace is smaller than war_verify_attn_quant_workspace_bytes")
+    code = _lib.war_verify_attn_quant(_ptr(d_q, torch.bfloat16), _strided(k_pool, 4, torch.float8_e4m3fn, torch.float8_e5m2),
+                                      _strided(v_pool, 4, torch.float8_e4m3fn, torch.float8_e5m2), _ptr(k_scale, torch.float32),
+                                      _ptr(v_scale, torch.float32), _ptr(d_page_table, torch.int32), _ptr(d_prefix_len, torch.int32),
+                                      _ptr(d_num_nodes, torch.int32), _ptr(d_parent, torch.int32), C.byref(params), _ptr(d_workspace),
+                                      _ptr(d_out, torch.bfloat16), _ptr(d_lse, torch.float32), _stream())
+    _check("war_verify_attn_quant", code)
+
+
+def war_target(d_logits: torch.Tensor, d_num_nodes: torch.Tensor, d_ids: Optional[torch.Tensor], d_parent: Optional[torch.Tensor],
+               d_target: torch.Tensor, d_ctx: Optional[torch.Tensor] = None, d_ctx_off: Optional[torch.Tensor] = None,
+               d_prompt_len: Optional[torch.Tensor] = None, d_repetition: Optional[torch.Tensor] = None,
+               d_presence: Optional[torch.Tensor] = None, d_frequency: Optional[torch.Tensor] = None,
+               d_bias_off: Optional[torch.Tensor] = None, d_bias_ids: Optional[torch.Tensor] = None,
+               d_bias_val: Optional[torch.Tensor] = None, d_mask: Optional[torch.Tensor] = None,
+               d_out: Optional[torch.Tensor] = None) -> None:
+    """Penalties, biases and grammar masks on d_logits (bf16 or float32 [B, N, V], unit stride along V), the chosen token of
+    every slot into d_target [B, N] (what war_accept takes), the processed logits into d_out where it is given.
+    d_mask: int32 words [B, N, ceil(V / 32)], unit stride along the words; expand() shares one mask."""
+    B, N, V = d_logits.shape
+    f32, i32, i64 = torch.float32, torch.int32, torch.int64
+    p = TargetParams()
+    p.B, p.N, p.V, p.dtype = B, N, V, int(d_logits.dtype == f32)
+    words = (V + 31) // 32
+    for t, strides, last in ((d_logits, p.logits_strides, V), (d_out, p.out_strides, V), (d_mask, p.mask_strides, words)):
+        if t is None:
+            continue
+        _shape(t, B, N, last)
+        if t.stride(2) != 1 and last > 1:
+            raise ValueError("logits, mask and out need unit stride along their last dimension")
+        strides[0], strides[1] = t.stride(0), t.stride(1)
+    if d_out is not None and d_out.dtype != d_logits.dtype:
+        raise ValueError("d_out must have the logits' type")
+    _shape(d_target, B, N)
+    for t in (d_ids, d_parent):
+        _shape(t, B, N)
+    for t in (d_num_nodes, d_prompt_len, d_repetition, d_presence, d_frequency):
+        _shape(t, B)
+    for t in (d_ctx_off, d_bias_off):
+        _shape(t, B + 1)
+    inputs = TargetInputs(_ptr(d_ctx, i32), _ptr(d_ctx_off, i64), _ptr(d_prompt_len, i32), _ptr(d_repetition, f32), _ptr(d_presence, f32),
+                          _ptr(d_frequency, f32), _ptr(d_bias_off, i64), _ptr(d_bias_ids, i32), _ptr(d_bias_val, f32),
+                          None if d_mask is None else _strided(d_mask, 3, i32))
+    if d_bias_off is not None and d_bias_ids is not None and d_bias_val is not None and d_bias_ids.numel() == 0:
+        inputs.d_bias_off = inputs.d_bias_ids = inputs.d_bias_val = None             # (an empty tensor has no address)
+    code = _lib.war_target(_strided(d_logits, 3, torch.bfloat16, f32), _ptr(d_num_nodes, i32), _ptr(d_ids, i32), _ptr(d_parent, i32),
+                           C.byref(inputs), C.byref(p), _ptr(d_target, i32),
+                           None if d_out is None else _strided(d_out, 3, torch.bfloat16, f32), _stream())
+    _check("war_target", code)
+
+
+def war_commit_quant(d_ids: torch.Tensor, d_accept_len: torch.Tensor, d_accept_path: torch.Tensor, d_bonus: torch.Tensor,
+                     k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page_table: torch.Tensor,
+                     d_prefix_len: torch.Tensor, d_tail: torch.Tensor, d_tail_len: torch.Tensor) -> None:
+    """war_commit for a float8_e4m3fn / float8_e5m2 cache; pools and scales are updated in place."""
+    B, N = d_ids.shape
+    q = CommitQuantParams()
+    q.kv_type, q.scale_block = _pool_args(k_pool, v_pool, k_scale, v_scale)
+    p = q.commit
+    p.B, p.N, p.P = B, N, d_tail.shape[1]
+    p.Hkv, p.D, p.page_size = k_pool.shape[1], k_pool.shape[3], k_pool.shape[2]
+    p.max_pages_per_req, p.num_pages = page_table.shape[1], k_pool.shape[0]
+    for i in range(4):
+        p.k_strides[i] = k_pool.stride(i)
+        p.v_strides[i] = v_pool.stride(i)
+    code = _lib.war_commit_quant(_ptr(d_ids, torch.int32), _ptr(d_accept_len, torch.int32), _ptr(d_accept_path, torch.int32),
+                                 _ptr(d_bonus, torch.int32), _strided(k_pool, 4, *KV_TYPES), _strided(v_pool, 4, *KV_TYPES),
+                                 _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), _ptr(page_table, torch.int32), C.byref(q),
+                                 _ptr(d_prefix_len, torch.int32), _ptr(d_tail, torch.int32), _ptr(d_tail_len, torch.int32), _stream())
+    _check("war_commit_quant", code)

@@ -139,7 +139,7 @@ __host__ __device__ __forceinline__ bool contiguous_split_pays(int rows_max, lon
 }
 
 constexpr int kFusedMaxChunks = 192;      // chunks per request at most (what the merge of a row group can hold at once)
-__device__ __forceinline__ int chunk_floor(int t_max) { return max(4, (t_max + kFusedMaxChunks - 1) / kFusedMaxChunks); }
+__device__ __forceinline__ int chunk_floor(int t_max, int max_chunks = kFusedMaxChunks) { return max(4, (t_max + max_chunks - 1) / max_chunks); }
 
 // Contiguous split with the cost of a unit in it.  A CTA pays for every unit it runs about as much as for
 // `unit_cost` tiles (its pipeline drains and fills again: epilogue, next Q tile, first loads; measured 12 to 21 us per
@@ -239,6 +239,7 @@ __device__ __forceinline__ bool next_unit(const FusedPlan* pl, Cursor& c, int B,
 // and launch, straight from a cold instruction cache, so its cost is its length: it reads only the two numbers per
 // request the plan depends on (the parent arrays are checked by the warps that use them, unit by unit), keeps to
 // 32-bit arithmetic and rolled loops, and has two block barriers on the contiguous path and five on the other.
+template <int kMaxChunks = kFusedMaxChunks>
 __device__ __noinline__ static void make(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ num_nodes,
                                         int B, int N, int Hkv, int G, int page_size, int max_pages,
                                         FusedPlanScratch* sc, FusedPlan* pl, int* status_word) {
@@ -340,11 +341,11 @@ __device__ __noinline__ static void make(const int32_t* __restrict__ prefix_len,
         return;
     }
 
-    // ---- searched chunk length (see chunk_search), never more than kFusedMaxChunks chunks per request ----
+    // ---- searched chunk length (see chunk_search), never more than kMaxChunks chunks per request ----
     long long ct = (tot + kTargetUnits - 1) / kTargetUnits;
     if (ct < kMinChunkTiles) ct = kMinChunkTiles;
     const int chunk_tiles = (int)ct;
-    const int best_c = chunk_search<kFusedThreads>(pl->tiles, sc->weight, B, max(chunk_floor(t_max), chunk_tiles), t_max, n_ctas, sc->keys);
+    const int best_c = chunk_search<kFusedThreads>(pl->tiles, sc->weight, B, max(chunk_floor(t_max, kMaxChunks), chunk_tiles), t_max, n_ctas, sc->keys);
     const int c_best = best_c;
     // ---- longest-first order, units per request, their offsets ----
     if (tid < B) {

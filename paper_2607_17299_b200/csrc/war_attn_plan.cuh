@@ -95,3 +95,8 @@ war_status_t war_attn_launch_sm100(const void* q, const void* k, const void* v, 
                                    const war_attn_params_t* p, const AttnWorkspace& w, bool fused,
                                    void* out, float* lse, int* status_word, cudaStream_t s);
 int war_attn_sm_count();                 // SMs of the current device (0 on error)
+
+// The planning and combine launches around either attention kernel (war_verify_attn.cu).
+war_status_t war_attn_launch_plan(const int32_t* prefix_len, const int32_t* num_nodes, const int32_t* parent, const war_attn_params_t* p,
+                                  const AttnWorkspace& w, int n_sm, int* status_word, cudaStream_t s);
+war_status_t war_attn_launch_combine(const war_attn_params_t* p, const AttnWorkspace& w, void* out, float* lse, cudaStream_t s);

@@ -1,0 +1,381 @@
+// The target's choice after every slot of a draft tree: penalties, biases and grammar masks on the logits, then the
+// largest value (and, if asked for, the processed logits).
+//
+// The logits are the traffic (64 times 131072 values a request against a few thousand context tokens), so a row is read
+// once, 16 bytes a lane, and what the penalties need is looked up on chip: a cluster of up to eight thread blocks takes
+// one request, each block a slice of the vocabulary.  Together they read the request's context once and count its tokens
+// into the slice that owns them (shared-memory atomics across the cluster); from then on a block holds, for its slice, a
+// counter and the bias entry of every token and one bit that says whether the token needs either.  Eight bits decide for
+// eight logits whether the fast path is enough: no penalty, no bias, only the grammar's mask and the comparison.  Rows are
+// independent of each other (tokens on a slot's path are looked up in the tree, not written into the counters), so warps
+// take pieces of rows without a barrier; the winners of a row meet in one 64-bit maximum per block, and the cluster's
+// first block compares the slices.  Ties go to the lowest token, whatever the order of the atomics.
+#include <cuda_bf16.h>
+#include <cooperative_groups.h>
+#include "war_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int kMaxSlots = 64;
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxSlices = 8;                 // thread blocks of a cluster
+constexpr int kMaxSlice = 32768;              // tokens a block can hold: 6 bytes and 2 bits each of 227 KB
+constexpr int kMaxVocab = kMaxSlices * kMaxSlice;
+constexpr int kSegment = 1024;                // logits of a row that a warp takes at a time
+constexpr int kMaxBias = 65534;               // bias entries of a request (numbered in 16 bits)
+constexpr uint32_t kSeen = 0x80000000u;
+
+struct TargetArgs {
+    const void* logits; void* out;
+    const int32_t *num_nodes, *ids, *parent, *ctx, *prompt_len, *bias_ids;
+    const int64_t *ctx_off, *bias_off;
+    const float *repetition, *presence, *frequency, *bias_val;
+    const uint32_t* mask;
+    int32_t* target;
+    int* status_word;
+    long long ls[2], os[2], ms[2];            // strides (request, slot) of logits and out in elements, of the mask in words
+    int N, V, slice, words;                   // words: mask words of a row
+    int count;                                // 1: count context tokens (a penalty is given)
+    int path;                                 // 1: ids are given (tokens on a slot's path count too)
+};
+
+struct Shared {
+    unsigned long long best[kMaxSlots];       // (ordered value << 32) | ~token; 0: none
+    unsigned long long anc[kMaxSlots];
+    int ids[kMaxSlots];
+    int bad;
+};
+
+template <class T> struct Wide;
+template <> struct Wide<float> {
+    static constexpr int kPer = 4;
+    static __device__ __forceinline__ void widen(const uint4& u, float* x) {
+        x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+    }
+    static __device__ __forceinline__ uint4 narrow(const float* x) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+    static __device__ __forceinline__ float load(const float* p) { return *p; }
+    static __device__ __forceinline__ void store(float* p, float x) { *p = x; }
+};
+template <> struct Wide<__nv_bfloat16> {
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ void widen(const uint4& u, float* x) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ uint4 narrow(const float* x) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+    static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+};
+
+// order-preserving map of a float that is no NaN and above -inf to an unsigned number above 0 (-0 counts as 0)
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// 32 bits of a bit string from bit v on; words past `words` read as 0
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* w, int v, int words) {
+    const int k = v >> 5, sh = v & 31;
+    uint32_t x = w[k] >> sh;
+    if (sh && k + 1 < words) x |= w[k + 1] << (32 - sh);
+    return x;
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads)
+war_target_kernel(const TargetArgs a) {
+    extern __shared__ __align__(16) uint32_t smem[];
+    __shared__ Shared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), slices = (int)cluster.num_blocks();
+    const int b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int W = a.slice, bit_words = W / 32;
+    uint32_t* special = smem;                                             // [bit_words + 1] counter, bias or tree token
+    uint32_t* tree = special + bit_words + 1;                             // [bit_words + 1] some slot's token
+    uint32_t* counter = tree + bit_words + 1;                             // [W] generated occurrences, bit 31: in the context
+    uint16_t* bias_at = reinterpret_cast<uint16_t*>(counter + (a.count ? W : 0));   // [W] bias entry + 1
+    const int v0 = rank * W, v1 = min(a.V, v0 + W);
+
+    const int n_in = a.num_nodes[b];
+    long long c0 = 0, c1 = 0;
+    if (a.count) { c0 = a.ctx_off[b]; c1 = a.ctx_off[b + 1]; }
+    long long e0 = 0, e1 = 0;
+    if (a.bias_off) { e0 = a.bias_off[b]; e1 = a.bias_off[b + 1]; }
+    int bad = 0;
+    if (n_in < 0 || n_in > a.N) bad = WAR_ERR_BAD_TREE;
+    if (c1 < c0 || c1 - c0 >= (1ll << 31) || e1 < e0 || e1 - e0 > kMaxBias) bad = WAR_ERR_INVALID_ARG;
+    for (int x = tid; x < 2 * (bit_words + 1); x += kThreads) special[x] = 0;
+    if (a.count) for (int x = tid; x < W; x += kThreads) counter[x] = 0;
+    if (a.bias_off) for (int x = tid; x < W / 2; x += kThreads) reinterpret_cast<uint32_t*>(bias_at)[x] = 0;
+    if (tid < kMaxSlots) { sh.best[tid] = 0; sh.ids[tid] = -1; }
+    if (warp == 0) {
+        // ancestor-or-self masks by pointer jumping; the root's bit is cleared (it is the context's last token)
+        const int n = bad ? 0 : n_in;
+        const int32_t* prow = a.parent + (size_t)b * a.N;
+        int p0 = 0, p1 = 0;
+        bool wrong = false;
+        if (a.path) {
+            p0 = lane > 0 && lane < n ? prow[lane] : 0; p1 = lane + 32 < n ? prow[lane + 32] : 0;
+            wrong = (lane > 0 && lane < n && (p0 < 0 || p0 >= lane)) || (lane + 32 < n && (p1 < 0 || p1 >= lane + 32));
+        }
+        wrong = __any_sync(0xffffffffu, wrong);
+        if (wrong) { p0 = 0; p1 = 0; }
+        unsigned long long m0 = 1ull << lane, m1 = 1ull << (lane + 32);
+        for (int r = 0; r < 6; ++r) {
+            const unsigned long long m00 = __shfl_sync(0xffffffffu, m0, p0 & 31), m01 = __shfl_sync(0xffffffffu, m1, p0 & 31);
+            const unsigned long long m10 = __shfl_sync(0xffffffffu, m0, p1 & 31), m11 = __shfl_sync(0xffffffffu, m1, p1 & 31);
+            const int q00 = __shfl_sync(0xffffffffu, p0, p0 & 31), q01 = __shfl_sync(0xffffffffu, p1, p0 & 31);
+            const int q10 = __shfl_sync(0xffffffffu, p0, p1 & 31), q11 = __shfl_sync(0xffffffffu, p1, p1 & 31);
+            m0 |= p0 >= 32 ? m01 : m00; m1 |= p1 >= 32 ? m11 : m10;
+            p0 = p0 >= 32 ? q01 : q00; p1 = p1 >= 32 ? q11 : q10;
+        }
+        sh.anc[lane] = m0 & ~1ull; sh.anc[lane + 32] = m1 & ~1ull;
+        if (lane == 0) sh.bad = bad ? bad : (wrong ? WAR_ERR_BAD_TREE : 0);
+    }
+    cluster.sync();                                                       // every block's tables are cleared
+    bad = sh.bad;
+    const int n = bad ? 0 : n_in;
+
+    if (n > 0) {
+        if (a.count) {
+            // this block's share of the context, counted into the blocks that own the tokens
+            const long long len = c1 - c0;
+            const int from = (int)(len * rank / slices), to = (int)(len * (rank + 1) / slices);
+            const int made = a.prompt_len ? a.prompt_len[b] : 0;
+            const int32_t* ctx = a.ctx + c0;
+            for (int x = from + tid; x < to; x += kThreads) {
+                const int tok = ctx[x];
+                if (tok < 0 || tok >= a.V) continue;
+                const int owner = tok / W;
+                uint32_t* at = cluster.map_shared_rank(counter + (tok - owner * W), owner);
+                if (x >= made) atomicAdd(at, 1u);
+                else atomicOr(at, kSeen);
+            }
+        }
+        if (a.bias_off && warp == kWarps - 1) {
+            // bias entries in order, so that the last one of a token counts: 32 at a time, the highest lane of equal tokens writes
+            for (long long e = e0; e < e1; e += 32) {
+                const int tok = e + lane < e1 ? a.bias_ids[e + lane] : -1 - lane;
+                const unsigned same = __match_any_sync(0xffffffffu, tok);
+                if (tok >= v0 && tok < v1 && 31 - __clz(same) == lane) {
+                    bias_at[tok - v0] = (uint16_t)(e + lane - e0 + 1);
+                    atomicOr(&special[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
+                }
+                __syncwarp();
+            }
+        }
+        if (a.path && tid < kMaxSlots && tid > 0 && tid < n) {
+            const int tok = a.ids[(size_t)b * a.N + tid];
+            sh.ids[tid] = tok;
+            if (a.count && tok >= v0 && tok < v1) {
+                atomicOr(&special[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
+                atomicOr(&tree[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
+            }
+        }
+    }
+    cluster.sync();                                                       // all counts have arrived
+    if (n > 0 && a.count) {
+        for (int x = warp; x < bit_words; x += kWarps) {
+            const unsigned hit = __ballot_sync(0xffffffffu, counter[x * 32 + lane] != 0);
+            if (lane == 0 && hit) atomicOr(&special[x], hit);
+        }
+    }
+    __syncthreads();
+
+    const float rep = a.repetition ? a.repetition[b] : 1.f, pres = a.presence ? a.presence[b] : 0.f, freq = a.frequency ? a.frequency[b] : 0.f;
+    // the value of a token that needs a counter or a bias
+    auto process = [&](float x, int v, int j) -> float {
+        const int l = v - v0;
+        if (a.count) {
+            const uint32_t c = counter[l];
+            uint32_t made = c & ~kSeen;
+            bool seen = c != 0;
+            if ((tree[l >> 5] >> (l & 31)) & 1u) {
+                unsigned long long m = sh.anc[j];
+                while (m) {
+                    const int s = __ffsll((long long)m) - 1;
+                    m &= m - 1;
+                    made += sh.ids[s] == v;
+                }
+                seen = seen || made != 0;
+            }
+            if (seen) x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
+            x = __fsub_rn(x, __fmul_rn(freq, (float)made));
+            if (made) x = __fsub_rn(x, pres);
+        }
+        if (a.bias_off) {
+            const int e = bias_at[l];
+            if (e) x = __fadd_rn(x, a.bias_val[e0 + e - 1]);
+        }
+        return x;
+    };
+
+    constexpr int kPer = Wide<T>::kPer;
+    constexpr int kLoads = kSegment / (32 * kPer);
+    const int z = blockIdx.z, zs = gridDim.z;
+    const int segments = v1 > v0 ? (v1 - v0 + kSegment - 1) / kSegment + 1 : 0;     // one more: rows need not start on 16 bytes
+    const int rows = (n - z + zs - 1) / zs;                               // rows z, z + zs, ... below n
+    for (int task = warp; task < rows * segments; task += kWarps) {
+        const int rj = task / segments, seg = task - rj * segments, j = z + rj * zs;
+        const T* row = reinterpret_cast<const T*>(a.logits) + b * a.ls[0] + j * a.ls[1];
+        T* out = a.out ? reinterpret_cast<T*>(a.out) + b * a.os[0] + j * a.os[1] : nullptr;
+        const uint32_t* mask = a.mask ? a.mask + b * a.ms[0] + j * a.ms[1] : nullptr;
+        // elements between the 16-byte boundary at or before the slice's first logit and that logit
+        const int skew = (int)(((uintptr_t)(row + v0) & 15) / sizeof(T));
+        const int first = v0 - skew + seg * kSegment;                     // a 16-byte boundary
+        if (first >= v1) continue;
+        const bool out_wide = out && (((uintptr_t)(out + first)) & 15) == 0;
+        float best = -INFINITY;
+        int best_v = 0x7fffffff;
+        uint4 in[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int v = first + (u * 32 + lane) * kPer;
+            if (v >= v0 && v + kPer <= v1) in[u] = __ldcs(reinterpret_cast<const uint4*>(row + v));
+        }
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int v = first + (u * 32 + lane) * kPer;
+            if (v >= v0 && v + kPer <= v1) {
+                float x[kPer];
+                Wide<T>::widen(in[u], x);
+                const uint32_t full = (1u << kPer) - 1;
+                const uint32_t odd = bits_at(special, v - v0, bit_words + 1) & full;
+                const uint32_t allowed = mask ? bits_at(mask, v, a.words) & full : full;
+                if (odd) {
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i)
+                        if ((odd >> i) & 1u) x[i] = process(x[i], v + i, j);
+                }
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    if (!((allowed >> i) & 1u)) x[i] = -INFINITY;
+                    if (x[i] > best) { best = x[i]; best_v = v + i; }
+                }
+                if (out) {
+                    if (out_wide) *reinterpret_cast<uint4*>(out + v) = Wide<T>::narrow(x);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) Wide<T>::store(out + v + i, x[i]);
+                    }
+                }
+            } else if (v + kPer > v0 && v < v1) {                         // the slice begins or ends inside these 16 bytes
+                for (int i = max(0, v0 - v); i < kPer && v + i < v1; ++i) {
+                    float y = Wide<T>::load(row + v + i);
+                    const int l = v + i - v0;
+                    if ((special[l >> 5] >> (l & 31)) & 1u) y = process(y, v + i, j);
+                    if (mask && !((mask[(v + i) >> 5] >> ((v + i) & 31)) & 1u)) y = -INFINITY;
+                    if (y > best) { best = y; best_v = v + i; }
+                    if (out) Wide<T>::store(out + v + i, y);
+                }
+            }
+        }
+        // a lane's tokens grow with u, so `>` kept the lowest of equal values
+        unsigned long long key = best > -INFINITY ? ((unsigned long long)ordered(best) << 32) | (uint32_t)~best_v : 0ull;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, o);
+            key = other > key ? other : key;
+        }
+        if (lane == 0 && key) atomicMax(&sh.best[j], key);
+    }
+    cluster.sync();                                                       // every slice's winners are there
+    if (rank == 0) {
+        for (int j = tid; j < a.N; j += kThreads) {
+            if (j % zs != z) continue;
+            unsigned long long key = 0;
+            if (j < n)
+                for (int r = 0; r < slices; ++r) {
+                    const unsigned long long other = *cluster.map_shared_rank(&sh.best[j], r);
+                    key = other > key ? other : key;
+                }
+            a.target[(size_t)b * a.N + j] = key ? (int32_t)~(uint32_t)key : -1;
+        }
+        if (bad && tid == 0) war_set_device_status(a.status_word, bad);
+    }
+    cluster.sync();                                                       // nobody leaves while its winners are read
+}
+
+constexpr int kMaxDevices = 64;
+template <class T>
+war_status_t allow_smem(int bytes) {
+    static int allowed[kMaxDevices];                                     // (two threads may both set the attribute: the same call)
+    int dev = 0;
+    WAR_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices) return WAR_ERR_UNSUPPORTED;
+    if (bytes > 48 * 1024 && !allowed[dev]) {
+        WAR_CUDA_TRY(cudaFuncSetAttribute(war_target_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024));
+        allowed[dev] = 1;
+    }
+    return WAR_OK;
+}
+
+template <class T>
+war_status_t launch(const TargetArgs& a, int slices, int B, int groups, size_t smem, cudaStream_t s) {
+    const war_status_t st = allow_smem<T>((int)smem);
+    if (st != WAR_OK) return st;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(slices, B, groups);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = slices; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, war_target_kernel<T>, a) != cudaSuccess) { (void)cudaGetLastError(); return WAR_ERR_CUDA; }
+    return WAR_OK;
+}
+
+}  // namespace
+
+extern "C" war_status_t war_target(const void* d_logits, const int32_t* d_num_nodes, const int32_t* d_ids, const int32_t* d_parent,
+                                   const war_target_inputs_t* in, const war_target_params_t* p, int32_t* d_target, void* d_out,
+                                   war_stream_t stream) {
+    if (!p || !in) return WAR_ERR_INVALID_ARG;
+    if (p->B < 0 || p->N < 1 || p->N > kMaxSlots || p->V < 1 || (p->dtype != 0 && p->dtype != 1)) return WAR_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i)
+        if (p->logits_strides[i] < 0 || p->out_strides[i] < 0 || p->mask_strides[i] < 0) return WAR_ERR_INVALID_ARG;
+    if (p->V > kMaxVocab || p->B > 65535) return WAR_ERR_UNSUPPORTED;
+    if (p->B == 0) return WAR_OK;
+    const int count = in->d_repetition || in->d_presence || in->d_frequency;
+    if (!d_logits || !d_num_nodes || !d_target || (count && (!in->d_ctx_off || (!d_ids) != (!d_parent)))) return WAR_ERR_INVALID_ARG;
+    if ((in->d_bias_off != nullptr) != (in->d_bias_ids != nullptr) || (in->d_bias_off != nullptr) != (in->d_bias_val != nullptr))
+        return WAR_ERR_INVALID_ARG;
+    const int size = p->dtype == 0 ? 2 : 4;
+    if (((uintptr_t)d_logits | (uintptr_t)d_out) % size) return WAR_ERR_INVALID_ARG;
+    int* status_word = war_status_word();
+    if (!status_word) return WAR_ERR_CUDA;
+    TargetArgs a;
+    a.logits = d_logits; a.out = d_out; a.num_nodes = d_num_nodes; a.ids = d_ids; a.parent = d_parent;
+    a.ctx = in->d_ctx; a.ctx_off = in->d_ctx_off; a.prompt_len = in->d_prompt_len;
+    a.bias_off = in->d_bias_off; a.bias_ids = in->d_bias_ids; a.bias_val = in->d_bias_val;
+    a.repetition = in->d_repetition; a.presence = in->d_presence; a.frequency = in->d_frequency;
+    a.mask = (const uint32_t*)in->d_mask; a.target = d_target; a.status_word = status_word;
+    for (int i = 0; i < 2; ++i) { a.ls[i] = p->logits_strides[i]; a.os[i] = p->out_strides[i]; a.ms[i] = p->mask_strides[i]; }
+    a.N = p->N; a.V = p->V; a.words = (p->V + 31) / 32;
+    a.count = count; a.path = count && d_ids != nullptr;
+    // slices of at least a segment per warp, whole mask words, at most eight
+    int slices = (p->V + kSegment * 2 - 1) / (kSegment * 2);
+    if (slices > kMaxSlices) slices = kMaxSlices;
+    a.slice = ((p->V + slices - 1) / slices + 31) / 32 * 32;
+    int groups = (148 * 4 + slices * p->B - 1) / (slices * p->B);
+    if (groups > p->N) groups = p->N;
+    const size_t smem = (size_t)(a.slice / 32 + 1) * 8 + (count ? (size_t)a.slice * 4 : 0) + (in->d_bias_off ? (size_t)a.slice * 2 : 0);
+    return p->dtype == 0 ? launch<__nv_bfloat16>(a, slices, p->B, groups, smem, stream)
+                         : launch<float>(a, slices, p->B, groups, smem, stream);
+}

@@ -622,6 +622,22 @@ war_status_t war_attn_launch_simple(const void* q, const void* k, const void* v,
     return WAR_OK;
 }
 
+war_status_t war_attn_launch_plan(const int32_t* prefix_len, const int32_t* num_nodes, const int32_t* parent, const war_attn_params_t* p,
+                                  const AttnWorkspace& w, int n_sm, int* status_word, cudaStream_t s) {
+    attn_plan_kernel<<<1, 1024, 0, s>>>(prefix_len, num_nodes, parent, p->B, p->N, p->Hkv, p->Hq / p->Hkv, p->page_size,
+                                       p->max_pages_per_req, n_sm, w, status_word);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
+}
+
+war_status_t war_attn_launch_combine(const war_attn_params_t* p, const AttnWorkspace& w, void* out, float* lse, cudaStream_t s) {
+    const int G = p->Hq / p->Hkv;
+    attn_combine_kernel<<<dim3(p->B * p->Hkv, (G * p->N + kCombineWarps - 1) / kCombineWarps), kCombineWarps * 32, 0, s>>>(
+        w, p->N, p->Hq, p->Hkv, G, (__nv_bfloat16*)out, lse);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
+}
+
 extern "C" size_t war_verify_attn_workspace_bytes(const war_attn_params_t* p) {
     if (check_params(p) != WAR_OK) return 0;
     return war_attn_workspace_layout(p, nullptr).bytes;
@@ -643,7 +659,6 @@ extern "C" war_status_t war_verify_attn(const void* d_q, const void* d_kpool, co
     int* status_word = war_status_word();
     if (!status_word) return WAR_ERR_CUDA;
     const AttnWorkspace w = war_attn_workspace_layout(p, d_workspace);
-    const int G = p->Hq / p->Hkv;
     const int n_sm = war_attn_sm_count();
     if (n_sm <= 0) return WAR_ERR_CUDA;
     // Few requests (the low-load regime the step exists for): one launch.  Every CTA of the attention kernel plans
@@ -652,17 +667,13 @@ extern "C" war_status_t war_verify_attn(const void* d_q, const void* d_kpool, co
     if (p->kernel == 0 && war_attn_fused_ok(p, w.row_blocks, n_sm))
         return war_attn_launch_sm100(d_q, d_kpool, d_vpool, d_page_table, d_prefix_len, d_num_nodes, d_parent, p, w, true, d_out,
                                      d_lse, status_word, stream);
-    attn_plan_kernel<<<1, 1024, 0, stream>>>(d_prefix_len, d_num_nodes, d_parent, p->B, p->N, p->Hkv, G, p->page_size,
-                                            p->max_pages_per_req, n_sm, w, status_word);
-    WAR_LAUNCH_CHECK();
+    st = war_attn_launch_plan(d_prefix_len, d_num_nodes, d_parent, p, w, n_sm, status_word, stream);
+    if (st != WAR_OK) return st;
     if (p->kernel == 1)
         st = war_attn_launch_simple(d_q, d_kpool, d_vpool, d_page_table, d_prefix_len, p, w, d_out, d_lse, status_word, stream);
     else
         st = war_attn_launch_sm100(d_q, d_kpool, d_vpool, d_page_table, d_prefix_len, d_num_nodes, d_parent, p, w, false, d_out,
                                    d_lse, status_word, stream);
     if (st != WAR_OK) return st;
-    attn_combine_kernel<<<dim3(p->B * p->Hkv, (G * p->N + kCombineWarps - 1) / kCombineWarps), kCombineWarps * 32, 0, stream>>>(
-        w, p->N, p->Hq, p->Hkv, G, (__nv_bfloat16*)d_out, d_lse);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_attn_launch_combine(p, w, d_out, d_lse, stream);
 }
