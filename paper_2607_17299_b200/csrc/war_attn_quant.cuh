@@ -9,8 +9,14 @@ struct AttnQuantPools {
     int kv, block;                        // type of the codes, tokens per scale
 };
 
-// fused: one launch, the kernel plans for itself and merges split units itself
-war_status_t war_attn_quant_launch_sm100(const void* q, const AttnQuantPools& pools, const int32_t* page_table,
-                                         const int32_t* prefix_len, const int32_t* num_nodes, const int32_t* parent,
-                                         const war_attn_params_t* p, const AttnWorkspace& w, bool fused,
-                                         void* out, float* lse, int* status_word, cudaStream_t s);
+// The tensor-core kernels: up to kQuantFewRows query rows per kv head, and more.  fused: one launch, the kernel plans for
+// itself and merges split units itself.
+constexpr int kQuantFewRows = 32;
+war_status_t war_attn_quant_launch_few(const void* q, const AttnQuantPools& pools, const int32_t* page_table,
+                                       const int32_t* prefix_len, const int32_t* num_nodes, const int32_t* parent,
+                                       const war_attn_params_t* p, const AttnWorkspace& w, bool fused,
+                                       void* out, float* lse, int* status_word, cudaStream_t s);
+war_status_t war_attn_quant_launch_many(const void* q, const AttnQuantPools& pools, const int32_t* page_table,
+                                        const int32_t* prefix_len, const int32_t* num_nodes, const int32_t* parent,
+                                        const war_attn_params_t* p, const AttnWorkspace& w, bool fused,
+                                        void* out, float* lse, int* status_word, cudaStream_t s);

@@ -1,5 +1,5 @@
 // Verify attention over the 8-bit cache: argument checks, the choice of the path and the plain CUDA-core kernel (kept as
-// the A/B reference of the tensor-core kernel in war_verify_attn_quant_sm100.cu).  The plan, the split of a request
+// the A/B reference of the tensor-core kernels in war_verify_attn_quant_few.cu and _many.cu).  The plan, the split of a request
 // over thread blocks and the merge of its parts are those of the bf16 cache.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -154,7 +154,7 @@ war_status_t check_params(const war_attn_quant_params_t* q) {
     if (p->D != 128 || (p->page_size != 8 && p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128))
         return WAR_ERR_UNSUPPORTED;
     if (!war_quant_block_ok(p->page_size, q->scale_block)) return WAR_ERR_UNSUPPORTED;
-    if ((p->Hq / p->Hkv) * p->N > 512 || p->B > kMaxPlanB) return WAR_ERR_UNSUPPORTED;
+    if ((p->Hq / p->Hkv) * p->N > 512 || p->B > kMaxPlanB || (long long)p->B * p->N * p->Hq >= (1ll << 31)) return WAR_ERR_UNSUPPORTED;
     if ((long long)p->max_pages_per_req * p->page_size >= (1ll << 30)) return WAR_ERR_UNSUPPORTED;    // contexts below 2^30 tokens
     if (!war_rows_aligned(p->k_strides, 1) || !war_rows_aligned(p->v_strides, 1)) return WAR_ERR_UNSUPPORTED;
     return WAR_OK;
@@ -189,8 +189,9 @@ extern "C" war_status_t war_verify_attn_quant(const void* d_q, const void* d_kpo
     pools.k = (const uint8_t*)d_kpool; pools.v = (const uint8_t*)d_vpool; pools.kscale = d_kscale; pools.vscale = d_vscale;
     for (int i = 0; i < 3; ++i) { pools.ks[i] = p->k_strides[i]; pools.vs[i] = p->v_strides[i]; }
     pools.kv = qp->kv_type; pools.block = qp->scale_block;
+    const auto launch = p->Hq / p->Hkv * p->N <= kQuantFewRows ? war_attn_quant_launch_few : war_attn_quant_launch_many;
     if (p->kernel == 0 && war_attn_fused_ok(p, w.row_blocks, n_sm))
-        return war_attn_quant_launch_sm100(d_q, pools, d_page_table, d_prefix_len, d_num_nodes, d_parent, p, w, true, d_out, d_lse,
+        return launch(d_q, pools, d_page_table, d_prefix_len, d_num_nodes, d_parent, p, w, true, d_out, d_lse,
                                            status_word, stream);
     st = war_attn_launch_plan(d_prefix_len, d_num_nodes, d_parent, p, w, n_sm, status_word, stream);
     if (st != WAR_OK) return st;
@@ -201,7 +202,7 @@ extern "C" war_status_t war_verify_attn_quant(const void* d_q, const void* d_kpo
                                                               p->scale * kLog2e, w, (__nv_bfloat16*)d_out, d_lse, status_word);
         WAR_LAUNCH_CHECK();
     } else {
-        st = war_attn_quant_launch_sm100(d_q, pools, d_page_table, d_prefix_len, d_num_nodes, d_parent, p, w, false, d_out, d_lse,
+        st = launch(d_q, pools, d_page_table, d_prefix_len, d_num_nodes, d_parent, p, w, false, d_out, d_lse,
                                          status_word, stream);
         if (st != WAR_OK) return st;
     }
