@@ -4,12 +4,15 @@
 // The logits are the traffic (64 times 131072 values a request against a few thousand context tokens), so a row is read
 // once, 16 bytes a lane, and what the penalties need is looked up on chip: a cluster of up to eight thread blocks takes
 // one request, each block a slice of the vocabulary.  Together they read the request's context once and count its tokens
-// into the slice that owns them (shared-memory atomics across the cluster); from then on a block holds, for its slice, a
-// counter and the bias entry of every token and one bit that says whether the token needs either.  Eight bits decide for
-// eight logits whether the fast path is enough: no penalty, no bias, only the grammar's mask and the comparison.  Rows are
-// independent of each other (tokens on a slot's path are looked up in the tree, not written into the counters), so warps
-// take pieces of rows without a barrier; the winners of a row meet in one 64-bit maximum per block, and the cluster's
-// first block compares the slices.  Ties go to the lowest token, whatever the order of the atomics.
+// into the slice that owns them (shared-memory atomics across the cluster).  Rows are independent of each other (tokens on a
+// slot's path are looked up in the tree, not written into the counters), so warps take pieces of rows without a barrier; the
+// winners of a row meet in one 64-bit maximum per block, and the cluster's first block compares the slices.  Ties go to the
+// lowest token, whatever the order of the atomics.
+//   choice only, penalties that cannot raise a value (repetition >= 1, the others >= 0: the usual case): a logit at or below
+//     the best processed value so far cannot win, so eight are dismissed with one packed maximum and only candidates are
+//     looked up and processed (a few hundred a row)
+//   processed logits wanted, or penalties that may raise: every value goes through the arithmetic, without branches
+//   tokens with a bias, and tokens of the tree, are few: each warp goes through them after its piece of a row
 #include <cuda_bf16.h>
 #include <cooperative_groups.h>
 #include "war_common.cuh"
@@ -19,10 +22,10 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int kMaxSlots = 64;
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxSlices = 8;                 // thread blocks of a cluster
-constexpr int kMaxSlice = 32768;              // tokens a block can hold: 6 bytes and 2 bits each of 227 KB
+constexpr int kMaxSlice = 32768;              // tokens a block can hold: 6 bytes and a bit each, of 227 KB
 constexpr int kMaxVocab = kMaxSlices * kMaxSlice;
 constexpr int kSegment = 1024;                // logits of a row that a warp takes at a time
 constexpr int kMaxBias = 65534;               // bias entries of a request (numbered in 16 bits)
@@ -40,6 +43,7 @@ struct TargetArgs {
     int N, V, slice, words;                   // words: mask words of a row
     int count;                                // 1: count context tokens (a penalty is given)
     int path;                                 // 1: ids are given (tokens on a slot's path count too)
+    int aligned;                              // 1: every row of logits starts on 16 bytes
 };
 
 struct Shared {
@@ -58,6 +62,10 @@ template <> struct Wide<float> {
     static __device__ __forceinline__ uint4 narrow(const float* x) {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
+    static __device__ __forceinline__ float top(const uint4& u) {
+        return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+    }
+    static __device__ __forceinline__ float pick(const uint4& u, int i) { return __uint_as_float(i < 2 ? (i ? u.y : u.x) : (i == 2 ? u.z : u.w)); }
     static __device__ __forceinline__ float load(const float* p) { return *p; }
     static __device__ __forceinline__ void store(float* p, float x) { *p = x; }
 };
@@ -77,6 +85,16 @@ template <> struct Wide<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    // the largest value that is no NaN (NaN: all are)
+    static __device__ __forceinline__ float top(const uint4& u) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ float pick(const uint4& u, int i) {
+        const uint32_t w = i < 4 ? (i < 2 ? u.x : u.y) : (i < 6 ? u.z : u.w);
+        return __uint_as_float((i & 1) ? w & 0xffff0000u : w << 16);
+    }
     static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
@@ -87,6 +105,8 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
+__device__ __forceinline__ uint32_t unordered(uint32_t u) { return (u & 0x80000000u) ? u & 0x7fffffffu : ~u; }
+
 // 32 bits of a bit string from bit v on; words past `words` read as 0
 __device__ __forceinline__ uint32_t bits_at(const uint32_t* w, int v, int words) {
     const int k = v >> 5, sh = v & 31;
@@ -96,7 +116,7 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t* w, int v, int words)
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 war_target_kernel(const TargetArgs a) {
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ Shared sh;
@@ -104,10 +124,10 @@ war_target_kernel(const TargetArgs a) {
     const int rank = (int)cluster.block_rank(), slices = (int)cluster.num_blocks();
     const int b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int W = a.slice, bit_words = W / 32;
-    uint32_t* special = smem;                                             // [bit_words + 1] counter, bias or tree token
-    uint32_t* tree = special + bit_words + 1;                             // [bit_words + 1] some slot's token
-    uint32_t* counter = tree + bit_words + 1;                             // [W] generated occurrences, bit 31: in the context
+    uint32_t* counter = smem;                                             // [W] generated occurrences, bit 31: in the context; when
+    const float* const made_of = reinterpret_cast<const float*>(counter); //     all values are processed: as floats, -1 not in the context
     uint16_t* bias_at = reinterpret_cast<uint16_t*>(counter + (a.count ? W : 0));   // [W] bias entry + 1
+    uint32_t* rare = reinterpret_cast<uint32_t*>(bias_at + (a.bias_off ? W : 0));   // [bit_words + 1] a bias, or some slot's token
     const int v0 = rank * W, v1 = min(a.V, v0 + W);
 
     const int n_in = a.num_nodes[b];
@@ -118,9 +138,10 @@ war_target_kernel(const TargetArgs a) {
     int bad = 0;
     if (n_in < 0 || n_in > a.N) bad = WAR_ERR_BAD_TREE;
     if (c1 < c0 || c1 - c0 >= (1ll << 31) || e1 < e0 || e1 - e0 > kMaxBias) bad = WAR_ERR_INVALID_ARG;
-    for (int x = tid; x < 2 * (bit_words + 1); x += kThreads) special[x] = 0;
-    if (a.count) for (int x = tid; x < W; x += kThreads) counter[x] = 0;
-    if (a.bias_off) for (int x = tid; x < W / 2; x += kThreads) reinterpret_cast<uint32_t*>(bias_at)[x] = 0;
+    for (int x = tid; x < bit_words + 1; x += kThreads) rare[x] = 0;
+    const uint4 zero = make_uint4(0, 0, 0, 0);                            // (W is a multiple of 32)
+    if (a.count) for (int x = tid; x < W / 4; x += kThreads) reinterpret_cast<uint4*>(counter)[x] = zero;
+    if (a.bias_off) for (int x = tid; x < W / 8; x += kThreads) reinterpret_cast<uint4*>(bias_at)[x] = zero;
     if (tid < kMaxSlots) { sh.best[tid] = 0; sh.ids[tid] = -1; }
     if (warp == 0) {
         // ancestor-or-self masks by pointer jumping; the root's bit is cleared (it is the context's last token)
@@ -157,6 +178,7 @@ war_target_kernel(const TargetArgs a) {
             const int from = (int)(len * rank / slices), to = (int)(len * (rank + 1) / slices);
             const int made = a.prompt_len ? a.prompt_len[b] : 0;
             const int32_t* ctx = a.ctx + c0;
+#pragma unroll 4
             for (int x = from + tid; x < to; x += kThreads) {
                 const int tok = ctx[x];
                 if (tok < 0 || tok >= a.V) continue;
@@ -173,7 +195,7 @@ war_target_kernel(const TargetArgs a) {
                 const unsigned same = __match_any_sync(0xffffffffu, tok);
                 if (tok >= v0 && tok < v1 && 31 - __clz(same) == lane) {
                     bias_at[tok - v0] = (uint16_t)(e + lane - e0 + 1);
-                    atomicOr(&special[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
+                    atomicOr(&rare[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
                 }
                 __syncwarp();
             }
@@ -182,55 +204,50 @@ war_target_kernel(const TargetArgs a) {
             const int tok = a.ids[(size_t)b * a.N + tid];
             sh.ids[tid] = tok;
             if (a.count && tok >= v0 && tok < v1) {
-                atomicOr(&special[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
-                atomicOr(&tree[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
+                atomicOr(&rare[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
             }
         }
     }
     cluster.sync();                                                       // all counts have arrived
-    if (n > 0 && a.count) {
-        for (int x = warp; x < bit_words; x += kWarps) {
-            const unsigned hit = __ballot_sync(0xffffffffu, counter[x * 32 + lane] != 0);
-            if (lane == 0 && hit) atomicOr(&special[x], hit);
-        }
-    }
-    __syncthreads();
-
     const float rep = a.repetition ? a.repetition[b] : 1.f, pres = a.presence ? a.presence[b] : 0.f, freq = a.frequency ? a.frequency[b] : 0.f;
-    // the value of a token that needs a counter or a bias
-    auto process = [&](float x, int v, int j) -> float {
-        const int l = v - v0;
-        if (a.count) {
-            const uint32_t c = counter[l];
-            uint32_t made = c & ~kSeen;
-            bool seen = c != 0;
-            if ((tree[l >> 5] >> (l & 31)) & 1u) {
-                unsigned long long m = sh.anc[j];
-                while (m) {
-                    const int s = __ffsll((long long)m) - 1;
-                    m &= m - 1;
-                    made += sh.ids[s] == v;
-                }
-                seen = seen || made != 0;
-            }
-            if (seen) x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
-            x = __fsub_rn(x, __fmul_rn(freq, (float)made));
-            if (made) x = __fsub_rn(x, pres);
-        }
-        if (a.bias_off) {
-            const int e = bias_at[l];
-            if (e) x = __fadd_rn(x, a.bias_val[e0 + e - 1]);
-        }
-        return x;
+    const bool dismiss = !a.out && rep >= 1.f && pres >= 0.f && freq >= 0.f;          // (uniform)
+    auto made_from = [](uint32_t c) -> float { return c == 0 ? -1.f : (float)(c & ~kSeen); };
+    if (n > 0 && a.count && !dismiss) {
+        for (int x = tid; x < W; x += kThreads) counter[x] = __float_as_uint(made_from(counter[x]));
+        __syncthreads();
+    }
+    // a value after the penalties; made < 0: neither in the context nor on the path
+    auto penalise = [&](float x, float made) -> float {
+        if (made < 0.f) return x;
+        x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
+        x = __fsub_rn(x, __fmul_rn(freq, made));
+        return made > 0.f ? __fsub_rn(x, pres) : x;
     };
 
     constexpr int kPer = Wide<T>::kPer;
     constexpr int kLoads = kSegment / (32 * kPer);
     const int z = blockIdx.z, zs = gridDim.z;
-    const int segments = v1 > v0 ? (v1 - v0 + kSegment - 1) / kSegment + 1 : 0;     // one more: rows need not start on 16 bytes
-    const int rows = (n - z + zs - 1) / zs;                               // rows z, z + zs, ... below n
-    for (int task = warp; task < rows * segments; task += kWarps) {
+    const int segments = v1 > v0 ? (v1 - v0 + (a.aligned ? 0 : kPer - 1) + kSegment - 1) / kSegment : 0;
+    const int rows = n > z ? (n - z + zs - 1) / zs : 0;                   // rows z, z + zs, ... below n
+    // a warp's pieces follow each other, so that a row's best value is known when most of it is read
+    const int tasks = rows * segments;
+    int of_row = -1, best_v = 0x7fffffff;
+    float best = -INFINITY, bar = -INFINITY;                              // a lane's best of the row; what a candidate must exceed
+    auto flush = [&]() {                                                  // the warp's best of the row goes to the block's
+        unsigned long long key = best > -INFINITY ? ((unsigned long long)ordered(best) << 32) | (uint32_t)~best_v : 0ull;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, o);
+            key = other > key ? other : key;
+        }
+        if (lane == 0 && key) atomicMax(&sh.best[of_row], key);
+    };
+    for (int task = (int)((long long)tasks * warp / kWarps); task < (int)((long long)tasks * (warp + 1) / kWarps); ++task) {
         const int rj = task / segments, seg = task - rj * segments, j = z + rj * zs;
+        if (j != of_row) {
+            if (of_row >= 0) flush();
+            of_row = j; best = -INFINITY; bar = -INFINITY; best_v = 0x7fffffff;
+        }
         const T* row = reinterpret_cast<const T*>(a.logits) + b * a.ls[0] + j * a.ls[1];
         T* out = a.out ? reinterpret_cast<T*>(a.out) + b * a.os[0] + j * a.os[1] : nullptr;
         const uint32_t* mask = a.mask ? a.mask + b * a.ms[0] + j * a.ms[1] : nullptr;
@@ -239,60 +256,126 @@ war_target_kernel(const TargetArgs a) {
         const int first = v0 - skew + seg * kSegment;                     // a 16-byte boundary
         if (first >= v1) continue;
         const bool out_wide = out && (((uintptr_t)(out + first)) & 15) == 0;
-        float best = -INFINITY;
-        int best_v = 0x7fffffff;
+        const bool table_wide = (skew & 3) == 0;
         uint4 in[kLoads];
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int v = first + (u * 32 + lane) * kPer;
+            in[u] = make_uint4(0, 0, 0, 0);
             if (v >= v0 && v + kPer <= v1) in[u] = __ldcs(reinterpret_cast<const uint4*>(row + v));
+        }
+        // the piece's mask words: at most 33, a lane each
+        uint32_t m_lane = 0xffffffffu, m_last = 0xffffffffu;
+        const int w0 = first >> 5;
+        if (mask) {
+            const int w = w0 + lane;
+            m_lane = w >= 0 && w < a.words ? mask[w] : 0;
+            m_last = w0 + 32 < a.words && skew ? mask[w0 + 32] : 0;
         }
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int v = first + (u * 32 + lane) * kPer;
-            if (v >= v0 && v + kPer <= v1) {
-                float x[kPer];
-                Wide<T>::widen(in[u], x);
-                const uint32_t full = (1u << kPer) - 1;
-                const uint32_t odd = bits_at(special, v - v0, bit_words + 1) & full;
-                const uint32_t allowed = mask ? bits_at(mask, v, a.words) & full : full;
-                if (odd) {
+            const bool whole = v >= v0 && v + kPer <= v1;
+            uint32_t allowed = 0xffffffffu;                               // bit i: v + i may be chosen
+            if (mask) {
+                const int k = (v >> 5) - w0;
+                allowed = __shfl_sync(0xffffffffu, m_lane, k & 31);
+                if (skew) {
+                    uint32_t next = __shfl_sync(0xffffffffu, m_lane, (k + 1) & 31);
+                    allowed = k == 32 ? m_last : allowed;
+                    next = k == 31 ? m_last : next;                       // (v + i never reaches word 33)
+                    allowed = __funnelshift_r(allowed, next, v & 31);
+                } else allowed >>= v & 31;
+            }
+            const bool may = dismiss && whole && Wide<T>::top(in[u]) > bar;
+            if (whole) {
+                if (dismiss) {
+                    if (may) {
+                        float x[kPer];
+                        Wide<T>::widen(in[u], x);
+                        uint32_t cand = 0;
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i)
-                        if ((odd >> i) & 1u) x[i] = process(x[i], v + i, j);
-                }
+                        for (int i = 0; i < kPer; ++i) cand |= (uint32_t)(x[i] > bar) << i;
+                        cand &= ~bits_at(rare, v - v0, bit_words + 1) & allowed;
+                        for (; cand; cand &= cand - 1) {
+                            const int i = __ffs(cand) - 1;
+                            const float raw = Wide<T>::pick(in[u], i);
+                            const float y = a.count ? penalise(raw, made_from(counter[v + i - v0])) : raw;
+                            if (y > best) { best = y; best_v = v + i; }
+                        }
+                    }
+                } else {
+                    const uint32_t few = bits_at(rare, v - v0, bit_words + 1);
+                    float x[kPer], y[kPer];
+                    Wide<T>::widen(in[u], x);
+                    if (a.count) {
+                        float made[kPer];
+                        if (table_wide) {
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    if (!((allowed >> i) & 1u)) x[i] = -INFINITY;
-                    if (x[i] > best) { best = x[i]; best_v = v + i; }
-                }
-                if (out) {
-                    if (out_wide) *reinterpret_cast<uint4*>(out + v) = Wide<T>::narrow(x);
-                    else {
+                            for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(made + i) = *reinterpret_cast<const float4*>(made_of + (v - v0) + i);
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < kPer; ++i) Wide<T>::store(out + v + i, x[i]);
+                            for (int i = 0; i < kPer; ++i) made[i] = made_of[v - v0 + i];
+                        }
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) y[i] = penalise(x[i], made[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) y[i] = x[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        if (!((allowed >> i) & 1u)) y[i] = -INFINITY;
+                        if ((few >> i) & 1u) y[i] = x[i];                 // (written again below)
+                        else if (y[i] > best) { best = y[i]; best_v = v + i; }
+                    }
+                    if (out) {
+                        if (out_wide) *reinterpret_cast<uint4*>(out + v) = Wide<T>::narrow(y);
+                        else {
+#pragma unroll
+                            for (int i = 0; i < kPer; ++i) Wide<T>::store(out + v + i, y[i]);
+                        }
                     }
                 }
             } else if (v + kPer > v0 && v < v1) {                         // the slice begins or ends inside these 16 bytes
                 for (int i = max(0, v0 - v); i < kPer && v + i < v1; ++i) {
-                    float y = Wide<T>::load(row + v + i);
                     const int l = v + i - v0;
-                    if ((special[l >> 5] >> (l & 31)) & 1u) y = process(y, v + i, j);
+                    if ((rare[l >> 5] >> (l & 31)) & 1u) continue;
+                    float y = Wide<T>::load(row + v + i);
+                    if (a.count) y = penalise(y, dismiss ? made_from(counter[l]) : made_of[l]);
                     if (mask && !((mask[(v + i) >> 5] >> ((v + i) & 31)) & 1u)) y = -INFINITY;
                     if (y > best) { best = y; best_v = v + i; }
                     if (out) Wide<T>::store(out + v + i, y);
                 }
             }
+            // later values of the row must exceed the warp's best (equal ones stand behind it)
+            if (dismiss && __any_sync(0xffffffffu, may)) bar = __uint_as_float(unordered(__reduce_max_sync(0xffffffffu, ordered(best))));
         }
-        // a lane's tokens grow with u, so `>` kept the lowest of equal values
-        unsigned long long key = best > -INFINITY ? ((unsigned long long)ordered(best) << 32) | (uint32_t)~best_v : 0ull;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, o);
-            key = other > key ? other : key;
+        // tokens with a bias and tokens of the tree, if they lie in this piece
+        __syncwarp();
+        const int l0 = max(first, v0) - v0, l1 = min(first + kSegment, v1) - v0;
+        for (int w = (l0 >> 5) + lane; w * 32 < l1; w += 32) for (uint32_t m = rare[w]; m; m &= m - 1) {
+            const int l = w * 32 + __ffs(m) - 1, v = v0 + l;
+            if (l < l0 || l >= l1) continue;
+            float x = Wide<T>::load(row + v);
+            if (a.count) {
+                float made = dismiss ? made_from(counter[l]) : made_of[l];
+                int on_path = 0;
+                for (unsigned long long m = sh.anc[j]; m; m &= m - 1) on_path += sh.ids[__ffsll((long long)m) - 1] == v;
+                if (on_path) made = fmaxf(made, 0.f) + (float)on_path;
+                x = penalise(x, made);
+            }
+            if (a.bias_off) {
+                const int k = bias_at[l];
+                if (k) x = __fadd_rn(x, a.bias_val[e0 + k - 1]);
+            }
+            if (mask && !((mask[v >> 5] >> (v & 31)) & 1u)) x = -INFINITY;
+            if (x > best || (x == best && v < best_v && x > -INFINITY)) { best = x; best_v = v; }
+            if (out) Wide<T>::store(out + v, x);
         }
-        if (lane == 0 && key) atomicMax(&sh.best[j], key);
+        __syncwarp();
     }
+    if (of_row >= 0) flush();
     cluster.sync();                                                       // every slice's winners are there
     if (rank == 0) {
         for (int j = tid; j < a.N; j += kThreads) {
@@ -369,13 +452,17 @@ extern "C" war_status_t war_target(const void* d_logits, const int32_t* d_num_no
     for (int i = 0; i < 2; ++i) { a.ls[i] = p->logits_strides[i]; a.os[i] = p->out_strides[i]; a.ms[i] = p->mask_strides[i]; }
     a.N = p->N; a.V = p->V; a.words = (p->V + 31) / 32;
     a.count = count; a.path = count && d_ids != nullptr;
-    // slices of at least a segment per warp, whole mask words, at most eight
-    int slices = (p->V + kSegment * 2 - 1) / (kSegment * 2);
-    if (slices > kMaxSlices) slices = kMaxSlices;
+    a.aligned = (((uintptr_t)d_logits | (uintptr_t)(p->logits_strides[0] * size) | (uintptr_t)(p->logits_strides[1] * size)) & 15) == 0;
+    // Slices: enough thread blocks to fill the GPU, whole mask words, at most eight, at least two segments each; a row that one
+    // block reads in a longer piece is dismissed faster.
+    const int most = (p->V + kSegment * 2 - 1) / (kSegment * 2), least = (p->V + kMaxSlice - 1) / kMaxSlice;
+    int slices = (148 * 4 + p->B - 1) / p->B;
+    slices = slices > most ? most : slices;
+    slices = slices > kMaxSlices ? kMaxSlices : slices < least ? least : slices;
     a.slice = ((p->V + slices - 1) / slices + 31) / 32 * 32;
     int groups = (148 * 4 + slices * p->B - 1) / (slices * p->B);
     if (groups > p->N) groups = p->N;
-    const size_t smem = (size_t)(a.slice / 32 + 1) * 8 + (count ? (size_t)a.slice * 4 : 0) + (in->d_bias_off ? (size_t)a.slice * 2 : 0);
+    const size_t smem = (size_t)(a.slice / 32 + 1) * 4 + (count ? (size_t)a.slice * 4 : 0) + (in->d_bias_off ? (size_t)a.slice * 2 : 0);
     return p->dtype == 0 ? launch<__nv_bfloat16>(a, slices, p->B, groups, smem, stream)
                          : launch<float>(a, slices, p->B, groups, smem, stream);
 }
