@@ -49,6 +49,7 @@ struct TargetArgs {
 struct Shared {
     unsigned long long best[kMaxSlots];       // (ordered value << 32) | ~token; 0: none
     unsigned long long anc[kMaxSlots];
+    uint32_t bar[kMaxSlots];                  // ordered value that some warp has found in the row; 0: none
     int ids[kMaxSlots];
     int bad;
 };
@@ -115,7 +116,7 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t* w, int v, int words)
     return x;
 }
 
-template <class T>
+template <class T, bool kOut>
 __global__ void __launch_bounds__(kThreads, 2)
 war_target_kernel(const TargetArgs a) {
     extern __shared__ __align__(16) uint32_t smem[];
@@ -142,7 +143,7 @@ war_target_kernel(const TargetArgs a) {
     const uint4 zero = make_uint4(0, 0, 0, 0);                            // (W is a multiple of 32)
     if (a.count) for (int x = tid; x < W / 4; x += kThreads) reinterpret_cast<uint4*>(counter)[x] = zero;
     if (a.bias_off) for (int x = tid; x < W / 8; x += kThreads) reinterpret_cast<uint4*>(bias_at)[x] = zero;
-    if (tid < kMaxSlots) { sh.best[tid] = 0; sh.ids[tid] = -1; }
+    if (tid < kMaxSlots) { sh.best[tid] = 0; sh.bar[tid] = 0; sh.ids[tid] = -1; }
     if (warp == 0) {
         // ancestor-or-self masks by pointer jumping; the root's bit is cleared (it is the context's last token)
         const int n = bad ? 0 : n_in;
@@ -167,25 +168,24 @@ war_target_kernel(const TargetArgs a) {
         sh.anc[lane] = m0 & ~1ull; sh.anc[lane + 32] = m1 & ~1ull;
         if (lane == 0) sh.bad = bad ? bad : (wrong ? WAR_ERR_BAD_TREE : 0);
     }
-    cluster.sync();                                                       // every block's tables are cleared
+    __syncthreads();                                                      // the tables are cleared
     bad = sh.bad;
     const int n = bad ? 0 : n_in;
 
     if (n > 0) {
         if (a.count) {
-            // this block's share of the context, counted into the blocks that own the tokens
-            const long long len = c1 - c0;
-            const int from = (int)(len * rank / slices), to = (int)(len * (rank + 1) / slices);
-            const int made = a.prompt_len ? a.prompt_len[b] : 0;
+            // every block reads the context and counts the tokens of its slice
             const int32_t* ctx = a.ctx + c0;
-#pragma unroll 4
-            for (int x = from + tid; x < to; x += kThreads) {
+            const int len = (int)(c1 - c0), made = a.prompt_len ? min(max(a.prompt_len[b], 0), len) : 0;
+#pragma unroll 8
+            for (int x = tid; x < made; x += kThreads) {
                 const int tok = ctx[x];
-                if (tok < 0 || tok >= a.V) continue;
-                const int owner = tok / W;
-                uint32_t* at = cluster.map_shared_rank(counter + (tok - owner * W), owner);
-                if (x >= made) atomicAdd(at, 1u);
-                else atomicOr(at, kSeen);
+                if (tok >= v0 && tok < v1) atomicOr(&counter[tok - v0], kSeen);
+            }
+#pragma unroll 8
+            for (int x = made + tid; x < len; x += kThreads) {
+                const int tok = ctx[x];
+                if (tok >= v0 && tok < v1) atomicAdd(&counter[tok - v0], 1u);
             }
         }
         if (a.bias_off && warp == kWarps - 1) {
@@ -208,9 +208,9 @@ war_target_kernel(const TargetArgs a) {
             }
         }
     }
-    cluster.sync();                                                       // all counts have arrived
+    __syncthreads();                                                      // all tokens are counted
     const float rep = a.repetition ? a.repetition[b] : 1.f, pres = a.presence ? a.presence[b] : 0.f, freq = a.frequency ? a.frequency[b] : 0.f;
-    const bool dismiss = !a.out && rep >= 1.f && pres >= 0.f && freq >= 0.f;          // (uniform)
+    const bool dismiss = !kOut && rep >= 1.f && pres >= 0.f && freq >= 0.f;          // (uniform)
     auto made_from = [](uint32_t c) -> float { return c == 0 ? -1.f : (float)(c & ~kSeen); };
     if (n > 0 && a.count && !dismiss) {
         for (int x = tid; x < W; x += kThreads) counter[x] = __float_as_uint(made_from(counter[x]));
@@ -222,6 +222,22 @@ war_target_kernel(const TargetArgs a) {
         x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
         x = __fsub_rn(x, __fmul_rn(freq, made));
         return made > 0.f ? __fsub_rn(x, pres) : x;
+    };
+
+    // the same without branches; `odd` is set where a division is not exactly rounded this way (Markstein's: a quotient that a
+    // residual corrects, here twice, from the rounded reciprocal; it needs values well inside the range)
+    const float rep_inv = __frcp_rn(rep);
+    const bool rep_plain = rep >= 0x1p-60f && rep <= 0x1p60f;
+    auto penalise_plain = [&](float x, float made, bool& odd) -> float {
+        float q = __fmul_rn(x, rep_inv);
+        q = __fmaf_rn(__fmaf_rn(-q, rep, x), rep_inv, q);
+        q = __fmaf_rn(__fmaf_rn(-q, rep, x), rep_inv, q);
+        const bool up = x > 0.f;
+        odd = odd || (up && made >= 0.f && !(x >= 0x1p-60f && x <= 0x1p60f && rep_plain));
+        float y = up ? q : __fmul_rn(x, rep);
+        y = __fsub_rn(y, __fmul_rn(freq, made));
+        y = made > 0.f ? __fsub_rn(y, pres) : y;
+        return made < 0.f ? x : y;
     };
 
     constexpr int kPer = Wide<T>::kPer;
@@ -249,14 +265,20 @@ war_target_kernel(const TargetArgs a) {
             of_row = j; best = -INFINITY; bar = -INFINITY; best_v = 0x7fffffff;
         }
         const T* row = reinterpret_cast<const T*>(a.logits) + b * a.ls[0] + j * a.ls[1];
-        T* out = a.out ? reinterpret_cast<T*>(a.out) + b * a.os[0] + j * a.os[1] : nullptr;
+        T* out = kOut ? reinterpret_cast<T*>(a.out) + b * a.os[0] + j * a.os[1] : nullptr;
         const uint32_t* mask = a.mask ? a.mask + b * a.ms[0] + j * a.ms[1] : nullptr;
         // elements between the 16-byte boundary at or before the slice's first logit and that logit
         const int skew = (int)(((uintptr_t)(row + v0) & 15) / sizeof(T));
         const int first = v0 - skew + seg * kSegment;                     // a 16-byte boundary
         if (first >= v1) continue;
-        const bool out_wide = out && (((uintptr_t)(out + first)) & 15) == 0;
+        const bool out_wide = kOut && (((uintptr_t)(out + first)) & 15) == 0;
         const bool table_wide = (skew & 3) == 0;
+        // what another warp found in the row counts as well (values equal to it still have to be looked at: they may stand before it)
+        if (dismiss) {
+            const uint32_t o = *reinterpret_cast<volatile uint32_t*>(&sh.bar[j]);
+            if (o) bar = fmaxf(bar, __uint_as_float(unordered(o - (o == 0x80000000u ? 2 : 1))));
+        }
+        const float bar_in = bar;
         uint4 in[kLoads];
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
@@ -287,26 +309,36 @@ war_target_kernel(const TargetArgs a) {
                     allowed = __funnelshift_r(allowed, next, v & 31);
                 } else allowed >>= v & 31;
             }
-            const bool may = dismiss && whole && Wide<T>::top(in[u]) > bar;
-            if (whole) {
-                if (dismiss) {
-                    if (may) {
-                        float x[kPer];
-                        Wide<T>::widen(in[u], x);
-                        uint32_t cand = 0;
+            if (dismiss) {
+                float x[kPer], top = whole ? Wide<T>::top(in[u]) : -INFINITY;
+                if (__any_sync(0xffffffffu, top > bar)) {
+                    // the largest of each lane first: after it most others are at or below the bar
+                    const float from = bar;
+                    uint32_t ok = whole ? allowed & ~bits_at(rare, v - v0, bit_words + 1) : 0;
+                    Wide<T>::widen(in[u], x);
 #pragma unroll
-                        for (int i = 0; i < kPer; ++i) cand |= (uint32_t)(x[i] > bar) << i;
-                        cand &= ~bits_at(rare, v - v0, bit_words + 1) & allowed;
-                        for (; cand; cand &= cand - 1) {
-                            const int i = __ffs(cand) - 1;
-                            const float raw = Wide<T>::pick(in[u], i);
-                            const float y = a.count ? penalise(raw, made_from(counter[v + i - v0])) : raw;
-                            if (y > best) { best = y; best_v = v + i; }
+                    for (int i = 0; i < kPer; ++i) x[i] = ((ok >> i) & 1u) && x[i] > from ? x[i] : -INFINITY;
+                    while (true) {
+                        top = x[0];
+                        int i = 0;
+#pragma unroll
+                        for (int k = 1; k < kPer; ++k) if (x[k] > top) { top = x[k]; i = k; }
+                        const bool look = top >= bar && top > -INFINITY;
+                        if (!__any_sync(0xffffffffu, look)) break;
+                        if (look) {
+                            const float y = a.count ? penalise(top, made_from(counter[v + i - v0])) : top;
+                            if (y > best || (y == best && v + i < best_v && y > -INFINITY)) { best = y; best_v = v + i; }
+#pragma unroll
+                            for (int k = 0; k < kPer; ++k) x[k] = k == i ? -INFINITY : x[k];
                         }
+                        bar = fmaxf(bar, __uint_as_float(unordered(__reduce_max_sync(0xffffffffu, ordered(best)))));
                     }
-                } else {
-                    const uint32_t few = bits_at(rare, v - v0, bit_words + 1);
-                    float x[kPer], y[kPer];
+                }
+            }
+            if (whole) {
+                if (!dismiss) {
+                    const uint32_t few = bits_at(rare, v - v0, bit_words + 1) & ((1u << kPer) - 1), ok = allowed & ~few;
+                    float x[kPer];
                     Wide<T>::widen(in[u], x);
                     if (a.count) {
                         float made[kPer];
@@ -317,23 +349,34 @@ war_target_kernel(const TargetArgs a) {
 #pragma unroll
                             for (int i = 0; i < kPer; ++i) made[i] = made_of[v - v0 + i];
                         }
+                        bool odd = false;
 #pragma unroll
-                        for (int i = 0; i < kPer; ++i) y[i] = penalise(x[i], made[i]);
-                    } else {
+                        for (int i = 0; i < kPer; ++i) x[i] = penalise_plain(x[i], made[i], odd);
+                        if (odd) {
 #pragma unroll
-                        for (int i = 0; i < kPer; ++i) y[i] = x[i];
+                            for (int i = 0; i < kPer; ++i) x[i] = penalise(Wide<T>::pick(in[u], i), made[i]);
+                        }
                     }
+                    float top = -INFINITY;
 #pragma unroll
                     for (int i = 0; i < kPer; ++i) {
-                        if (!((allowed >> i) & 1u)) y[i] = -INFINITY;
-                        if ((few >> i) & 1u) y[i] = x[i];                 // (written again below)
-                        else if (y[i] > best) { best = y[i]; best_v = v + i; }
+                        x[i] = (ok >> i) & 1u ? x[i] : -INFINITY;
+                        top = fmaxf(top, x[i]);
                     }
-                    if (out) {
-                        if (out_wide) *reinterpret_cast<uint4*>(out + v) = Wide<T>::narrow(y);
+                    if (top > best) {
+                        best = top;
+#pragma unroll
+                        for (int i = kPer - 1; i >= 0; --i) best_v = x[i] == top ? v + i : best_v;
+                    }
+                    if (kOut) {
+                        if (few) {                                        // as they were, for the list below (out may be the logits)
+#pragma unroll
+                            for (int i = 0; i < kPer; ++i) x[i] = (few >> i) & 1u ? Wide<T>::pick(in[u], i) : x[i];
+                        }
+                        if (out_wide) __stcs(reinterpret_cast<uint4*>(out + v), Wide<T>::narrow(x));
                         else {
 #pragma unroll
-                            for (int i = 0; i < kPer; ++i) Wide<T>::store(out + v + i, y[i]);
+                            for (int i = 0; i < kPer; ++i) Wide<T>::store(out + v + i, x[i]);
                         }
                     }
                 }
@@ -345,11 +388,9 @@ war_target_kernel(const TargetArgs a) {
                     if (a.count) y = penalise(y, dismiss ? made_from(counter[l]) : made_of[l]);
                     if (mask && !((mask[(v + i) >> 5] >> ((v + i) & 31)) & 1u)) y = -INFINITY;
                     if (y > best) { best = y; best_v = v + i; }
-                    if (out) Wide<T>::store(out + v + i, y);
+                    if (kOut) Wide<T>::store(out + v + i, y);
                 }
             }
-            // later values of the row must exceed the warp's best (equal ones stand behind it)
-            if (dismiss && __any_sync(0xffffffffu, may)) bar = __uint_as_float(unordered(__reduce_max_sync(0xffffffffu, ordered(best))));
         }
         // tokens with a bias and tokens of the tree, if they lie in this piece
         __syncwarp();
@@ -371,7 +412,12 @@ war_target_kernel(const TargetArgs a) {
             }
             if (mask && !((mask[v >> 5] >> (v & 31)) & 1u)) x = -INFINITY;
             if (x > best || (x == best && v < best_v && x > -INFINITY)) { best = x; best_v = v; }
-            if (out) Wide<T>::store(out + v, x);
+            if (kOut) Wide<T>::store(out + v, x);
+        }
+        // later values of the row must exceed the warp's best
+        if (dismiss) {
+            bar = fmaxf(bar, __uint_as_float(unordered(__reduce_max_sync(0xffffffffu, ordered(best)))));
+            if (lane == 0 && bar > bar_in) atomicMax(&sh.bar[j], ordered(bar));
         }
         __syncwarp();
     }
@@ -390,26 +436,26 @@ war_target_kernel(const TargetArgs a) {
         }
         if (bad && tid == 0) war_set_device_status(a.status_word, bad);
     }
-    cluster.sync();                                                       // nobody leaves while its winners are read
+    cluster.sync();                                                       // no block leaves while its winners are read
 }
 
 constexpr int kMaxDevices = 64;
-template <class T>
+template <class T, bool kOut>
 war_status_t allow_smem(int bytes) {
     static int allowed[kMaxDevices];                                     // (two threads may both set the attribute: the same call)
     int dev = 0;
     WAR_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= kMaxDevices) return WAR_ERR_UNSUPPORTED;
     if (bytes > 48 * 1024 && !allowed[dev]) {
-        WAR_CUDA_TRY(cudaFuncSetAttribute(war_target_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024));
+        WAR_CUDA_TRY(cudaFuncSetAttribute(war_target_kernel<T, kOut>, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024));
         allowed[dev] = 1;
     }
     return WAR_OK;
 }
 
-template <class T>
+template <class T, bool kOut>
 war_status_t launch(const TargetArgs& a, int slices, int B, int groups, size_t smem, cudaStream_t s) {
-    const war_status_t st = allow_smem<T>((int)smem);
+    const war_status_t st = allow_smem<T, kOut>((int)smem);
     if (st != WAR_OK) return st;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(slices, B, groups);
@@ -420,7 +466,7 @@ war_status_t launch(const TargetArgs& a, int slices, int B, int groups, size_t s
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = slices; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, war_target_kernel<T>, a) != cudaSuccess) { (void)cudaGetLastError(); return WAR_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, war_target_kernel<T, kOut>, a) != cudaSuccess) { (void)cudaGetLastError(); return WAR_ERR_CUDA; }
     return WAR_OK;
 }
 
@@ -453,16 +499,17 @@ extern "C" war_status_t war_target(const void* d_logits, const int32_t* d_num_no
     a.N = p->N; a.V = p->V; a.words = (p->V + 31) / 32;
     a.count = count; a.path = count && d_ids != nullptr;
     a.aligned = (((uintptr_t)d_logits | (uintptr_t)(p->logits_strides[0] * size) | (uintptr_t)(p->logits_strides[1] * size)) & 15) == 0;
-    // Slices: enough thread blocks to fill the GPU, whole mask words, at most eight, at least two segments each; a row that one
-    // block reads in a longer piece is dismissed faster.
+    // Slices of whole mask words, at most eight, at least two segments each, so many that the requests fill the GPU (two thread
+    // blocks an SM); rows are dealt to more clusters of a request only if that leaves room: each counts the context again.
+    const int resident = 2 * 148;
     const int most = (p->V + kSegment * 2 - 1) / (kSegment * 2), least = (p->V + kMaxSlice - 1) / kMaxSlice;
-    int slices = (148 * 4 + p->B - 1) / p->B;
+    int slices = (resident * 2 + p->B - 1) / p->B;
     slices = slices > most ? most : slices;
     slices = slices > kMaxSlices ? kMaxSlices : slices < least ? least : slices;
     a.slice = ((p->V + slices - 1) / slices + 31) / 32 * 32;
-    int groups = (148 * 4 + slices * p->B - 1) / (slices * p->B);
-    if (groups > p->N) groups = p->N;
+    int groups = resident / (slices * p->B);
+    groups = groups < 1 ? 1 : groups > p->N ? p->N : groups;
     const size_t smem = (size_t)(a.slice / 32 + 1) * 4 + (count ? (size_t)a.slice * 4 : 0) + (in->d_bias_off ? (size_t)a.slice * 2 : 0);
-    return p->dtype == 0 ? launch<__nv_bfloat16>(a, slices, p->B, groups, smem, stream)
-                         : launch<float>(a, slices, p->B, groups, smem, stream);
+    if (p->dtype == 0) return d_out ? launch<__nv_bfloat16, true>(a, slices, p->B, groups, smem, stream) : launch<__nv_bfloat16, false>(a, slices, p->B, groups, smem, stream);
+    return d_out ? launch<float, true>(a, slices, p->B, groups, smem, stream) : launch<float, false>(a, slices, p->B, groups, smem, stream);
 }
