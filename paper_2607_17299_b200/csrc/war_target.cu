@@ -63,6 +63,22 @@ template <> struct Wide<float> {
     static __device__ __forceinline__ uint4 narrow(const float* x) {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
+    static __device__ __forceinline__ uint4 nothing() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+    static __device__ __noinline__ uint4 part(const float* p, int from, int to) {    // elements from .. to - 1, -inf elsewhere
+        uint4 r;
+        r.x = from <= 0 && to > 0 ? __float_as_uint(p[0]) : 0xff800000u;
+        r.y = from <= 1 && to > 1 ? __float_as_uint(p[1]) : 0xff800000u;
+        r.z = from <= 2 && to > 2 ? __float_as_uint(p[2]) : 0xff800000u;
+        r.w = from <= 3 && to > 3 ? __float_as_uint(p[3]) : 0xff800000u;
+        return r;
+    }
+    static __device__ __forceinline__ uint4 keep(const uint4& u, uint32_t ok) {      // -inf where ok's bit is clear
+        return make_uint4(ok & 1 ? u.x : 0xff800000u, ok & 2 ? u.y : 0xff800000u, ok & 4 ? u.z : 0xff800000u, ok & 8 ? u.w : 0xff800000u);
+    }
+    static __device__ __forceinline__ int find(const uint4& u, float x) {            // an element that equals x, if one does
+        return __uint_as_float(u.x) == x ? 0 : __uint_as_float(u.y) == x ? 1 : __uint_as_float(u.z) == x ? 2 : 3;
+    }
+    // the largest value that is no NaN (NaN: all are)
     static __device__ __forceinline__ float top(const uint4& u) {
         return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
     }
@@ -86,7 +102,35 @@ template <> struct Wide<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    // the largest value that is no NaN (NaN: all are)
+    static __device__ __forceinline__ uint4 nothing() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+    static __device__ __noinline__ uint4 part(const __nv_bfloat16* p, int from, int to) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = from <= 2 * i && to > 2 * i ? reinterpret_cast<const uint16_t*>(p)[2 * i] : 0xff80u;
+            const uint32_t hi = from <= 2 * i + 1 && to > 2 * i + 1 ? reinterpret_cast<const uint16_t*>(p)[2 * i + 1] : 0xff80u;
+            w[i] = lo | hi << 16;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ uint32_t keep2(uint32_t w, uint32_t ok) {
+        const uint32_t m = (ok & 1 ? 0xffffu : 0u) | (ok & 2 ? 0xffff0000u : 0u);
+        return (w & m) | (0xff80ff80u & ~m);
+    }
+    static __device__ __forceinline__ uint4 keep(const uint4& u, uint32_t ok) {
+        return make_uint4(keep2(u.x, ok), keep2(u.y, ok >> 2), keep2(u.z, ok >> 4), keep2(u.w, ok >> 6));
+    }
+    static __device__ __forceinline__ int find(const uint4& u, float x) {
+        int i = 7;
+        if (__uint_as_float(u.w << 16) == x) i = 6;
+        if (__uint_as_float(u.z & 0xffff0000u) == x) i = 5;
+        if (__uint_as_float(u.z << 16) == x) i = 4;
+        if (__uint_as_float(u.y & 0xffff0000u) == x) i = 3;
+        if (__uint_as_float(u.y << 16) == x) i = 2;
+        if (__uint_as_float(u.x & 0xffff0000u) == x) i = 1;
+        if (__uint_as_float(u.x << 16) == x) i = 0;
+        return i;
+    }
     static __device__ __forceinline__ float top(const uint4& u) {
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
         const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
@@ -224,17 +268,15 @@ war_target_kernel(const TargetArgs a) {
         return made > 0.f ? __fsub_rn(x, pres) : x;
     };
 
-    // the same without branches; `odd` is set where a division is not exactly rounded this way (Markstein's: a quotient that a
-    // residual corrects, here twice, from the rounded reciprocal; it needs values well inside the range)
+    // the same without branches, where |x| is inside [2^-60, 2^60] (Markstein's division: a quotient from the rounded reciprocal
+    // that the residual corrects, here twice; it is the rounded quotient as long as nothing leaves the normal range)
     const float rep_inv = __frcp_rn(rep);
     const bool rep_plain = rep >= 0x1p-60f && rep <= 0x1p60f;
-    auto penalise_plain = [&](float x, float made, bool& odd) -> float {
+    auto penalise_plain = [&](float x, float made) -> float {
         float q = __fmul_rn(x, rep_inv);
         q = __fmaf_rn(__fmaf_rn(-q, rep, x), rep_inv, q);
         q = __fmaf_rn(__fmaf_rn(-q, rep, x), rep_inv, q);
-        const bool up = x > 0.f;
-        odd = odd || (up && made >= 0.f && !(x >= 0x1p-60f && x <= 0x1p60f && rep_plain));
-        float y = up ? q : __fmul_rn(x, rep);
+        float y = x > 0.f ? q : __fmul_rn(x, rep);
         y = __fsub_rn(y, __fmul_rn(freq, made));
         y = made > 0.f ? __fsub_rn(y, pres) : y;
         return made < 0.f ? x : y;
@@ -283,112 +325,126 @@ war_target_kernel(const TargetArgs a) {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const int v = first + (u * 32 + lane) * kPer;
-            in[u] = make_uint4(0, 0, 0, 0);
             if (v >= v0 && v + kPer <= v1) in[u] = __ldcs(reinterpret_cast<const uint4*>(row + v));
+            else {                                                        // (a slice may begin or end inside 16 bytes)
+                in[u] = Wide<T>::nothing();
+                if (v + kPer > v0 && v < v1) in[u] = Wide<T>::part(row + v, v0 - v, v1 - v);
+            }
         }
-        // the piece's mask words: at most 33, a lane each
+        // the piece's mask words: at most 33, a lane each; tokens that may be chosen here, rare ones are looked at below
         uint32_t m_lane = 0xffffffffu, m_last = 0xffffffffu;
         const int w0 = first >> 5;
-        if (mask) {
-            const int w = w0 + lane;
-            m_lane = w >= 0 && w < a.words ? mask[w] : 0;
-            m_last = w0 + 32 < a.words && skew ? mask[w0 + 32] : 0;
-        }
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int v = first + (u * 32 + lane) * kPer;
-            const bool whole = v >= v0 && v + kPer <= v1;
-            uint32_t allowed = 0xffffffffu;                               // bit i: v + i may be chosen
+        auto load_mask = [&]() {
             if (mask) {
-                const int k = (v >> 5) - w0;
-                allowed = __shfl_sync(0xffffffffu, m_lane, k & 31);
-                if (skew) {
-                    uint32_t next = __shfl_sync(0xffffffffu, m_lane, (k + 1) & 31);
-                    allowed = k == 32 ? m_last : allowed;
-                    next = k == 31 ? m_last : next;                       // (v + i never reaches word 33)
-                    allowed = __funnelshift_r(allowed, next, v & 31);
-                } else allowed >>= v & 31;
+                const int w = w0 + lane;
+                m_lane = w >= 0 && w < a.words ? mask[w] : 0;
+                m_last = w0 + 32 < a.words && skew ? mask[w0 + 32] : 0;
             }
-            if (dismiss) {
-                float x[kPer], top = whole ? Wide<T>::top(in[u]) : -INFINITY;
-                if (__any_sync(0xffffffffu, top > bar)) {
-                    // the largest of each lane first: after it most others are at or below the bar
-                    const float from = bar;
-                    uint32_t ok = whole ? allowed & ~bits_at(rare, v - v0, bit_words + 1) : 0;
-                    Wide<T>::widen(in[u], x);
+        };
+        auto allowed_at = [&](int v) -> uint32_t {
+            if (!mask) return 0xffffffffu;
+            const int k = (v >> 5) - w0;
+            const uint32_t w = __shfl_sync(0xffffffffu, m_lane, k & 31);
+            if (!skew) return w >> (v & 31);
+            const uint32_t next = __shfl_sync(0xffffffffu, m_lane, (k + 1) & 31);
+            return __funnelshift_r(k == 32 ? m_last : w, k == 31 ? m_last : next, v & 31);      // (v + i never reaches word 33)
+        };
+        auto rare_at = [&](int v) -> uint32_t {                           // (bits past the slice's do not matter)
+            return v >= v0 && v < v1 ? bits_at(rare, v - v0, bit_words + 1) : v < v0 && v + kPer > v0 ? rare[0] << (v0 - v) : 0;
+        };
+        if (dismiss) {
+            float top = Wide<T>::top(in[0]);
 #pragma unroll
-                    for (int i = 0; i < kPer; ++i) x[i] = ((ok >> i) & 1u) && x[i] > from ? x[i] : -INFINITY;
-                    while (true) {
-                        top = x[0];
-                        int i = 0;
+            for (int u = 1; u < kLoads; ++u) top = fmaxf(top, Wide<T>::top(in[u]));
+            if (__any_sync(0xffffffffu, top > bar)) {
+                load_mask();
 #pragma unroll
-                        for (int k = 1; k < kPer; ++k) if (x[k] > top) { top = x[k]; i = k; }
-                        const bool look = top >= bar && top > -INFINITY;
-                        if (!__any_sync(0xffffffffu, look)) break;
-                        if (look) {
-                            const float y = a.count ? penalise(top, made_from(counter[v + i - v0])) : top;
-                            if (y > best || (y == best && v + i < best_v && y > -INFINITY)) { best = y; best_v = v + i; }
+                for (int u = 0; u < kLoads; ++u) {
+                    const int v = first + (u * 32 + lane) * kPer;
+                    in[u] = Wide<T>::keep(in[u], allowed_at(v) & ~rare_at(v));
+                }
+                // each lane looks at its largest: after that most others are at or below the bar
+                const float from = bar;
+                while (true) {
+                    uint4 q = in[0];
+                    int at = 0, i = 0;
+                    top = Wide<T>::top(q);
 #pragma unroll
-                            for (int k = 0; k < kPer; ++k) x[k] = k == i ? -INFINITY : x[k];
-                        }
-                        bar = fmaxf(bar, __uint_as_float(unordered(__reduce_max_sync(0xffffffffu, ordered(best)))));
+                    for (int u = 1; u < kLoads; ++u) {
+                        const float t = Wide<T>::top(in[u]);
+                        if (t > top || !(top == top)) { top = t; q = in[u]; at = u; }
                     }
+                    const bool look = top > from && top >= bar;
+                    if (!__any_sync(0xffffffffu, look)) break;
+                    i = Wide<T>::find(q, top);
+                    if (look) {
+                        const int v = first + (at * 32 + lane) * kPer + i;
+                        const float y = a.count ? penalise(top, made_from(counter[v - v0])) : top;
+                        if (y > best || (y == best && v < best_v && y > -INFINITY)) { best = y; best_v = v; }
+                        q = Wide<T>::keep(q, ~(1u << i));
+#pragma unroll
+                        for (int u = 0; u < kLoads; ++u) if (at == u) in[u] = q;
+                    }
+                    bar = fmaxf(bar, __uint_as_float(unordered(__reduce_max_sync(0xffffffffu, ordered(best)))));
                 }
             }
-            if (whole) {
-                if (!dismiss) {
-                    const uint32_t few = bits_at(rare, v - v0, bit_words + 1) & ((1u << kPer) - 1), ok = allowed & ~few;
-                    float x[kPer];
-                    Wide<T>::widen(in[u], x);
-                    if (a.count) {
-                        float made[kPer];
-                        if (table_wide) {
+        } else {
+            load_mask();
 #pragma unroll
-                            for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(made + i) = *reinterpret_cast<const float4*>(made_of + (v - v0) + i);
+            for (int u = 0; u < kLoads; ++u) {
+                const int v = first + (u * 32 + lane) * kPer;
+                const uint32_t allowed = allowed_at(v), few = rare_at(v) & ((1u << kPer) - 1), ok = allowed & ~few;
+                if (v + kPer <= v0 || v >= v1) continue;
+                float x[kPer];
+                Wide<T>::widen(in[u], x);
+                if (a.count) {
+                    float made[kPer];
+                    if (table_wide && v >= v0 && v + kPer <= v1) {
+#pragma unroll
+                        for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(made + i) = *reinterpret_cast<const float4*>(made_of + (v - v0) + i);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) made[i] = made_of[min(max(v + i - v0, 0), W - 1)];
+                    }
+                    float seen = made[0], low = fabsf(x[0]), high = x[0];
+#pragma unroll
+                    for (int i = 1; i < kPer; ++i) { seen = fmaxf(seen, made[i]); low = fminf(low, fabsf(x[i])); high = fmaxf(high, x[i]); }
+                    if (seen >= 0.f) {
+                        if (low >= 0x1p-60f && high <= 0x1p60f && rep_plain) {
+#pragma unroll
+                            for (int i = 0; i < kPer; ++i) x[i] = penalise_plain(x[i], made[i]);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < kPer; ++i) made[i] = made_of[v - v0 + i];
-                        }
-                        bool odd = false;
-#pragma unroll
-                        for (int i = 0; i < kPer; ++i) x[i] = penalise_plain(x[i], made[i], odd);
-                        if (odd) {
-#pragma unroll
-                            for (int i = 0; i < kPer; ++i) x[i] = penalise(Wide<T>::pick(in[u], i), made[i]);
-                        }
-                    }
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < kPer; ++i) {
-                        x[i] = (ok >> i) & 1u ? x[i] : -INFINITY;
-                        top = fmaxf(top, x[i]);
-                    }
-                    if (top > best) {
-                        best = top;
-#pragma unroll
-                        for (int i = kPer - 1; i >= 0; --i) best_v = x[i] == top ? v + i : best_v;
-                    }
-                    if (kOut) {
-                        if (few) {                                        // as they were, for the list below (out may be the logits)
-#pragma unroll
-                            for (int i = 0; i < kPer; ++i) x[i] = (few >> i) & 1u ? Wide<T>::pick(in[u], i) : x[i];
-                        }
-                        if (out_wide) __stcs(reinterpret_cast<uint4*>(out + v), Wide<T>::narrow(x));
-                        else {
-#pragma unroll
-                            for (int i = 0; i < kPer; ++i) Wide<T>::store(out + v + i, x[i]);
+                            for (int i = 0; i < kPer; ++i) x[i] = penalise(x[i], made[i]);
                         }
                     }
                 }
-            } else if (v + kPer > v0 && v < v1) {                         // the slice begins or ends inside these 16 bytes
-                for (int i = max(0, v0 - v); i < kPer && v + i < v1; ++i) {
-                    const int l = v + i - v0;
-                    if ((rare[l >> 5] >> (l & 31)) & 1u) continue;
-                    float y = Wide<T>::load(row + v + i);
-                    if (a.count) y = penalise(y, dismiss ? made_from(counter[l]) : made_of[l]);
-                    if (mask && !((mask[(v + i) >> 5] >> ((v + i) & 31)) & 1u)) y = -INFINITY;
-                    if (y > best) { best = y; best_v = v + i; }
-                    if (kOut) Wide<T>::store(out + v + i, y);
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    x[i] = (ok >> i) & 1u ? x[i] : -INFINITY;
+                    top = fmaxf(top, x[i]);
+                }
+                if (v < v0 || v + kPer > v1) {
+                    top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) if (v + i >= v0 && v + i < v1) top = fmaxf(top, x[i]);
+                }
+                if (top > best) {
+                    best = top;
+#pragma unroll
+                    for (int i = kPer - 1; i >= 0; --i) best_v = x[i] == top && v + i >= v0 ? v + i : best_v;
+                }
+                if (kOut) {
+                    if (few) {                                            // as they were, for the list below (out may be the logits)
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) x[i] = (few >> i) & 1u ? Wide<T>::pick(in[u], i) : x[i];
+                    }
+                    if (out_wide && v >= v0 && v + kPer <= v1) __stcs(reinterpret_cast<uint4*>(out + v), Wide<T>::narrow(x));
+                    else {
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) if (v + i >= v0 && v + i < v1) Wide<T>::store(out + v + i, x[i]);
+                    }
                 }
             }
         }
