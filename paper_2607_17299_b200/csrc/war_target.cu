@@ -321,16 +321,12 @@ war_target_kernel(const TargetArgs a) {
             if (o) bar = fmaxf(bar, __uint_as_float(unordered(o - (o == 0x80000000u ? 2 : 1))));
         }
         const float bar_in = bar;
-        uint4 in[kLoads];
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
+        auto fetch = [&](int u) -> uint4 {
             const int v = first + (u * 32 + lane) * kPer;
-            if (v >= v0 && v + kPer <= v1) in[u] = __ldcs(reinterpret_cast<const uint4*>(row + v));
-            else {                                                        // (a slice may begin or end inside 16 bytes)
-                in[u] = Wide<T>::nothing();
-                if (v + kPer > v0 && v < v1) in[u] = Wide<T>::part(row + v, v0 - v, v1 - v);
-            }
-        }
+            if (v >= v0 && v + kPer <= v1) return __ldcs(reinterpret_cast<const uint4*>(row + v));
+            // (a slice may begin or end inside 16 bytes)
+            return v + kPer > v0 && v < v1 ? Wide<T>::part(row + v, v0 - v, v1 - v) : Wide<T>::nothing();
+        };
         // the piece's mask words: at most 33, a lane each; tokens that may be chosen here, rare ones are looked at below
         uint32_t m_lane = 0xffffffffu, m_last = 0xffffffffu;
         const int w0 = first >> 5;
@@ -353,6 +349,9 @@ war_target_kernel(const TargetArgs a) {
             return v >= v0 && v < v1 ? bits_at(rare, v - v0, bit_words + 1) : v < v0 && v + kPer > v0 ? rare[0] << (v0 - v) : 0;
         };
         if (dismiss) {
+            uint4 in[kLoads];
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) in[u] = fetch(u);
             float top = Wide<T>::top(in[0]);
 #pragma unroll
             for (int u = 1; u < kLoads; ++u) top = fmaxf(top, Wide<T>::top(in[u]));
@@ -389,14 +388,19 @@ war_target_kernel(const TargetArgs a) {
                 }
             }
         } else {
+            // (rolled, three loads ahead: unrolled, its code no longer stays in the instruction cache)
+            uint4 in0 = fetch(0), in1 = fetch(1), in2 = fetch(2);
             load_mask();
-#pragma unroll
+#pragma unroll 1
             for (int u = 0; u < kLoads; ++u) {
+                const uint4 in = in0;
+                in0 = in1; in1 = in2;
+                if (u + 3 < kLoads) in2 = fetch(u + 3);
                 const int v = first + (u * 32 + lane) * kPer;
                 const uint32_t allowed = allowed_at(v), few = rare_at(v) & ((1u << kPer) - 1), ok = allowed & ~few;
                 if (v + kPer <= v0 || v >= v1) continue;
                 float x[kPer];
-                Wide<T>::widen(in[u], x);
+                Wide<T>::widen(in, x);
                 if (a.count) {
                     float made[kPer];
                     if (table_wide && v >= v0 && v + kPer <= v1) {
@@ -438,7 +442,7 @@ war_target_kernel(const TargetArgs a) {
                 if (kOut) {
                     if (few) {                                            // as they were, for the list below (out may be the logits)
 #pragma unroll
-                        for (int i = 0; i < kPer; ++i) x[i] = (few >> i) & 1u ? Wide<T>::pick(in[u], i) : x[i];
+                        for (int i = 0; i < kPer; ++i) x[i] = (few >> i) & 1u ? Wide<T>::pick(in, i) : x[i];
                     }
                     if (out_wide && v >= v0 && v + kPer <= v1) __stcs(reinterpret_cast<uint4*>(out + v), Wide<T>::narrow(x));
                     else {
@@ -559,7 +563,7 @@ extern "C" war_status_t war_target(const void* d_logits, const int32_t* d_num_no
     // blocks an SM); rows are dealt to more clusters of a request only if that leaves room: each counts the context again.
     const int resident = 2 * 148;
     const int most = (p->V + kSegment * 2 - 1) / (kSegment * 2), least = (p->V + kMaxSlice - 1) / kMaxSlice;
-    int slices = (resident * 2 + p->B - 1) / p->B;
+    int slices = (resident * 3 / 2 + p->B - 1) / p->B;
     slices = slices > most ? most : slices;
     slices = slices > kMaxSlices ? kMaxSlices : slices < least ? least : slices;
     a.slice = ((p->V + slices - 1) / slices + 31) / 32 * 32;
