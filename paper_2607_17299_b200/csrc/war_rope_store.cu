@@ -10,10 +10,10 @@
 // Nothing here computes much: each value is read once and written once, and what matters is that every SM has rows to
 // move.  A thread block works for one request: it fills a table of (c, s) for the request's slots (shared by all heads
 // and both roles), and its warps then take tasks,
-//   rows    one slot, up to kHeadsPerTask heads: half a warp per row, eight elements (16 bytes) a lane, the partner
-//           element eight lanes' worth away comes by shuffle; the lane's (c, s) stay in registers over the heads
+//   rows    one slot, up to kHeadsPerTask heads: eight lanes a row, two groups of eight elements (16 bytes) a lane, chosen so
+//           that an element and its partner are the same lane's; the lane's (c, s) stay in registers over the heads
 //   blocks  (8-bit pools) one head's K or V rows of one scale block: largest magnitude first, then the scale, the
-//           re-encoding of older rows if the scale has grown, and the new rows (read again, from L1)
+//           re-encoding of older rows if the scale has grown, and the new rows (turned again from the kept input)
 // and the request's tasks are dealt over several thread blocks when there are few requests.
 #include <cuda_bf16.h>
 #include <math.h>
@@ -23,10 +23,13 @@
 namespace {
 
 constexpr int kMaxSlots = 64;
-constexpr int kThreads = 256;
+constexpr int kThreads = 384;
 constexpr int kWarps = kThreads / 32;
 constexpr int kHeadsPerTask = 8;
-constexpr int kTargetBlocks = 148 * 6;        // thread blocks that keep a B200 busy with rows
+constexpr int kResident = 148 * 2;            // thread blocks that a B200 holds at a time
+// How a lane's elements are laid out: kSplit (a pair is half the rotation apart), kAdjacent (a pair is two neighbours), both
+// where the rotation covers whole lanes; kOdd takes every other rot_dim, through shared memory.
+constexpr int kSplit = 0, kAdjacent = 1, kOdd = 2;
 
 struct StoreArgs {
     const __nv_bfloat16 *q, *k, *v;
@@ -43,81 +46,113 @@ struct StoreArgs {
     int N, Hq, Hkv, page_size, max_pages, half, interleaved, block, blocks_per_page;
 };
 
-struct Row { float x[8]; };
+struct Raw { uint4 a, b; };                   // a lane's two groups of a row
+struct Row { float a[8], b[8]; };
+struct Turn { float c[8], s[8]; };            // of the lane's eight pairs
 
-__device__ __forceinline__ Row widen(const uint4 u) {
-    Row r;
+__device__ __forceinline__ void widen(const uint4& u, float* x) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { r.x[2 * i] = __uint_as_float(w[i] << 16); r.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    return r;
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
 }
-__device__ __forceinline__ uint4 narrow(const Row& r) {
+__device__ __forceinline__ Row widen(const Raw& r) {
+    Row x;
+    widen(r.a, x.a); widen(r.b, x.b);
+    return x;
+}
+__device__ __forceinline__ uint4 narrow(const float* x) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(r.x[2 * i], r.x[2 * i + 1]);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// This lane's eight (c, s): elements 8 * sub .. 8 * sub + 7 of a head.  Elements that do not rotate get (1, 0).
-struct Turn { float c[8], s[8]; };
-__device__ __forceinline__ Turn load_turn(const float2* table, int sub, int half, int interleaved) {
+// What a lane knows about its place in a row.
+struct Place {
+    int s, a, b;                              // lane of the row (0 to 7); first elements of its groups
+    int half, interleaved;
+    bool turns;                               // its elements rotate (kSplit, kAdjacent)
+    float* scratch;                           // 128 floats of this row's eight lanes (kOdd)
+};
+template <int kMode>
+__device__ __forceinline__ Place place(int lane, int half, int interleaved, float* scratch) {
+    Place p;
+    p.s = lane & 7; p.half = half; p.interleaved = interleaved; p.scratch = scratch;
+    const int g = half >> 3;                                              // lanes that rotate
+    p.turns = p.s < g;
+    const bool split = kMode == kSplit && p.turns;
+    // kSplit: group s and the one half the rotation later; lanes past the rotation share the groups behind it: 2 * s and 2 * s + 1
+    p.a = split ? 8 * p.s : 16 * p.s;
+    p.b = split ? 8 * p.s + half : 16 * p.s + 8;
+    return p;
+}
+
+// Where pair i of a slot stands in its row of the table: so that eight lanes read 16 bytes each side by side.
+template <int kMode>
+__device__ __forceinline__ int table_at(int i, int half) {
+    return kMode == kOdd ? i : ((i & 7) >> 1) * (half >> 3) * 2 + (i >> 3) * 2 + (i & 1);
+}
+template <int kMode>
+__device__ __forceinline__ Turn load_turn(const float2* table, const Place& p) {
     Turn t;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int e = sub * 8 + i;
-        const int pair = interleaved ? e >> 1 : (e < half ? e : e - half);
-        float2 cs = make_float2(1.f, 0.f);
-        if (e < 2 * half) cs = table[pair];
-        const bool first = interleaved ? !(e & 1) : e < half;
-        t.c[i] = cs.x;
-        t.s[i] = first ? -cs.y : cs.y;
+    for (int k = 0; k < 4; ++k) {
+        float4 v = make_float4(1.f, 0.f, 1.f, 0.f);
+        if (kMode != kOdd && p.turns) v = reinterpret_cast<const float4*>(table)[k * (p.half >> 3) + p.s];
+        t.c[2 * k] = v.x; t.s[2 * k] = v.y; t.c[2 * k + 1] = v.z; t.s[2 * k + 1] = v.w;
     }
     return t;
 }
 
-// Rotates a row held by 16 lanes, eight elements each; `scratch`: 128 floats of this half-warp, used only when the
-// partner of an element does not sit at the same place of another lane.  All 32 lanes call it together.
-__device__ __forceinline__ void rotate(Row& r, const Turn& t, int sub, int lane, int half, int interleaved, float* scratch) {
-    Row p;
-    if (interleaved) {
+// separate roundings of the two products: the value does not depend on which of them a fused operation would keep
+__device__ __forceinline__ void turn_pair(float& x, float& y, float c, float s) {
+    const float u = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s)), v = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
+    x = u; y = v;
+}
+// Rotates the rows of a warp, four of them.  All 32 lanes call it together.
+template <int kMode>
+__device__ __forceinline__ void rotate(Row& r, const Turn& t, const float2* table, const Place& p) {
+    if constexpr (kMode == kSplit) {
+        if (p.turns) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p.x[i] = r.x[i ^ 1];
-    } else if ((half & 7) == 0) {
-        const int off = half >> 3;                                        // lanes between a pair's two elements
-        const int src = (lane & 16) | ((sub < off ? sub + off : sub - off) & 15);
+            for (int i = 0; i < 8; ++i) turn_pair(r.a[i], r.b[i], t.c[i], t.s[i]);
+        }
+    } else if constexpr (kMode == kAdjacent) {
+        if (p.turns) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p.x[i] = __shfl_sync(0xffffffffu, r.x[i], src);
+            for (int i = 0; i < 4; ++i) {
+                turn_pair(r.a[2 * i], r.a[2 * i + 1], t.c[i], t.s[i]);
+                turn_pair(r.b[2 * i], r.b[2 * i + 1], t.c[i + 4], t.s[i + 4]);
+            }
+        }
     } else {
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) scratch[sub * 8 + i] = r.x[i];
+        for (int i = 0; i < 8; ++i) { p.scratch[p.a + i] = r.a[i]; p.scratch[p.b + i] = r.b[i]; }
+        __syncwarp();
+#pragma unroll 1
+        for (int k = p.s; k < p.half; k += 8) {
+            const float2 cs = table[k];
+            float* x = p.scratch + (p.interleaved ? 2 * k : k);
+            turn_pair(x[0], x[p.interleaved ? 1 : p.half], cs.x, cs.y);
+        }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = sub * 8 + i;
-            const int o = e < half ? e + half : (e < 2 * half ? e - half : e);
-            p.x[i] = scratch[o];
-        }
-    }
-    // separate roundings of the two products: the value does not depend on which of them a fused operation would keep
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float y = __fadd_rn(__fmul_rn(r.x[i], t.c[i]), __fmul_rn(p.x[i], t.s[i]));
-        r.x[i] = sub * 8 + i < 2 * half ? y : r.x[i];
+        for (int i = 0; i < 8; ++i) { r.a[i] = p.scratch[p.a + i]; r.b[i] = p.scratch[p.b + i]; }
     }
 }
 
-__global__ void __launch_bounds__(kThreads)
-war_rope_store_kernel(const StoreArgs a, const int kv, const int parts) {
-    extern __shared__ float2 s_table[];                                   // [N][half]
+template <int kv, int kMode>
+__global__ void __launch_bounds__(kThreads, 2)
+war_rope_store_kernel(const StoreArgs a, const int parts) {
+    extern __shared__ __align__(16) float2 s_table[];                     // [N][half]
     __shared__ int s_depth[kMaxSlots];
-    __shared__ float s_scratch[kWarps][2][128];
+    __shared__ float s_scratch[kMode == kOdd ? kWarps : 1][4][128];
     const int b = blockIdx.x, part = blockIdx.y;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, sub = lane & 15, side = lane >> 4;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, side = lane >> 3;
     const int n = a.num_nodes[b], pl = a.prefix_len[b];
     bool bad = n < 0 || n > a.N || pl < 0;
     if (!bad && warp == 0) {
@@ -151,15 +186,6 @@ war_rope_store_kernel(const StoreArgs a, const int kv, const int parts) {
         if (tid == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
         return;
     }
-    for (int x = tid; x < n * a.half; x += kThreads) {
-        const int j = x / a.half, i = x - j * a.half;
-        const double turns = (double)(pl + s_depth[j]) * ((double)a.inv_freq[i] * 0.15915494309189533577);
-        double s, c;
-        sincospi(2.0 * (turns - rint(turns)), &s, &c);
-        s_table[x] = make_float2((float)(c * (double)a.factor), (float)(s * (double)a.factor));
-    }
-    __syncthreads();
-
     const int32_t* pt = a.page_table + (size_t)b * a.max_pages;
     const int first_block = pl / a.block;
     const int blocks = kv == kKvBf16 ? 0 : (pl + n - 1) / a.block - first_block + 1;
@@ -167,104 +193,179 @@ war_rope_store_kernel(const StoreArgs a, const int kv, const int parts) {
     const int heads = a.Hq + (kv == kKvBf16 ? 2 * a.Hkv : 0);             // heads the row tasks cover: q, then k and v of a bf16 pool
     const int chunks = (heads + kHeadsPerTask - 1) / kHeadsPerTask;
     const int tasks = block_tasks + n * chunks;
-    float* scratch = s_scratch[warp][side];
+    const Place at = place<kMode>(lane, a.half, a.interleaved, s_scratch[kMode == kOdd ? warp : 0][side]);
 
-    for (int task = part * kWarps + warp; task < tasks; task += parts * kWarps) {
+    constexpr int kKept = 2;                                              // rows of a lane that are in registers at a time
+    static_assert(kHeadsPerTask == 4 * kKept, "a row task is one load");
+    Raw in[kKept];
+    auto fetch = [&](int u, const __nv_bfloat16* src, bool valid) {
+        in[u].a = in[u].b = make_uint4(0, 0, 0, 0);
+        if (valid) {
+            in[u].a = *reinterpret_cast<const uint4*>(src + at.a);
+            in[u].b = *reinterpret_cast<const uint4*>(src + at.b);
+        }
+    };
+    auto fetch_heads = [&](int j, int h0) {
+#pragma unroll
+        for (int u = 0; u < kKept; ++u) {
+            const int h = h0 + 4 * u + side;
+            fetch(u, h < a.Hq ? a.q + b * a.qs[0] + j * a.qs[1] + h * a.qs[2]
+                     : h < a.Hq + a.Hkv ? a.k + b * a.ks[0] + j * a.ks[1] + (h - a.Hq) * a.ks[2]
+                                        : a.v + b * a.vs[0] + j * a.vs[1] + (h - a.Hq - a.Hkv) * a.vs[2], h < heads);
+        }
+    };
+    auto fetch_rows = [&](int which, int h, int j, int j1) {
+        const long long* ss = which ? a.vs : a.ks;
+        const __nv_bfloat16* src = (which ? a.v : a.k) + b * ss[0] + h * ss[2];
+#pragma unroll
+        for (int u = 0; u < kKept; ++u) fetch(u, src + (j + 4 * u + side) * ss[1], j + 4 * u + side < j1);
+    };
+    auto fetch_task = [&](int task) {
+        if (task >= block_tasks) {
+            const int r = task - block_tasks, j = r / chunks;
+            fetch_heads(j, (r - j * chunks) * kHeadsPerTask);
+        } else {
+            const int pos0 = (first_block + (task >> 1) / a.Hkv) * a.block;
+            fetch_rows(task & 1, (task >> 1) % a.Hkv, max(0, pos0 - pl), min(n, pos0 + a.block - pl));
+        }
+    };
+    // the first task's values arrive while the table is filled
+    int task = part * kWarps + warp;
+    if (task < tasks) fetch_task(task);
+    for (int x = tid; x < n * a.half; x += kThreads) {
+        const int j = x / a.half, i = x - j * a.half;
+        const double turns = (double)(pl + s_depth[j]) * ((double)a.inv_freq[i] * 0.15915494309189533577);
+        double s, c;
+        sincospi(2.0 * (turns - rint(turns)), &s, &c);
+        s_table[j * a.half + table_at<kMode>(i, a.half)] = make_float2((float)(c * (double)a.factor), (float)(s * (double)a.factor));
+    }
+    __syncthreads();
+
+
+    for (bool first = true; task < tasks; task += parts * kWarps, first = false) {
+        if (!first) fetch_task(task);
         if (task >= block_tasks) {
             const int r = task - block_tasks, j = r / chunks, h0 = (r - j * chunks) * kHeadsPerTask;
-            const Turn turn = load_turn(s_table + j * a.half, sub, a.half, a.interleaved);
+            const float2* table = s_table + j * a.half;
+            const Turn turn = load_turn<kMode>(table, at);
             const int h1 = min(h0 + kHeadsPerTask, heads);
-            uint4 in[kHeadsPerTask / 2];
 #pragma unroll
-            for (int u = 0; u < kHeadsPerTask / 2; ++u) {
-                const int h = h0 + 2 * u + side;
-                in[u] = make_uint4(0, 0, 0, 0);
-                if (h < h1) {
-                    const __nv_bfloat16* src = h < a.Hq ? a.q + b * a.qs[0] + j * a.qs[1] + h * a.qs[2]
-                                             : h < a.Hq + a.Hkv ? a.k + b * a.ks[0] + j * a.ks[1] + (h - a.Hq) * a.ks[2]
-                                                                : a.v + b * a.vs[0] + j * a.vs[1] + (h - a.Hq - a.Hkv) * a.vs[2];
-                    in[u] = *reinterpret_cast<const uint4*>(src + sub * 8);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kHeadsPerTask / 2; ++u) {
-                if (h0 + 2 * u >= h1) break;                              // (uniform: both halves of the warp rotate together)
-                const int h = h0 + 2 * u + side;
+            for (int u = 0; u < kKept; ++u) {
+                if (h0 + 4 * u >= h1) break;                              // (uniform: the warp's rows rotate together)
+                const int h = h0 + 4 * u + side;
                 Row row = widen(in[u]);
-                rotate(row, turn, sub, lane, a.half, a.interleaved, scratch);
+                rotate<kMode>(row, turn, table, at);
                 if (h >= h1) continue;
-                const uint4 out = h < a.Hq + a.Hkv ? narrow(row) : in[u];  // v is copied as it is
+                if (h < a.Hq + a.Hkv) { in[u].a = narrow(row.a); in[u].b = narrow(row.b); }    // v is copied as it is
+                __nv_bfloat16* dst;
                 if (h < a.Hq) {
-                    *reinterpret_cast<uint4*>(a.q_out + (((size_t)b * a.N + j) * a.Hq + h) * 128 + sub * 8) = out;
+                    dst = a.q_out + (((size_t)b * a.N + j) * a.Hq + h) * 128;
                 } else {
                     const int pos = pl + j;
                     const long long page = pt[pos / a.page_size];
                     if (page < 0 || page >= a.num_pages) {
-                        if (sub == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
+                        if (at.s == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
                         continue;
                     }
                     const bool is_k = h < a.Hq + a.Hkv;
                     const long long* st = is_k ? a.kp : a.vp;
                     const int kh = h - a.Hq - (is_k ? 0 : a.Hkv);
-                    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(is_k ? a.kpool : a.vpool) + page * st[0] + kh * st[1] + (long long)(pos % a.page_size) * st[2];
-                    *reinterpret_cast<uint4*>(dst + sub * 8) = out;
+                    dst = reinterpret_cast<__nv_bfloat16*>(is_k ? a.kpool : a.vpool) + page * st[0] + kh * st[1] + (long long)(pos % a.page_size) * st[2];
+                }
+                *reinterpret_cast<uint4*>(dst + at.a) = in[u].a;
+                *reinterpret_cast<uint4*>(dst + at.b) = in[u].b;
+            }
+            continue;
+        }
+        if constexpr (kv != kKvBf16) {
+            // ---- one scale block of one head's K or V
+            const int which = task & 1, h = (task >> 1) % a.Hkv, t = (task >> 1) / a.Hkv;
+            const int pos0 = (first_block + t) * a.block;
+            const int j0 = max(0, pos0 - pl), j1 = min(n, pos0 + a.block - pl);
+            const long long page = pt[pos0 / a.page_size];
+            if (page < 0 || page >= a.num_pages) {
+                if (lane == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
+                continue;
+            }
+            const long long* ps = which ? a.vp : a.kp;
+            const int row0 = pos0 % a.page_size;
+            uint8_t* dst = (which ? a.vpool : a.kpool) + page * ps[0] + h * ps[1] + (long long)row0 * ps[2];
+            float* scale = (which ? a.vscale : a.kscale) + (page * a.Hkv + h) * a.blocks_per_page + row0 / a.block;
+            const int old = min(max(pl - pos0, 0), a.block);              // rows of earlier tokens in the block
+            const float s_old = old > 0 ? *scale : 0.f;
+            auto turned = [&](const Raw& raw, int j) -> Row {
+                Row r = widen(raw);
+                if (!which) {
+                    const float2* table = s_table + min(j + side, j1 - 1) * a.half;
+                    rotate<kMode>(r, load_turn<kMode>(table, at), table, at);
+                }
+                return r;
+            };
+            float top = 0.f;
+            for (int j = j0; j < j1; j += 4 * kKept) {
+                if (j > j0) fetch_rows(which, h, j, j1);
+#pragma unroll
+                for (int u = 0; u < kKept; ++u) {
+                    const Row r = turned(in[u], j + 4 * u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(r.a[i]), fabsf(r.b[i])));
                 }
             }
-            continue;
-        }
-        // ---- one scale block of one head's K or V
-        const int which = task & 1, h = (task >> 1) % a.Hkv, t = (task >> 1) / a.Hkv;
-        const int pos0 = (first_block + t) * a.block;
-        const int j0 = max(0, pos0 - pl), j1 = min(n, pos0 + a.block - pl);
-        const long long page = pt[pos0 / a.page_size];
-        if (page < 0 || page >= a.num_pages) {
-            if (lane == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
-            continue;
-        }
-        const long long* ss = which ? a.vs : a.ks;
-        const __nv_bfloat16* src = (which ? a.v : a.k) + b * ss[0] + h * ss[2];
-        const long long* ps = which ? a.vp : a.kp;
-        const int row0 = pos0 % a.page_size;
-        uint8_t* dst = (which ? a.vpool : a.kpool) + page * ps[0] + h * ps[1] + (long long)row0 * ps[2];
-        float* scale = (which ? a.vscale : a.kscale) + (page * a.Hkv + h) * a.blocks_per_page + row0 / a.block;
-        const int old = min(max(pl - pos0, 0), a.block);                  // rows of earlier tokens in the block
-        const float s_old = old > 0 ? *scale : 0.f;
-        auto fetch = [&](int j) -> Row {
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (j < j1) u = *reinterpret_cast<const uint4*>(src + j * ss[1] + sub * 8);
-            Row r = widen(u);
-            if (!which) rotate(r, load_turn(s_table + min(j, j1 - 1) * a.half, sub, a.half, a.interleaved), sub, lane, a.half, a.interleaved, scratch);
-            return r;
-        };
-        float top = 0.f;
-        for (int j = j0; j < j1; j += 2) {
-            const Row r = fetch(j + side);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(r.x[i]));
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        float s_new = fmaxf(s_old, quant::pow2_scale(top, kv));
-        if (!(s_new > 0.f)) s_new = 1.f;
-        if (s_new != s_old && old > 0) {
-            const float ratio = s_old / s_new;
-            for (int r = side; r < old; r += 2) {
-                uint2* p = reinterpret_cast<uint2*>(dst + r * ps[2]) + sub;
-                *p = quant::recode8(*p, ratio, kv);
+            top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));    // (not negative, no NaN: ordered as integers)
+            float s_new = fmaxf(s_old, quant::pow2_scale(top, kv));
+            if (!(s_new > 0.f)) s_new = 1.f;
+            if (s_new != s_old && old > 0) {
+                const float ratio = s_old / s_new;
+                for (int r = side; r < old; r += 4) {
+                    uint4* p = reinterpret_cast<uint4*>(dst + r * ps[2]) + at.s;
+                    const uint4 c = *p;
+                    const uint2 lo = quant::recode8(make_uint2(c.x, c.y), ratio, kv), hi = quant::recode8(make_uint2(c.z, c.w), ratio, kv);
+                    *p = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                }
             }
-        }
-        for (int j = j0; j < j1; j += 2) {
-            const Row r = fetch(j + side);
-            if (j + side >= j1) continue;
-            uint32_t w[2];
+            // dividing by a power of two is multiplying by its reciprocal; a scale that was there may be another number
+            const bool pow2 = (__float_as_uint(s_new) & 0x7fffffu) == 0 && s_new >= kSmallestScale;
+            const float inv = 1.f / s_new;
+            auto codes = [&](float* x) -> uint2 {
+                if (pow2) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                w[i] = quant::encode2(r.x[4 * i] / s_new, r.x[4 * i + 1] / s_new, kv) |
-                       (quant::encode2(r.x[4 * i + 2] / s_new, r.x[4 * i + 3] / s_new, kv) << 16);
-            reinterpret_cast<uint2*>(dst + (long long)(pl + j + side - pos0) * ps[2])[sub] = make_uint2(w[0], w[1]);
+                    for (int i = 0; i < 8; ++i) x[i] *= inv;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = __fdiv_rn(x[i], s_new);
+                }
+                return make_uint2(quant::encode2(x[0], x[1], kv) | (quant::encode2(x[2], x[3], kv) << 16),
+                                  quant::encode2(x[4], x[5], kv) | (quant::encode2(x[6], x[7], kv) << 16));
+            };
+            for (int j = j0; j < j1; j += 4 * kKept) {
+                if (j1 - j0 > 4 * kKept) fetch_rows(which, h, j, j1);     // (else they are there)
+#pragma unroll
+                for (int u = 0; u < kKept; ++u) {
+                    const int x = j + 4 * u + side;
+                    if (j + 4 * u >= j1) break;
+                    Row r = turned(in[u], j + 4 * u);
+                    if (x >= j1) continue;
+                    uint8_t* to = dst + (long long)(pl + x - pos0) * ps[2];
+                    *reinterpret_cast<uint2*>(to + at.a) = codes(r.a);
+                    *reinterpret_cast<uint2*>(to + at.b) = codes(r.b);
+                }
+            }
+            if (lane == 0 && s_new != s_old) *scale = s_new;
         }
-        if (lane == 0 && s_new != s_old) *scale = s_new;
     }
+}
+
+template <int kv, int kMode>
+war_status_t launch(const StoreArgs& a, dim3 grid, size_t table, cudaStream_t s) {
+    if (kMode == kOdd && table > 8 * 1024)                                // next to its scratch: past the 48 KB that need no request
+        WAR_CUDA_TRY(cudaFuncSetAttribute(war_rope_store_kernel<kv, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024));
+    war_rope_store_kernel<kv, kMode><<<grid, kThreads, table, s>>>(a, (int)grid.y);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
+}
+template <int kv>
+war_status_t launch(const StoreArgs& a, int mode, dim3 grid, size_t table, cudaStream_t s) {
+    return mode == kSplit ? launch<kv, kSplit>(a, grid, table, s) : mode == kAdjacent ? launch<kv, kAdjacent>(a, grid, table, s) : launch<kv, kOdd>(a, grid, table, s);
 }
 
 }  // namespace
@@ -311,13 +412,14 @@ extern "C" war_status_t war_rope_store(const void* d_q, const void* d_k, const v
     const long long heads = p->Hq + (p->kv_type == kKvBf16 ? 2ll * p->Hkv : 0);
     const long long tasks = (p->kv_type == kKvBf16 ? 0 : 2ll * p->Hkv * ((p->N + a.block - 2) / a.block + 1)) +
                             (long long)p->N * ((heads + kHeadsPerTask - 1) / kHeadsPerTask);
-    long long parts = (kTargetBlocks + p->B - 1) / p->B;
+    long long parts = kResident / p->B;
     if (parts > (tasks + kWarps - 1) / kWarps) parts = (tasks + kWarps - 1) / kWarps;
     if (parts < 1) parts = 1;
+    const int mode = p->rot_dim % 16 != 0 ? kOdd : p->interleaved ? kAdjacent : kSplit;
     const size_t table = sizeof(float2) * (size_t)p->N * (size_t)(a.half > 0 ? a.half : 1);
-    war_rope_store_kernel<<<dim3(p->B, (unsigned)parts), kThreads, table, stream>>>(a, p->kv_type, (int)parts);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    const dim3 grid(p->B, (unsigned)parts);
+    return p->kv_type == kKvBf16 ? launch<kKvBf16>(a, mode, grid, table, stream)
+         : p->kv_type == kKvE4M3 ? launch<kKvE4M3>(a, mode, grid, table, stream) : launch<kKvE5M2>(a, mode, grid, table, stream);
 }
 
 // Frequencies of the rotation, worked out on the host in 64 bits and rounded once.
