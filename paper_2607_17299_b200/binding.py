@@ -7,6 +7,8 @@ raises."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import math
 import os
 from typing import Optional, Tuple
 
@@ -441,25 +443,40 @@ def _strided(t: torch.Tensor, ndim: int, *dtypes) -> int:
     return t.data_ptr()
 
 
-def _pool_args(k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale, v_scale):
-    """(kv_type, scale_block) of a cache; checks that the two pools and their scales belong together."""
-    kv = KV_TYPES.get(k_pool.dtype)
-    if kv is None or v_pool.dtype != k_pool.dtype or v_pool.shape != k_pool.shape or k_pool.dim() != 4:
+# What a call works out from its tensors' types, shapes and strides alone is kept by them: for a decoding step's small
+# tensors, filling these structures anew takes longer than the kernels.
+_by_layout = functools.lru_cache(maxsize=512)
+
+
+def _layout(t: Optional[torch.Tensor]):
+    return None if t is None else (t.dtype, t.shape, t.stride())
+
+
+@_by_layout
+def _pool_layout(k_pool, v_pool, k_scale, v_scale):
+    """(kv_type, scale_block) of a cache, from _layout of its tensors; checks that pools and scales belong together."""
+    kv = KV_TYPES.get(k_pool[0])
+    if kv is None or v_pool[0] != k_pool[0] or v_pool[1] != k_pool[1] or len(k_pool[1]) != 4:
         raise ValueError("pools must be [pages, Hkv, page_size, D] of one shape and one of the types " + ", ".join(map(str, KV_TYPES)))
     if kv == 0:
         if k_scale is not None or v_scale is not None:
             raise ValueError("a bf16 cache has no scales")
         return kv, 0
-    pages, Hkv, pg, _ = k_pool.shape
+    pages, Hkv, pg, _ = k_pool[1]
     for t in (k_scale, v_scale):
-        if t is None or t.dim() != 3 or t.shape[:2] != (pages, Hkv) or t.shape[2] < 1 or pg % t.shape[2] or t.shape != k_scale.shape:
+        if t is None or len(t[1]) != 3 or tuple(t[1][:2]) != (pages, Hkv) or t[1][2] < 1 or pg % t[1][2] or t[1] != k_scale[1]:
             raise ValueError("scales must be float32 [pages, Hkv, page_size / scale_block], the same for K and V")
-    return kv, pg // k_scale.shape[2]
+    return kv, pg // k_scale[1][2]
 
 
-def _shape(t: Optional[torch.Tensor], *want) -> None:
-    if t is not None and tuple(t.shape) != want:
-        raise ValueError(f"expected shape {want}, got {tuple(t.shape)}")
+def _pool_args(k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale, v_scale):
+    return _pool_layout(_layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
+
+
+def _want(t, *want) -> None:
+    """Checks the shape in a _layout."""
+    if t is not None and tuple(t[1]) != want:
+        raise ValueError(f"expected shape {want}, got {tuple(t[1])}")
 
 
 def war_rope_frequencies(rot_dim: int, base: float, kind: str = "plain", scale: float = 1.0, original_length: float = 0.0,
@@ -472,6 +489,32 @@ def war_rope_frequencies(rot_dim: int, base: float, kind: str = "plain", scale: 
     return out, float(f.value)
 
 
+@_by_layout
+def _store_params(q, k, v, freq, table, prefix, nodes, parent, k_pool, v_pool, k_scale, v_scale, q_out, interleaved, factor) -> RopeStoreParams:
+    if len(k[1]) != 4:
+        raise ValueError("d_k must be [B, N, Hkv, D]")
+    B, N, Hkv, D = k[1]
+    kv, block = _pool_layout(k_pool, v_pool, k_scale, v_scale)
+    _want(v, B, N, Hkv, D)
+    _want(k_pool, k_pool[1][0], Hkv, k_pool[1][2], D)
+    if tuple(prefix) != (B,) or tuple(nodes) != (B,) or tuple(parent) != (B, N):
+        raise ValueError("d_prefix_len and d_num_nodes must be [B], d_parent [B, N]")
+    if len(table) != 2 or table[0] != B or (q is None) != (q_out is None):
+        raise ValueError("page_table must be [B, max_pages]; d_q and d_q_out come together")
+    p = RopeStoreParams()
+    p.B, p.N, p.Hkv, p.D = B, N, Hkv, D
+    if q is not None:
+        if len(q[1]) != 4 or tuple(q[1]) != (B, N, q[1][2], D) or q_out != q[1]:
+            raise ValueError("d_q and d_q_out must be [B, N, Hq, D]")
+        p.Hq, p.q_strides[:] = q[1][2], q[2]
+    else:
+        p.Hq, p.q_strides[3] = 0, 1
+    p.page_size, p.max_pages_per_req, p.num_pages = k_pool[1][2], table[1], k_pool[1][0]
+    p.kv_type, p.scale_block, p.rot_dim, p.interleaved, p.factor = kv, block, 2 * math.prod(freq), int(interleaved), factor
+    p.k_strides[:], p.v_strides[:], p.kpool_strides[:], p.vpool_strides[:] = k[2], v[2], k_pool[2], v_pool[2]
+    return p
+
+
 def war_rope_store(d_q: Optional[torch.Tensor], d_k: torch.Tensor, d_v: torch.Tensor, d_inv_freq: torch.Tensor, page_table: torch.Tensor,
                    d_prefix_len: torch.Tensor, d_num_nodes: torch.Tensor, d_parent: torch.Tensor, k_pool: torch.Tensor,
                    v_pool: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor],
@@ -480,30 +523,9 @@ def war_rope_store(d_q: Optional[torch.Tensor], d_k: torch.Tensor, d_v: torch.Te
     bf16 [B, N, H, D], any strides the library accepts (the parts of one projection, say); rot_dim = 2 * len(d_inv_freq).
     Pools [pages, Hkv, page_size, D]: bf16 (no scales), or float8_e4m3fn / float8_e5m2 with float32 scales
     [pages, Hkv, page_size / scale_block]; updated in place.  d_q and d_q_out None: nothing but the store."""
-    B, N, Hkv, D = d_k.shape
-    kv, block = _pool_args(k_pool, v_pool, k_scale, v_scale)
-    _shape(d_v, B, N, Hkv, D)
-    _shape(k_pool, k_pool.shape[0], Hkv, k_pool.shape[2], D)
-    _shape(d_prefix_len, B)
-    _shape(d_num_nodes, B)
-    _shape(d_parent, B, N)
-    if page_table.dim() != 2 or page_table.shape[0] != B or (d_q is None) != (d_q_out is None):
-        raise ValueError("page_table must be [B, max_pages]; d_q and d_q_out come together")
-    p = RopeStoreParams()
-    p.B, p.N, p.Hkv, p.D = B, N, Hkv, D
-    if d_q is not None:
-        _shape(d_q, B, N, d_q.shape[2], D)
-        _shape(d_q_out, B, N, d_q.shape[2], D)
-        p.Hq = d_q.shape[2]
-        for i in range(4):
-            p.q_strides[i] = d_q.stride(i)
-    else:
-        p.Hq, p.q_strides[3] = 0, 1
-    p.page_size, p.max_pages_per_req, p.num_pages = k_pool.shape[2], page_table.shape[1], k_pool.shape[0]
-    p.kv_type, p.scale_block, p.rot_dim, p.interleaved, p.factor = kv, block, 2 * d_inv_freq.numel(), int(interleaved), factor
-    for i in range(4):
-        p.k_strides[i], p.v_strides[i] = d_k.stride(i), d_v.stride(i)
-        p.kpool_strides[i], p.vpool_strides[i] = k_pool.stride(i), v_pool.stride(i)
+    p = _store_params(_layout(d_q), _layout(d_k), _layout(d_v), d_inv_freq.shape, page_table.shape, d_prefix_len.shape, d_num_nodes.shape,
+                      d_parent.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale),
+                      None if d_q_out is None else d_q_out.shape, bool(interleaved), float(factor))
     bf16 = torch.bfloat16
     code = _lib.war_rope_store(None if d_q is None else _strided(d_q, 4, bf16), _strided(d_k, 4, bf16), _strided(d_v, 4, bf16),
                                _ptr(d_inv_freq, torch.float32), _ptr(page_table, torch.int32), _ptr(d_prefix_len, torch.int32),
@@ -549,6 +571,29 @@ def war_verify_attn_quant(d_q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch
     _check("war_verify_attn_quant", code)
 
 
+@_by_layout
+def _target_params(logits, out, mask, target, per_slot, per_request, offsets) -> TargetParams:
+    if len(logits[1]) != 3:
+        raise ValueError("d_logits must be [B, N, V]")
+    B, N, V = logits[1]
+    p = TargetParams()
+    p.B, p.N, p.V, p.dtype = B, N, V, int(logits[0] == torch.float32)
+    for t, strides, last in ((logits, p.logits_strides, V), (out, p.out_strides, V), (mask, p.mask_strides, (V + 31) // 32)):
+        if t is None:
+            continue
+        _want(t, B, N, last)
+        if t[2][2] != 1 and last > 1:
+            raise ValueError("logits, mask and out need unit stride along their last dimension")
+        strides[0], strides[1] = t[2][0], t[2][1]
+    if out is not None and out[0] != logits[0]:
+        raise ValueError("d_out must have the logits' type")
+    for shapes, want in (((target,) + per_slot, (B, N)), (per_request, (B,)), (offsets, (B + 1,))):
+        for shape in shapes:
+            if shape is not None and tuple(shape) != want:
+                raise ValueError(f"expected shape {want}, got {tuple(shape)}")
+    return p
+
+
 def war_target(d_logits: torch.Tensor, d_num_nodes: torch.Tensor, d_ids: Optional[torch.Tensor], d_parent: Optional[torch.Tensor],
                d_target: torch.Tensor, d_ctx: Optional[torch.Tensor] = None, d_ctx_off: Optional[torch.Tensor] = None,
                d_prompt_len: Optional[torch.Tensor] = None, d_repetition: Optional[torch.Tensor] = None,
@@ -559,27 +604,11 @@ def war_target(d_logits: torch.Tensor, d_num_nodes: torch.Tensor, d_ids: Optiona
     """Penalties, biases and grammar masks on d_logits (bf16 or float32 [B, N, V], unit stride along V), the chosen token of
     every slot into d_target [B, N] (what war_accept takes), the processed logits into d_out where it is given.
     d_mask: int32 words [B, N, ceil(V / 32)], unit stride along the words; expand() shares one mask."""
-    B, N, V = d_logits.shape
     f32, i32, i64 = torch.float32, torch.int32, torch.int64
-    p = TargetParams()
-    p.B, p.N, p.V, p.dtype = B, N, V, int(d_logits.dtype == f32)
-    words = (V + 31) // 32
-    for t, strides, last in ((d_logits, p.logits_strides, V), (d_out, p.out_strides, V), (d_mask, p.mask_strides, words)):
-        if t is None:
-            continue
-        _shape(t, B, N, last)
-        if t.stride(2) != 1 and last > 1:
-            raise ValueError("logits, mask and out need unit stride along their last dimension")
-        strides[0], strides[1] = t.stride(0), t.stride(1)
-    if d_out is not None and d_out.dtype != d_logits.dtype:
-        raise ValueError("d_out must have the logits' type")
-    _shape(d_target, B, N)
-    for t in (d_ids, d_parent):
-        _shape(t, B, N)
-    for t in (d_num_nodes, d_prompt_len, d_repetition, d_presence, d_frequency):
-        _shape(t, B)
-    for t in (d_ctx_off, d_bias_off):
-        _shape(t, B + 1)
+    p = _target_params(_layout(d_logits), _layout(d_out), None if d_mask is None else (None, d_mask.shape, d_mask.stride()), d_target.shape,
+                       tuple(None if t is None else t.shape for t in (d_ids, d_parent)),
+                       tuple(None if t is None else t.shape for t in (d_num_nodes, d_prompt_len, d_repetition, d_presence, d_frequency)),
+                       tuple(None if t is None else t.shape for t in (d_ctx_off, d_bias_off)))
     inputs = TargetInputs(_ptr(d_ctx, i32), _ptr(d_ctx_off, i64), _ptr(d_prompt_len, i32), _ptr(d_repetition, f32), _ptr(d_presence, f32),
                           _ptr(d_frequency, f32), _ptr(d_bias_off, i64), _ptr(d_bias_ids, i32), _ptr(d_bias_val, f32),
                           None if d_mask is None else _strided(d_mask, 3, i32))
@@ -591,20 +620,24 @@ def war_target(d_logits: torch.Tensor, d_num_nodes: torch.Tensor, d_ids: Optiona
     _check("war_target", code)
 
 
+@_by_layout
+def _commit_params(ids, tail, table, k_pool, v_pool, k_scale, v_scale) -> CommitQuantParams:
+    q = CommitQuantParams()
+    q.kv_type, q.scale_block = _pool_layout(k_pool, v_pool, k_scale, v_scale)
+    p = q.commit
+    p.B, p.N = ids
+    p.P = tail[1]
+    p.num_pages, p.Hkv, p.page_size, p.D = k_pool[1]
+    p.max_pages_per_req = table[1]
+    p.k_strides[:], p.v_strides[:] = k_pool[2], v_pool[2]
+    return q
+
+
 def war_commit_quant(d_ids: torch.Tensor, d_accept_len: torch.Tensor, d_accept_path: torch.Tensor, d_bonus: torch.Tensor,
                      k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page_table: torch.Tensor,
                      d_prefix_len: torch.Tensor, d_tail: torch.Tensor, d_tail_len: torch.Tensor) -> None:
     """war_commit for a float8_e4m3fn / float8_e5m2 cache; pools and scales are updated in place."""
-    B, N = d_ids.shape
-    q = CommitQuantParams()
-    q.kv_type, q.scale_block = _pool_args(k_pool, v_pool, k_scale, v_scale)
-    p = q.commit
-    p.B, p.N, p.P = B, N, d_tail.shape[1]
-    p.Hkv, p.D, p.page_size = k_pool.shape[1], k_pool.shape[3], k_pool.shape[2]
-    p.max_pages_per_req, p.num_pages = page_table.shape[1], k_pool.shape[0]
-    for i in range(4):
-        p.k_strides[i] = k_pool.stride(i)
-        p.v_strides[i] = v_pool.stride(i)
+    q = _commit_params(d_ids.shape, d_tail.shape, page_table.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
     code = _lib.war_commit_quant(_ptr(d_ids, torch.int32), _ptr(d_accept_len, torch.int32), _ptr(d_accept_path, torch.int32),
                                  _ptr(d_bonus, torch.int32), _strided(k_pool, 4, *KV_TYPES), _strided(v_pool, 4, *KV_TYPES),
                                  _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), _ptr(page_table, torch.int32), C.byref(q),
