@@ -108,7 +108,13 @@ def status_string(code: int) -> str:
     return _lib.war_status_string(int(code)).decode()
 
 
+# (building a torch.cuda.Stream for every call takes 3 us of the host; the raw handle is the same)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -452,6 +458,25 @@ def _layout(t: Optional[torch.Tensor]):
     return None if t is None else (t.dtype, t.shape, t.stride())
 
 
+def _address(t: Optional[torch.Tensor]) -> Optional[int]:
+    """Address of a device tensor whose type and strides have been looked at through _layout."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("device buffers must be CUDA tensors")
+    return t.data_ptr()
+
+
+def _is_contiguous(t) -> bool:
+    """As Tensor.is_contiguous, of a _layout."""
+    step = 1
+    for size, stride in zip(reversed(t[1]), reversed(t[2])):
+        if size != 1 and stride != step and 0 not in t[1]:
+            return False
+        step *= size
+    return True
+
+
 @_by_layout
 def _pool_layout(k_pool, v_pool, k_scale, v_scale):
     """(kv_type, scale_block) of a cache, from _layout of its tensors; checks that pools and scales belong together."""
@@ -466,6 +491,8 @@ def _pool_layout(k_pool, v_pool, k_scale, v_scale):
     for t in (k_scale, v_scale):
         if t is None or len(t[1]) != 3 or tuple(t[1][:2]) != (pages, Hkv) or t[1][2] < 1 or pg % t[1][2] or t[1] != k_scale[1]:
             raise ValueError("scales must be float32 [pages, Hkv, page_size / scale_block], the same for K and V")
+        if t[0] != torch.float32 or not _is_contiguous(t):
+            raise ValueError("scales must be contiguous float32")
     return kv, pg // k_scale[1][2]
 
 
@@ -495,6 +522,8 @@ def _store_params(q, k, v, freq, table, prefix, nodes, parent, k_pool, v_pool, k
         raise ValueError("d_k must be [B, N, Hkv, D]")
     B, N, Hkv, D = k[1]
     kv, block = _pool_layout(k_pool, v_pool, k_scale, v_scale)
+    if k[0] != torch.bfloat16 or v[0] != torch.bfloat16 or (q is not None and q[0] != torch.bfloat16):
+        raise ValueError("d_q, d_k and d_v must be bfloat16")
     _want(v, B, N, Hkv, D)
     _want(k_pool, k_pool[1][0], Hkv, k_pool[1][2], D)
     if tuple(prefix) != (B,) or tuple(nodes) != (B,) or tuple(parent) != (B, N):
@@ -526,12 +555,10 @@ def war_rope_store(d_q: Optional[torch.Tensor], d_k: torch.Tensor, d_v: torch.Te
     p = _store_params(_layout(d_q), _layout(d_k), _layout(d_v), d_inv_freq.shape, page_table.shape, d_prefix_len.shape, d_num_nodes.shape,
                       d_parent.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale),
                       None if d_q_out is None else d_q_out.shape, bool(interleaved), float(factor))
-    bf16 = torch.bfloat16
-    code = _lib.war_rope_store(None if d_q is None else _strided(d_q, 4, bf16), _strided(d_k, 4, bf16), _strided(d_v, 4, bf16),
-                               _ptr(d_inv_freq, torch.float32), _ptr(page_table, torch.int32), _ptr(d_prefix_len, torch.int32),
-                               _ptr(d_num_nodes, torch.int32), _ptr(d_parent, torch.int32), C.byref(p),
-                               _strided(k_pool, 4, *KV_TYPES), _strided(v_pool, 4, *KV_TYPES), _ptr(k_scale, torch.float32),
-                               _ptr(v_scale, torch.float32), _ptr(d_q_out, bf16), _stream())
+    code = _lib.war_rope_store(_address(d_q), _address(d_k), _address(d_v), _ptr(d_inv_freq, torch.float32), _ptr(page_table, torch.int32),
+                               _ptr(d_prefix_len, torch.int32), _ptr(d_num_nodes, torch.int32), _ptr(d_parent, torch.int32), C.byref(p),
+                               _address(k_pool), _address(v_pool), _address(k_scale), _address(v_scale), _ptr(d_q_out, torch.bfloat16),
+                               _stream())
     _check("war_rope_store", code)
 
 
@@ -639,7 +666,7 @@ def war_commit_quant(d_ids: torch.Tensor, d_accept_len: torch.Tensor, d_accept_p
     """war_commit for a float8_e4m3fn / float8_e5m2 cache; pools and scales are updated in place."""
     q = _commit_params(d_ids.shape, d_tail.shape, page_table.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
     code = _lib.war_commit_quant(_ptr(d_ids, torch.int32), _ptr(d_accept_len, torch.int32), _ptr(d_accept_path, torch.int32),
-                                 _ptr(d_bonus, torch.int32), _strided(k_pool, 4, *KV_TYPES), _strided(v_pool, 4, *KV_TYPES),
-                                 _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), _ptr(page_table, torch.int32), C.byref(q),
+                                 _ptr(d_bonus, torch.int32), _address(k_pool), _address(v_pool), _address(k_scale), _address(v_scale),
+                                 _ptr(page_table, torch.int32), C.byref(q),
                                  _ptr(d_prefix_len, torch.int32), _ptr(d_tail, torch.int32), _ptr(d_tail_len, torch.int32), _stream())
     _check("war_commit_quant", code)
