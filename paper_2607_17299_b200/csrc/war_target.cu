@@ -152,13 +152,8 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 
 __device__ __forceinline__ uint32_t unordered(uint32_t u) { return (u & 0x80000000u) ? u & 0x7fffffffu : ~u; }
 
-// 32 bits of a bit string from bit v on; words past `words` read as 0
-__device__ __forceinline__ uint32_t bits_at(const uint32_t* w, int v, int words) {
-    const int k = v >> 5, sh = v & 31;
-    uint32_t x = w[k] >> sh;
-    if (sh && k + 1 < words) x |= w[k + 1] << (32 - sh);
-    return x;
-}
+// 32 bits of a bit string from bit v on (the word after them is read too)
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* w, int v) { return __funnelshift_r(w[v >> 5], w[(v >> 5) + 1], v & 31); }
 
 template <class T, bool kOut>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -321,9 +316,10 @@ war_target_kernel(const TargetArgs a) {
             if (o) bar = fmaxf(bar, __uint_as_float(unordered(o - (o == 0x80000000u ? 2 : 1))));
         }
         const float bar_in = bar;
+        const bool inner = first >= v0 && first + kSegment <= v1;         // (uniform) nothing ends in this piece
         auto fetch = [&](int u) -> uint4 {
             const int v = first + (u * 32 + lane) * kPer;
-            if (v >= v0 && v + kPer <= v1) return __ldcs(reinterpret_cast<const uint4*>(row + v));
+            if (inner || (v >= v0 && v + kPer <= v1)) return __ldcs(reinterpret_cast<const uint4*>(row + v));
             // (a slice may begin or end inside 16 bytes)
             return v + kPer > v0 && v < v1 ? Wide<T>::part(row + v, v0 - v, v1 - v) : Wide<T>::nothing();
         };
@@ -346,7 +342,8 @@ war_target_kernel(const TargetArgs a) {
             return __funnelshift_r(k == 32 ? m_last : w, k == 31 ? m_last : next, v & 31);      // (v + i never reaches word 33)
         };
         auto rare_at = [&](int v) -> uint32_t {                           // (bits past the slice's do not matter)
-            return v >= v0 && v < v1 ? bits_at(rare, v - v0, bit_words + 1) : v < v0 && v + kPer > v0 ? rare[0] << (v0 - v) : 0;
+            if (inner) return bits_at(rare, v - v0);
+            return v >= v0 && v < v1 ? bits_at(rare, v - v0) : v < v0 && v + kPer > v0 ? rare[0] << (v0 - v) : 0;
         };
         if (dismiss) {
             uint4 in[kLoads];
@@ -398,14 +395,17 @@ war_target_kernel(const TargetArgs a) {
                 if (u + 3 < kLoads) in2 = fetch(u + 3);
                 const int v = first + (u * 32 + lane) * kPer;
                 const uint32_t allowed = allowed_at(v), few = rare_at(v) & ((1u << kPer) - 1), ok = allowed & ~few;
-                if (v + kPer <= v0 || v >= v1) continue;
+                if (!inner && (v + kPer <= v0 || v >= v1)) continue;
                 float x[kPer];
                 Wide<T>::widen(in, x);
                 if (a.count) {
                     float made[kPer];
-                    if (table_wide && v >= v0 && v + kPer <= v1) {
+                    if (table_wide && (inner || (v >= v0 && v + kPer <= v1))) {
 #pragma unroll
                         for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(made + i) = *reinterpret_cast<const float4*>(made_of + (v - v0) + i);
+                    } else if (inner) {
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) made[i] = made_of[v - v0 + i];
                     } else {
 #pragma unroll
                         for (int i = 0; i < kPer; ++i) made[i] = made_of[min(max(v + i - v0, 0), W - 1)];
@@ -429,7 +429,7 @@ war_target_kernel(const TargetArgs a) {
                     x[i] = (ok >> i) & 1u ? x[i] : -INFINITY;
                     top = fmaxf(top, x[i]);
                 }
-                if (v < v0 || v + kPer > v1) {
+                if (!inner && (v < v0 || v + kPer > v1)) {
                     top = -INFINITY;
 #pragma unroll
                     for (int i = 0; i < kPer; ++i) if (v + i >= v0 && v + i < v1) top = fmaxf(top, x[i]);
@@ -444,10 +444,10 @@ war_target_kernel(const TargetArgs a) {
 #pragma unroll
                         for (int i = 0; i < kPer; ++i) x[i] = (few >> i) & 1u ? Wide<T>::pick(in, i) : x[i];
                     }
-                    if (out_wide && v >= v0 && v + kPer <= v1) __stcs(reinterpret_cast<uint4*>(out + v), Wide<T>::narrow(x));
+                    if (out_wide && (inner || (v >= v0 && v + kPer <= v1))) __stcs(reinterpret_cast<uint4*>(out + v), Wide<T>::narrow(x));
                     else {
 #pragma unroll
-                        for (int i = 0; i < kPer; ++i) if (v + i >= v0 && v + i < v1) Wide<T>::store(out + v + i, x[i]);
+                        for (int i = 0; i < kPer; ++i) if (inner || (v + i >= v0 && v + i < v1)) Wide<T>::store(out + v + i, x[i]);
                     }
                 }
             }
