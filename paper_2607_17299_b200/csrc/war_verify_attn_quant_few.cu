@@ -1,16 +1,26 @@
-// Tensor-core verify attention over the 8-bit cache for sm_100a.  The skeleton is that of war_verify_attn_sm100.cu (work
-// units, warp roles, a ring of TMA-filled slots, two softmax groups with an accumulator each, one launch for up to 64
-// requests); what differs is the arithmetic, because the cache's bytes go to the tensor cores as they are:
+// Tensor-core verify attention over the 8-bit cache for sm_100a, for calls with at most 32 query rows per kv head
+// (war_verify_attn_quant_many.cu has the others).  Work units, the ring of TMA-filled slots and the merge of split requests are
+// those of war_verify_attn_sm100.cu; what differs is the arithmetic, because the cache's bytes go to the tensor cores as
+// they are, and which operand is the wide one, because a product of 128 rows is wasted on 4 to 32 of them:
 //
-//   S = Qh K' + Ql K'      q (scaled by a power of two per row) = Qh + Ql, both e4m3: eight kind::f8f6f4 products of 32 dims
-//   p = exp2(S * (row's constant * K's scale of the key's block) - m)
-//   O += Ph V' + Pl V'     p * (V's scale of the key's block) = Ph + Pl, e4m3 and e5m2: eight products of 32 keys
+//   S = K Qh' + K Ql'      128 keys x the rows; q (scaled by a power of two per row) = Qh + Ql, both e4m3
+//   p = exp2(S * (row's constant * K's scale of the key's block) - the row's reference)
+//   O' += V' Ph + V' Pl    128 dims x the rows; p * (V's scale of the key's block) = Ph + Pl, e4m3 and e5m2
 //
-// Converting the cache to 16 bits on chip instead would move every element through shared memory three more times (read,
-// written twice as wide, read twice as wide by the tensor cores), 192 of the 128 bytes an SM moves a cycle; splitting the
-// small operands keeps the tensor work of the bf16 kernel per key (sixteen products of 64 cycles a tile) and its precision.
-// A tile of 128 keys is 16 KB of K and 16 KB of V, rows of 128 bytes in the 128-byte swizzle, for either memory order: one
-// tensor map (d, token, head, page) with the pool's own strides, one copy per (page, head).
+// So a softmax thread has one key and all rows, and a tile of 128 keys costs sixteen products of 16 or 32 columns, each bound
+// by the 4 KB of K or V that it reads from shared memory.  Rows' maxima lie across the lanes: a tile is worked out relative
+// to the reference of the tiles before, the group's four warps vote whether some value exceeds it by more than
+// 2^kRescaleThreshold, and only then the maxima are taken and the tile is worked out again (once or twice a unit).
+// Converting the cache to 16 bits on chip instead would move every element through shared memory three more times.
+// Four groups take tiles in turn, each with its own S, P, O, maxima and sums: one group's chain S -> exponentials -> P is
+// about 6000 cycles long against the 1350 in which HBM brings a tile.  They are merged at the end of a unit.
+// A tile is 16 KB of K and 16 KB of V, rows of 128 bytes in the 128-byte swizzle, for either memory order: one tensor map
+// (d, token, head, page) with the pool's own strides, one copy per (page, head).
+//
+// Bound by HBM for 16 rows and fewer (64 requests of about 14000 keys, 8 kv heads, 1.82 GB: 329 us, 5.5 TB/s); for 32 rows the
+// exponentials and conversions of the softmax warps add up to more (465 us, 3.9 TB/s).  Single tokens (8 requests of 4096
+// keys, 67 MB): 30 us, of which planning takes 5 and the merge of split requests 6.  A row per lane, as for more rows, takes
+// 600 us and more for 32 rows; three slots fewer in the ring 10 % more.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -34,14 +44,14 @@ constexpr uint32_t kTmemCols = 512;
 constexpr int kMaxRows = 32;
 // The largest scaled weight is 2^kRescaleThreshold (a stale maximum) * 2 (V's scale against its reference) * kWeightTop = 448,
 // the largest e4m3 value.
-constexpr float kRescaleThreshold = 4.0f;          // log2 units
-constexpr float kWeightTop = 14.f;
-constexpr float kMargin = 2.f;                      // a new reference lies this far above the maximum
+constexpr float kRescaleThreshold = 3.0f;          // log2 units
+constexpr float kWeightTop = 28.f;
+constexpr float kMargin = 1.f;                      // a new reference lies this far above the maximum
 constexpr float kNoMax = 1e30f;                     // stands for minus the maximum of a row that has seen no key yet
 
 // shared memory map (offsets from a 1024-byte aligned base)
 constexpr int kOffQ = 0;                            // [high, low parts][32 rows][128 dims]
-constexpr int kOffP = 8192;                         // [group][128 keys][high, low parts of up to 32 rows]
+constexpr int kOffP = 8192;                         // [group][128 keys][high, low parts of 16 or 32 rows]
 constexpr int kGroupP = 8192;
 constexpr int kOffRing = kOffP + kGroups * kGroupP;
 constexpr int kOffBar = kOffRing + kSlots * kSlotBytes;
@@ -84,7 +94,7 @@ struct SoftmaxShared {
         float sum[kGroups][4][kMaxRows]; // [group][warp]: the row sums at the end of a unit,
         int most[kGroups][4][kMaxRows];  // a tile's row maxima before
     };
-    float f[kGroups][kMaxRows];          // factors of the groups' O in the epilogue
+    alignas(16) float f[kGroups][kMaxRows];          // factors of the groups' O in the epilogue
     float v_unit[kGroups];               // what a group's O is relative to
     alignas(16) int viol[2][kGroups][4]; // [tile parity][group][warp]
 };
@@ -94,31 +104,6 @@ static_assert(kOffSoft + (int)sizeof(SoftmaxShared) <= kOffFused, "shared memory
 // loads: K0, K1, K2, K3, V0, K4, V1, K5, ..., the last four V.
 __device__ __forceinline__ uint32_t seq_k(uint32_t ld0, int t) { return ld0 + t + max(0, t - (kGroups - 1)); }
 __device__ __forceinline__ uint32_t seq_v(uint32_t ld0, int t, int T) { return ld0 + t + min(T, t + kGroups); }
-
-// Four scaled weights (two pairs, each divided by 256) as high and low e4m3 codes, four of each.  A half of x / 256 holds in
-// its bits 7 to 14 the e4m3 code of x (the two exponent biases differ by 8): cut off there it is the high part; the
-// remainder is exact and non-negative, below an eighth of x, and goes into the low part eight times as large, rounded by
-// adding half a step before the cut.  Together they hold x to 2^-8 of itself, or to 2^-13 for the smallest.
-__device__ __forceinline__ void split_weights(float2 x01, float2 x23, uint32_t& high, uint32_t& low) {
-    asm("{\n.reg .b32 y0, y1, h0, h1, d0, d1;\n"
-        "cvt.rn.f16x2.f32 y0, %3, %2;\n"
-        "cvt.rn.f16x2.f32 y1, %5, %4;\n"
-        "and.b32 h0, y0, 0x7f807f80;\n"
-        "and.b32 h1, y1, 0x7f807f80;\n"
-        "sub.rn.f16x2 d0, y0, h0;\n"
-        "sub.rn.f16x2 d1, y1, h1;\n"
-        "mul.rn.f16x2 d0, d0, %6;\n"
-        "mul.rn.f16x2 d1, d1, %6;\n"
-        "add.u32 h0, y0, y0;\n"
-        "add.u32 h1, y1, y1;\n"
-        "add.u32 d0, d0, 0x00400040;\n"
-        "add.u32 d1, d1, 0x00400040;\n"
-        "add.u32 d0, d0, d0;\n"
-        "add.u32 d1, d1, d1;\n"
-        "prmt.b32 %0, h0, h1, 0x7531;\n"
-        "prmt.b32 %1, d0, d1, 0x7531;\n}\n"
-        : "=r"(high), "=r"(low) : "f"(x01.x), "f"(x01.y), "f"(x23.x), "f"(x23.y), "r"(0x48004800u));
-}
 
 // descriptor upper word for the 64-byte swizzle
 __device__ __forceinline__ constexpr uint32_t umma_desc_hi64(uint32_t sbo_bytes) { return (sbo_bytes >> 4) | (1u << 14) | (4u << 29); }
@@ -310,7 +295,8 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
         // P: rows of 64 bytes in the 64-byte swizzle, MN-major
         constexpr uint32_t hi = umma_desc_hi(1024), hi_p = umma_desc_hi64(512);
         const uint32_t ring_lo = umma_desc_lo(sRing, 16), q_lo = umma_desc_lo(sQ, 16), p_lo = umma_desc_lo(smem_u32(smem + kOffP), 16);
-        const uint32_t idesc_s = umma_idesc8(kRp, a.kv_e5m2, 0, 0, 0), idesc_o = umma_idesc8(2 * kRp, a.kv_e5m2, 0, 1, 1);
+        const uint32_t idesc_s = umma_idesc8(kRp, a.kv_e5m2, 0, 0, 0), idesc_hi = umma_idesc8(kRp, a.kv_e5m2, 0, 1, 1),
+                       idesc_lo = umma_idesc8(kRp, a.kv_e5m2, 1, 1, 1);
         auto mma_s = [&](int g, uint32_t slot) {                               // S = K Q high + K Q low, 32 dims at a time
             const uint32_t k_lo = ring_lo + slot * (kSlotBytes >> 4), d_s = tmem + (uint32_t)g * 64u;
 #pragma unroll
@@ -356,8 +342,11 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                     const uint32_t v_lo = ring_lo + slot * (kSlotBytes >> 4), d_o = tmem + 256u + (uint32_t)g * 64u;
                     const uint32_t p_g = p_lo + (uint32_t)g * (kGroupP >> 4);
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)                       // O += V^T [P high, P low], 32 keys at a time
-                        umma_f8(d_o, pack64(v_lo + ks * (4096u >> 4), hi), pack64(p_g + ks * (2048u >> 4), hi_p), idesc_o, ks > 0 || t >= kGroups);
+                    for (int ks = 0; ks < 4; ++ks) {                     // O += V^T P high + V^T P low, 32 keys at a time
+                        const uint64_t v_desc = pack64(v_lo + ks * (4096u >> 4), hi);
+                        umma_f8(d_o, v_desc, pack64(p_g + ks * (2048u >> 4), hi_p), idesc_hi, ks > 0 || t >= kGroups);
+                        umma_f8(d_o, v_desc, pack64(p_g + ks * (2048u >> 4) + (kRp >> 4), hi_p), idesc_lo, 1u);
+                    }
                     if (has_s) mma_s(g, slot_k);
                     umma_commit(&bars->pv_done[g]);
                     umma_commit(&bars->empty[slot]);
@@ -591,10 +580,10 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                 if ((viol || v_corr != 1.f) && t != grp) {
                     // (S of this tile was committed behind the group's last P V product: O is stable)
 #pragma unroll 1
-                    for (int c = 0; c < 2 * kRp; c += 8) {
+                    for (int c = 0; c < kRp; c += 8) {
                         uint32_t o[8];
                         tmem_ld8(tO + c, o);
-                        const float* const f = &sh->corr[grp][c & (kRp - 1)];
+                        const float* const f = &sh->corr[grp][c];
                         tmem_wait_ld();
 #pragma unroll
                         for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (viol ? f[e] * v_corr : v_corr));
@@ -688,20 +677,28 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
             if (!ok) break;
             // O^T: this thread has dimension `key` of every row; eight rows at a time, dealt to the groups
             static_assert(kRp <= 8 * kGroups, "eight rows a group");
-            const int live = tree_ok ? min(min(kRp, R), grp * 8 + 8) : 0;
-#pragma unroll 1                                                           // (once per unit: kept small)
-            for (int r = grp * 8; r < live; ++r) {
-                float o = 0.f;
+            const int live = tree_ok ? min(kRp, R) - grp * 8 : 0;
+            if (live > 0) {                                                // (once per unit: kept small)
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = 0.f;
 #pragma unroll 1
                 for (int g = 0; g < kGroups && g < T; ++g) {
-                    uint32_t h, lo;
-                    tmem_ld1(t_lane + 256u + g * 64u + r, h);
-                    tmem_ld1(t_lane + 256u + g * 64u + kRp + r, lo);
+                    uint32_t x[8];
+                    tmem_ld8(t_lane + 256u + g * 64u + grp * 8u, x);
+                    const float4 f0 = *reinterpret_cast<const float4*>(&sh->f[g][grp * 8]), f1 = *reinterpret_cast<const float4*>(&sh->f[g][grp * 8 + 4]);
+                    const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
                     tmem_wait_ld();
-                    o = fmaf(fmaf(__uint_as_float(lo), 0.125f, __uint_as_float(h)), sh->f[g][r], o);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = fmaf(__uint_as_float(x[e]), f[e], o[e]);
                 }
-                if (split) a.w.part_o[((size_t)un.slot * a.w.rows + r) * 128 + key] = o;
-                else a.out[(size_t)sh->q_row[r] * 128 + key] = __float2bfloat16_rn(o);
+                float* const part = a.w.part_o + ((size_t)un.slot * a.w.rows + grp * 8) * 128 + key;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (e >= live) break;
+                    if (split) part[e * 128] = o[e];
+                    else a.out[(size_t)sh->q_row[grp * 8 + e] * 128 + key] = __float2bfloat16_rn(o[e]);
+                }
             }
             tc_fence_before();
             warp_arrive(&bars->epi_done, lane);

@@ -76,32 +76,6 @@ __device__ __forceinline__ void tmem_zero16(uint32_t taddr) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%1], {%0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0};" ::"r"(0), "r"(taddr) : "memory");
 }
 
-// Four scaled weights (two pairs, each divided by 256) as high (e4m3) and low (e5m2) codes, four of each.  The pipe that
-// holds the 8-bit conversions is the busiest but one here, so both codes are cut out of halves: a half of x / 256 holds in
-// its bits 7 to 14 the e4m3 code of x (the two exponent biases differ by 8), rounded by adding half a step before the cut;
-// the remainder is exact, and its e5m2 code is a half's upper byte, rounded the same way.  Together they hold x to 2^-8 of
-// itself, or to 2^-17 for the smallest.
-__device__ __forceinline__ void split_weights(float2 x01, float2 x23, uint32_t& high, uint32_t& low) {
-    asm("{\n.reg .b32 y0, y1, h0, h1, d0, d1, s0, s1;\n"
-        "cvt.rn.f16x2.f32 y0, %3, %2;\n"
-        "cvt.rn.f16x2.f32 y1, %5, %4;\n"
-        "add.u32 h0, y0, 0x00400040;\n"
-        "add.u32 h1, y1, 0x00400040;\n"
-        "and.b32 h0, h0, 0x7f807f80;\n"
-        "and.b32 h1, h1, 0x7f807f80;\n"
-        "sub.rn.f16x2 d0, y0, h0;\n"
-        "sub.rn.f16x2 d1, y1, h1;\n"
-        "mul.rn.f16x2 d0, d0, %6;\n"
-        "mul.rn.f16x2 d1, d1, %6;\n"
-        "add.u32 s0, h0, h0;\n"
-        "add.u32 s1, h1, h1;\n"
-        "add.u32 d0, d0, 0x00800080;\n"
-        "add.u32 d1, d1, 0x00800080;\n"
-        "prmt.b32 %0, s0, s1, 0x7531;\n"
-        "prmt.b32 %1, d0, d1, 0x7531;\n}\n"
-        : "=r"(high), "=r"(low) : "f"(x01.x), "f"(x01.y), "f"(x23.x), "f"(x23.y), "r"(0x5c005c00u));
-}
-
 // kFused: see attn_sm100_kernel.
 template <bool kFused>
 __global__ void __launch_bounds__(kThreads, 1)

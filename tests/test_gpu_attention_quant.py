@@ -1,12 +1,13 @@
 """GPU parity: war_verify_attn_quant against the fp64 checker on the values the 8-bit cache stands for.
 
 Tolerances.  A weight p * (V's scale) reaches the tensor cores as two 8-bit parts that hold it to 2^-8 of itself (high part
-e4m3: at most 2^-4 off, the remainder's e5m2 code at most 2^-3 of that, and half a step of 2^-16 at the type's lower end,
-2^-17 / 56 of the largest weight and V scale); the output's bf16 adds 2^-8 of itself.  So per element
-    |error| <= 2^-8 |out| + 1.05 * (2^-7 / 2 * sum w |v| + keys * 2^-17 / 14 * max |v|)
-(weights are relative to a maximum that may be stale by a factor of 4, hence 56 / 4), and because the roundings are
-independent the root mean square over many elements stays below 2^-8 of the output's.  The log-sum-exp sees only 32-bit
-arithmetic and queries held to 2^-18 of a row's largest."""
+e4m3: at most 2^-4 off, the remainder's e5m2 code at most 2^-3 of that, and half a step of 2^-16 at the type's lower end);
+the largest weight of a row is scaled to at least 14 (28 times p, and p is relative to a reference at most a factor of 2
+above the row's maximum).  The output's bf16 adds 2^-8 of itself.  So per element
+    |error| <= 2^-8 |out| + 1.05 * (2^-8 * sum w |v| + keys * 2^-17 / 14 * max |v|)
+(w: weights that sum to 1; the last term relative to the sum of weights where the largest counts 1, which is at least 1), and
+because the roundings are independent the root mean square over many elements stays below 2^-8 of the output's.  The
+log-sum-exp sees only 32-bit arithmetic and queries held to 2^-18 of a row's largest."""
 import numpy as np
 import pytest
 import torch
@@ -166,6 +167,34 @@ def test_one_key_takes_all_and_zero_queries(war):
     c.q[:, 1] *= 40                                              # logits of +-100: one weight near 1
     c.d_q = c.q.to(DEV)
     c.check(*c.run(war))
+
+
+@pytest.mark.parametrize("kernel", [0, 1])
+@pytest.mark.parametrize("N", [4, 8, 24])                       # 16, 32 and 96 query rows
+def test_many_small_weights(war, N, kernel):
+    """One key with a weight of 1 and 60000 with 2^-14.3 each, which together outweigh it four times: what a long context
+    behind its first token looks like.  None of the small ones may be lost, and as they are all the same their roundings
+    do not cancel: half a step of 2^-16, relative to at least 14, each."""
+    c = Case(90, "e4m3", [60000], N, 4, 1, 64, 64, dirty=False, spread=0.0)
+    rng = np.random.default_rng(91)
+    code = lambda x: torch.as_tensor(x, dtype=torch.float32).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    c.q = torch.ones_like(c.q)
+    c.ck[:] = 0
+    c.ck[c.pt[0, 0], 0, 5] = code(0.875)
+    c.cv[:] = code(1 + 0.25 * rng.standard_normal(c.cv.shape))
+    c.sk[:], c.sv[:] = 1.0, 1.0
+    c.d_q, c.k, c.v = c.q.to(DEV), Q.to_device(c.ck, c.kv, False), Q.to_device(c.cv, c.kv, False)
+    c.dsk, c.dsv = torch.from_numpy(c.sk).to(DEV), torch.from_numpy(c.sv).to(DEV)
+    out, lse = c.run(war, kernel)
+    c.check(out, lse)
+    n, L = int(c.nn[0]), int(c.prefix[0] + c.nn[0])
+    pg, r = c.pt[0, np.arange(L) // 64], np.arange(L) % 64
+    K, V = O.decode(c.ck[pg, :, r], c.kv), O.decode(c.cv[pg, :, r], c.kv)
+    want, want_lse = A.verify_attention_request(c.q[0].double().numpy(), K, V, 60000, c.parent[0], n, c.scale)
+    weight = np.exp(want_lse - 128 * 0.875 * c.scale)[:, :, None]          # of all keys, that of the largest being 1
+    bound = 2.0 ** -7 * np.abs(want) + 1.05 * L * 2.0 ** -17 / 14 * np.abs(V).max() / weight
+    err = np.abs(out[0, :n].double().cpu().numpy() - want)
+    assert (err <= bound).all(), float((err / bound).max())
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
