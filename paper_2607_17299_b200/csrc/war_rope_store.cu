@@ -306,6 +306,7 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
                 if (j > j0) fetch_rows(which, h, j, j1);
 #pragma unroll
                 for (int u = 0; u < kKept; ++u) {
+                    if (j + 4 * u >= j1) break;                           // (uniform)
                     const Row r = turned(in[u], j + 4 * u);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(r.a[i]), fabsf(r.b[i])));

@@ -154,6 +154,17 @@ def test_store_matches_checker(war, case):
     assert war.war_device_status() == 0
 
 
+@pytest.mark.parametrize("kv,rot,interleaved", [("e4m3", 126, False), ("bf16", 126, True), ("e5m2", 100, True), ("e4m3", 48, False),
+                                                ("e4m3", 112, True), ("bf16", 16, False), ("e5m2", 16, True), ("bf16", 34, False)])
+def test_store_rotations(war, kv, rot, interleaved):
+    """Every layout of a lane's pairs, the largest table (64 slots) where the rotation ends inside a lane; blocks of more rows
+    than stay in registers."""
+    s = Store(27, kv, [33, 900], 64, 9, 2, 32, 32, rot, interleaved, full=True)
+    s.run(war)
+    s.check()
+    assert war.war_device_status() == 0
+
+
 @pytest.mark.parametrize("kw", [dict(pow2=False), dict(zero=True), dict(magnitude=1e-30), dict(magnitude=1e30), dict(magnitude=300.0)])
 def test_store_scales(war, kw):
     """Old scales that are no powers of two, rows of zeros, rows far smaller and far larger than what the block holds."""
