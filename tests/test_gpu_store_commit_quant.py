@@ -379,3 +379,43 @@ def test_whole_steps_in_a_row(war, kv):
             text[b] += [int(ids[b, j]) for j in w_path[b, :w_alen[b]]] + [int(w_bonus[b])]
             assert int(dpl[b]) == len(text[b]) - 1
         assert war.war_device_status() == 0
+
+
+@pytest.mark.parametrize("N", [3, 24])                           # 12 and 96 query rows per kv head
+def test_pages_far_into_a_pool(war, N):
+    """Store, attention and commit in a pool of more than 2^32 bytes give what they give in a small one."""
+    rng = np.random.default_rng(61)
+    B, Hq, Hkv, page, P = 2, 8, 2, 16, 8
+    prefix = np.array([37, 200], np.int32)
+    pt, total = Q.pages(rng, prefix + N, page)
+    far = (1 << 20) + 40 - total                                 # 4096 bytes a page
+    nn, parent = Q.trees(rng, B, N, full=True)
+    ck, sk = Q.cache(rng, "e4m3", total, Hkv, page, 16, pow2=True)
+    cv, sv = Q.cache(rng, "e4m3", total, Hkv, page, 16, pow2=True)
+    g = torch.Generator().manual_seed(61)
+    q, k, v = (torch.randn((B, N, h, 128), generator=g).to(torch.bfloat16).to(DEV) for h in (Hq, Hkv, Hkv))
+    freq = war.war_rope_frequencies(128, 10000.0)[0].to(DEV)
+    alen = dev(np.array([1, 2], np.int32))
+    path = np.full((B, N), -1, np.int32)
+    path[0, 0], path[1, :2] = 1, [1, 2]
+    ids, bonus = dev(rng.integers(0, 99, (B, N)).astype(np.int32)), dev(np.array([5, 6], np.int32))
+    results = []
+    for shift in (0, far):
+        pools = []
+        for codes, scale in ((ck, sk), (cv, sv)):
+            big, s = torch.empty((shift + total, Hkv, page, 128), dtype=torch.uint8, device=DEV), torch.ones((shift + total, Hkv, 1), device=DEV)
+            big[shift:], s[shift:] = dev(codes), dev(scale)
+            pools += [big.view(torch.float8_e4m3fn), s]
+        kp, ks, vp, vs = pools
+        table = dev(np.where(pt < total, pt + shift, pt).astype(np.int32))
+        dpl, tail, tl = dev(prefix), torch.zeros((B, P), dtype=torch.int32, device=DEV), dev(np.array([3, 8], np.int32))
+        out, lse, q_rot = torch.zeros_like(q), torch.zeros((B, N, Hq), device=DEV), torch.zeros_like(q)
+        war.war_rope_store(q, k, v, freq, table, dpl, dev(nn), dev(parent), kp, vp, ks, vs, q_rot)
+        params = war.attn_quant_params(q_rot, kp, vp, ks, vs, table, 128 ** -0.5)
+        war.war_verify_attn_quant(q_rot, kp, vp, ks, vs, table, dpl, dev(nn), dev(parent), params, war.new_quant_workspace(params, DEV), out, lse)
+        war.war_commit_quant(ids, alen, dev(path), bonus, kp, vp, ks, vs, table, dpl, tail, tl)
+        torch.cuda.synchronize()
+        assert war.war_device_status() == 0
+        results.append([out, lse, q_rot, dpl, tail, tl] + [x[shift:].view(torch.uint8) if x.dim() == 4 else x[shift:] for x in pools])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)

@@ -129,6 +129,50 @@ def test_matches_checker(war, case):
     Case(*case[:5], **case[5]).check(war)
 
 
+MORE = [
+    (41, 160, 3, 20000, "bf16", dict(coarse=True)),              # many requests: few slices, long pieces, ties across warps
+    (42, 8, 12, 40000, "f32", dict(coarse=True, ctx=9000)),
+    (43, 2, 9, 30001, "bf16", dict(pad=3, coarse=True, mask=0.002)),      # a grammar that leaves a token in 500
+    (44, 2, 9, 30001, "f32", dict(pad=1, mask=0.0005, bias=40)),
+]
+
+
+@pytest.mark.parametrize("case", MORE, ids=[str(c[0]) for c in MORE])
+def test_matches_checker_at_size(war, case):
+    Case(*case[:5], **case[5]).check(war)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["equal", "rising", "falling"])
+def test_rows_that_are_hard_to_dismiss(war, kind, dtype):
+    """All logits equal (zeros of both signs: the lowest token allowed wins), and rows where every value is a new largest one."""
+    c = Case(45, 3, 7, 25013, dtype, pad=5, mask=0.5 if kind == "equal" else 0.9)
+    V = c.V
+    if kind == "equal":
+        row = torch.where(torch.arange(V) % 3 == 0, torch.tensor(-0.0), torch.tensor(0.0))
+    else:
+        row = torch.linspace(-8, 8, V) if kind == "rising" else torch.linspace(8, -8, V)
+    c.logits = row.to(c.dtype).expand(3, 7, V).clone()
+    c.d_logits.copy_(c.logits)
+    c.check(war)
+
+
+def test_logits_far_apart(war):
+    """Requests 2^32 elements apart, in and out."""
+    c = Case(46, 2, 3, 4001, "bf16")
+    step = (1 << 32) + 4096
+    buf = torch.empty(step + 3 * 4001, dtype=torch.bfloat16, device=DEV)
+    far = buf.as_strided((2, 3, 4001), (step, 4001, 1))
+    far.copy_(c.d_logits)
+    c.d_logits = far
+    rows, want = c.want()
+    np.testing.assert_array_equal(c.run(war), want)
+    np.testing.assert_array_equal(c.run(war, out=far), want)
+    h = far.cpu()
+    for (b, j), row in rows.items():
+        assert torch.equal(h[b, j].nan_to_num(nan=1e9), torch.from_numpy(row).to(c.dtype).nan_to_num(nan=1e9))
+
+
 def test_out_in_place(war):
     Case(31, 2, 6, 3001, "bf16", pad=3).check(war, in_place=True)
 
