@@ -227,16 +227,21 @@ war_target_kernel(const TargetArgs a) {
                 if (tok >= v0 && tok < v1) atomicAdd(&counter[tok - v0], 1u);
             }
         }
-        if (a.bias_off && warp == kWarps - 1) {
-            // bias entries in order, so that the last one of a token counts: 32 at a time, the highest lane of equal tokens writes
-            for (long long e = e0; e < e1; e += 32) {
-                const int tok = e + lane < e1 ? a.bias_ids[e + lane] : -1 - lane;
-                const unsigned same = __match_any_sync(0xffffffffu, tok);
-                if (tok >= v0 && tok < v1 && 31 - __clz(same) == lane) {
-                    bias_at[tok - v0] = (uint16_t)(e + lane - e0 + 1);
-                    atomicOr(&rare[(tok - v0) >> 5], 1u << ((tok - v0) & 31));
+        if (a.bias_off) {
+            // the last entry of a token counts: the largest number in its half of a word
+            for (long long e = e0 + tid; e < e1; e += kThreads) {
+                const int tok = a.bias_ids[e];
+                if (tok < v0 || tok >= v1) continue;
+                const int l = tok - v0, sh16 = (l & 1) * 16;
+                const uint32_t k = (uint32_t)(e - e0 + 1);
+                uint32_t* at = reinterpret_cast<uint32_t*>(bias_at) + (l >> 1);
+                uint32_t now = *reinterpret_cast<volatile uint32_t*>(at);
+                while (((now >> sh16) & 0xffffu) < k) {
+                    const uint32_t before = now;
+                    now = atomicCAS(at, before, (before & ~(0xffffu << sh16)) | (k << sh16));
+                    if (now == before) break;
                 }
-                __syncwarp();
+                atomicOr(&rare[l >> 5], 1u << (l & 31));
             }
         }
         if (a.path && tid < kMaxSlots && tid > 0 && tid < n) {

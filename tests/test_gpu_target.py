@@ -134,6 +134,7 @@ MORE = [
     (42, 8, 12, 40000, "f32", dict(coarse=True, ctx=9000)),
     (43, 2, 9, 30001, "bf16", dict(pad=3, coarse=True, mask=0.002)),      # a grammar that leaves a token in 500
     (44, 2, 9, 30001, "f32", dict(pad=1, mask=0.0005, bias=40)),
+    (47, 2, 3, 5000, "bf16", dict(bias=20000)),                  # most tokens have a bias, many have several
 ]
 
 
