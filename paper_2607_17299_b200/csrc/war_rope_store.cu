@@ -15,6 +15,11 @@
 //   blocks  (8-bit pools) one head's K or V rows of one scale block: largest magnitude first, then the scale, the
 //           re-encoding of older rows if the scale has grown, and the new rows (turned again from the kept input)
 // and the request's tasks are dealt over several thread blocks when there are few requests.
+//
+// Measured: 128 requests of 64 slots, 64 + 8 heads, bf16 pool (336 MB): 63 us, 5.3 TB/s (sixteen lanes a row with the partner
+// fetched by shuffle took 93).  256 requests of 8 slots, 32 + 8 heads, e4m3 pool (46 MB): 19 us (37 before); there the work is
+// in the scale blocks, which pass their values twice, and in the table's 64-bit functions, a seventh of all instructions.  One
+// slot of 8 requests: 4.7 us, the chain of dependent reads.
 #include <cuda_bf16.h>
 #include <math.h>
 #include "war_common.cuh"

@@ -3,8 +3,8 @@
 //
 // The logits are the traffic (64 times 131072 values a request against a few thousand context tokens), so a row is read
 // once, 16 bytes a lane, and what the penalties need is looked up on chip: a cluster of up to eight thread blocks takes
-// one request, each block a slice of the vocabulary.  Together they read the request's context once and count its tokens
-// into the slice that owns them (shared-memory atomics across the cluster).  Rows are independent of each other (tokens on a
+// one request, each block a slice of the vocabulary, and counts the context's tokens that
+// fall into it (each block reads the whole context; sending counts to the owner across the cluster took 2.5 times as long).  Rows are independent of each other (tokens on a
 // slot's path are looked up in the tree, not written into the counters), so warps take pieces of rows without a barrier; the
 // winners of a row meet in one 64-bit maximum per block, and the cluster's first block compares the slices.  Ties go to the
 // lowest token, whatever the order of the atomics.
@@ -13,6 +13,13 @@
 //     looked up and processed (a few hundred a row)
 //   processed logits wanted, or penalties that may raise: every value goes through the arithmetic, without branches
 //   tokens with a bias, and tokens of the tree, are few: each warp goes through them after its piece of a row
+//
+// Measured: the choice for 256 requests of 8 slots and 32000 bf16 logits with contexts of up to 32768 tokens takes 90 us, of
+// which the rows alone (no penalties, biases, masks) 45 (131 MB, 2.9 TB/s: two thread blocks' tables fill an SM, the start of
+// a row has no bar yet, and 512 blocks go through in two waves), counting the contexts about 25 and looking candidates up the
+// rest; looking every value up, as a first version did, took 449.  All values of 32 requests of 32 slots and 131071
+// float32 logits: 400 us for 1.09 GB (2.7 TB/s), 240 without penalties; there the arithmetic, about 280 instructions for 128
+// values, is the bound.  One slot of 8 requests: 9.7 us, a launch and four dependent reads.
 #include <cuda_bf16.h>
 #include <cooperative_groups.h>
 #include "war_common.cuh"
@@ -565,7 +572,7 @@ extern "C" war_status_t war_target(const void* d_logits, const int32_t* d_num_no
     a.count = count; a.path = count && d_ids != nullptr;
     a.aligned = (((uintptr_t)d_logits | (uintptr_t)(p->logits_strides[0] * size) | (uintptr_t)(p->logits_strides[1] * size)) & 15) == 0;
     // Slices of whole mask words, at most eight, at least two segments each, so many that the requests fill the GPU (two thread
-    // blocks an SM); rows are dealt to more clusters of a request only if that leaves room: each counts the context again.
+    // blocks an SM, 1.5 waves of them: 256 requests of 32000 tokens take 90 us with two slices, 106 with three); rows are dealt to more clusters of a request only if that leaves room: each counts the context again.
     const int resident = 2 * 148;
     const int most = (p->V + kSegment * 2 - 1) / (kSegment * 2), least = (p->V + kMaxSlice - 1) / kMaxSlice;
     int slices = (resident * 3 / 2 + p->B - 1) / p->B;

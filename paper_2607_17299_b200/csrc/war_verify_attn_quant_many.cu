@@ -13,6 +13,11 @@
 // A tile of 128 keys is 16 KB of K and 16 KB of V, rows of 128 bytes in the 128-byte swizzle, for either memory order: one
 // tensor map (d, token, head, page) with the pool's own strides, one copy per (page, head).  The scales of a tile travel
 // with it, sixteen 4-byte asynchronous copies for K and for V, so that no softmax warp waits for global memory.
+//
+// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 605 us, 2.6 TB/s and 656 TFLOP/s.  Bound by the
+// chain of a tile, S -> maximum -> exponentials and 8-bit parts -> P, about 4900 cycles in either of the two groups (11 instructions
+// an element) against the 1200 of its sixteen products; TMEM has no room for a third group's S next to two O.  Sixteen softmax
+// warps, two threads a row, took 754 us: what they gain in overlap they lose in registers and in agreeing on a maximum.
 #include <type_traits>
 #include "war_attn_quant_sm100_parts.cuh"
 
