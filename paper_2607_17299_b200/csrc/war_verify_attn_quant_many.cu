@@ -41,7 +41,7 @@ constexpr int kOffQ = 0;                            // high parts, then low part
 constexpr int kOffRing = 32768;
 constexpr int kOffBar = kOffRing + kSlots * kSlotBytes;
 constexpr int kOffStats = kOffBar + 512;
-constexpr int kOffScales = kOffStats + 3072;        // [tile of the CTA & 15][K, V][8-key group]
+constexpr int kOffScales = kOffStats + 3 * 256 * 4;        // [tile of the CTA & 15][K, V][8-key group]
 constexpr int kOffFused = kOffScales + 2048;
 constexpr int kSmemBytes = kOffFused + 768 + 1024;
 // Scales are kept for 16 tiles.  While a tile y is unfinished its V slot stays taken, and so do the slots of every later V

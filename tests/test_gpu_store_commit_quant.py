@@ -419,3 +419,79 @@ def test_pages_far_into_a_pool(war, N):
         results.append([out, lse, q_rot, dpl, tail, tl] + [x[shift:].view(torch.uint8) if x.dim() == 4 else x[shift:] for x in pools])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+def test_steps_in_graphs_on_two_streams(war):
+    """Store, attention, choice and commit of two batches, each captured into a graph with its own buffers and replayed at the
+    same time on streams of their own, give what the calls give one after the other."""
+    rng = np.random.default_rng(62)
+    B, N, Hq, Hkv, page, V, P = 3, 6, 8, 2, 16, 3000, 8
+
+    class Batch:
+        def __init__(self, seed):
+            prefix = np.array([30, 15, 700], np.int32)
+            self.pt, total = Q.pages(rng, prefix + 8 * N, page)
+            self.nn, self.parent = Q.trees(rng, B, N, full=True)
+            self.start = [Q.to_device(c, "e4m3", False) if c.dtype == np.uint8 else dev(c)
+                          for c in (*Q.cache(rng, "e4m3", total, Hkv, page, 16, pow2=True), *Q.cache(rng, "e4m3", total, Hkv, page, 16, pow2=True))]
+            g = torch.Generator().manual_seed(seed)
+            self.q, self.k, self.v = (torch.randn((B, N, h, 128), generator=g).to(torch.bfloat16).to(DEV) for h in (Hq, Hkv, Hkv))
+            self.logits = torch.randn((B, N, V), generator=g).to(DEV)
+            self.prefix, self.tail, self.tail_len = prefix, rng.integers(0, V, (B, P)).astype(np.int32), np.full(B, P, np.int32)
+            self.ids, self.bonus = dev(rng.integers(0, V, (B, N)).astype(np.int32)), dev(np.array([1, 2, 3], np.int32))
+            path = np.full((B, N), -1, np.int32)
+            path[:, 0] = 1
+            self.path, self.alen = dev(path), dev(np.array([1, 1, 0], np.int32))
+            self.table, self.d_nn, self.d_par = dev(self.pt), dev(self.nn), dev(self.parent)
+            self.freq = war.war_rope_frequencies(128, 10000.0)[0].to(DEV)
+            self.rep = torch.full((B,), 1.2, device=DEV)
+            self.ctx, self.off = dev(rng.integers(0, V, 90).astype(np.int32)), dev(np.array([0, 30, 60, 90], np.int64))
+            self.out, self.lse, self.q_rot = torch.zeros_like(self.q), torch.zeros((B, N, Hq), device=DEV), torch.zeros_like(self.q)
+            self.target = torch.zeros((B, N), dtype=torch.int32, device=DEV)
+            self.reset()
+            self.params = war.attn_quant_params(self.q_rot, *self.pools[::2], *self.pools[1::2], self.table, 128 ** -0.5)
+            self.ws = war.new_quant_workspace(self.params, DEV)
+
+        def reset(self):
+            if not hasattr(self, "pools"):
+                self.pools = [t.clone() for t in self.start]
+                self.pools[0], self.pools[2] = self.pools[0].view(torch.float8_e4m3fn), self.pools[2].view(torch.float8_e4m3fn)
+                self.state = [dev(self.prefix), dev(self.tail), dev(self.tail_len)]
+            for t, s in zip(self.pools, self.start):
+                t.view(torch.uint8).copy_(s.view(torch.uint8))
+            for t, s in zip(self.state, (self.prefix, self.tail, self.tail_len)):
+                t.copy_(dev(s))
+
+        def step(self):
+            kp, ks, vp, vs = self.pools
+            war.war_rope_store(self.q, self.k, self.v, self.freq, self.table, self.state[0], self.d_nn, self.d_par, kp, vp, ks, vs, self.q_rot)
+            war.war_verify_attn_quant(self.q_rot, kp, vp, ks, vs, self.table, self.state[0], self.d_nn, self.d_par, self.params, self.ws, self.out, self.lse)
+            war.war_target(self.logits, self.d_nn, self.ids, self.d_par, self.target, d_ctx=self.ctx, d_ctx_off=self.off, d_repetition=self.rep)
+            war.war_commit_quant(self.ids, self.alen, self.path, self.bonus, kp, vp, ks, vs, self.table, *self.state)
+
+        def results(self):
+            return [t.clone() for t in (self.out, self.lse, self.q_rot, self.target, *self.state)] + [t.view(torch.uint8).clone() for t in self.pools]
+
+    batches = [Batch(1), Batch(2)]
+    want = []
+    for b in batches:
+        for _ in range(3):                                       # three steps: the prefix advances
+            b.step()
+        want.append(b.results())
+        b.reset()
+    torch.cuda.synchronize()
+    streams, graphs = [torch.cuda.Stream() for _ in batches], []
+    for b in batches:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.step()
+        graphs.append(g)
+    for _ in range(3):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert war.war_device_status() == 0
+    for b, w in zip(batches, want):
+        for x, y in zip(b.results(), w):
+            assert torch.equal(x, y)
