@@ -58,7 +58,7 @@ static_assert(kThreads * 168 >= 256 * kRegsSoftmax + 128 * kRegsOther, "the hand
 
 struct Bars {
     uint64_t full[kSlots], empty[kSlots];
-    uint64_t s_ready[2], p_ready[2], pv_done[2], turn[2];
+    uint64_t s_ready[2][2], p_ready[2][2], pv_done[2][2];     // [group][half of a tile]
     uint64_t scales[kScaleTiles];        // a tile's scales are there (16 lanes of either producer)
     uint64_t exch;                       // the epilogue's exchange buffer has been written / read
     uint64_t q_ready, stats_ready, epi_done;
@@ -77,8 +77,8 @@ __device__ __forceinline__ void umma_f8_ts(uint32_t d_tmem, uint32_t a_tmem, uin
         "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n}\n"
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void tmem_zero16(uint32_t taddr) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%1], {%0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0, %0};" ::"r"(0), "r"(taddr) : "memory");
+__device__ __forceinline__ void tmem_zero8(uint32_t taddr) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%1], {%0, %0, %0, %0, %0, %0, %0, %0};" ::"r"(0), "r"(taddr) : "memory");
 }
 
 // kFused: see attn_sm100_kernel.
@@ -131,8 +131,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
 
     if (tid == 0) {
         for (int i = 0; i < kSlots; ++i) { mbar_init(&bars->full[i], 1); mbar_init(&bars->empty[i], 1); }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars->s_ready[i], 1); mbar_init(&bars->p_ready[i], 4); mbar_init(&bars->pv_done[i], 1); mbar_init(&bars->turn[i], 1);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&bars->s_ready[0][i], 1); mbar_init(&bars->p_ready[0][i], 4); mbar_init(&bars->pv_done[0][i], 1);
         }
         for (int i = 0; i < kScaleTiles; ++i) mbar_init(&bars->scales[i], 32);
         mbar_init(&bars->q_ready, 8);
@@ -245,20 +245,20 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         // other's products run.  They take turns burst by burst: mixed bursts would both end late.  Group 1's issuer also
         // counts the split units of this CTA whose partial result is out (fused-plan variant).
         const int g = warp - kWarpMma;
-        uint32_t ld0 = 0, cg = 0, units_done = 0, outs = 0, turns = 0;
+        uint32_t ld0 = 0, cg = 0, units_done = 0, outs = 0;
         // operand types of one product: the 8-bit parts of q and of the weights against the cache's codes
-        const uint32_t idesc_s = umma_idesc8(128, 0, a.kv_e5m2, 0, 0), idesc_hi = umma_idesc8(128, 0, a.kv_e5m2, 0, 1),
+        const uint32_t idesc_s = umma_idesc8(64, 0, a.kv_e5m2, 0, 0), idesc_hi = umma_idesc8(128, 0, a.kv_e5m2, 0, 1),
                        idesc_lo = umma_idesc8(128, 1, a.kv_e5m2, 0, 1);
         // every tile is rows of 128 bytes, 8-row groups 1 KB apart: Q and K as K-major operands, V as an MN-major one
         constexpr uint32_t hi = umma_desc_hi(1024);
         const uint32_t q_lo = umma_desc_lo(sQ, 16), ring_lo = umma_desc_lo(sRing, 16);
         const uint32_t d_s = tmem + (uint32_t)g * 128u, d_o = d_s + 256u;           // S and later P, O of this group
-        auto mma_s = [&](uint32_t slot) {
-            const uint32_t k_lo = ring_lo + slot * (kSlotBytes >> 4);
+        auto mma_s = [&](uint32_t slot, int half) {
+            const uint32_t k_lo = ring_lo + slot * (kSlotBytes >> 4) + (uint32_t)half * (8192u >> 4);
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)                               // 32 dims at a time: high parts of q, then low parts
-                umma_f8(d_s, pack64(q_lo + (uint32_t)(ks >> 2) * (16384u >> 4) + (ks & 3) * 2u, hi), pack64(k_lo + (ks & 3) * 2u, hi), idesc_s, ks > 0);
-            umma_commit(&bars->s_ready[g]);
+                umma_f8(d_s + (uint32_t)half * 64u, pack64(q_lo + (uint32_t)(ks >> 2) * (16384u >> 4) + (ks & 3) * 2u, hi), pack64(k_lo + (ks & 3) * 2u, hi), idesc_s, ks > 0);
+            umma_commit(&bars->s_ready[g][half]);
         };
         bool ok = true;
         fused_plan::Cursor cur{0, 0, 0};
@@ -279,35 +279,39 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
                 if (ok) {
                     tc_fence_after();
-                    if (lane == 0) { mma_s(slot); umma_commit(&bars->empty[slot]); }
+                    if (lane == 0) { mma_s(slot, 0); mma_s(slot, 1); umma_commit(&bars->empty[slot]); }
                     __syncwarp();
                 }
             }
             for (int t = g; t < T && ok; t += 2, ++cg) {
                 const uint32_t sq = seq_v(ld0, t, T), slot = sq % kSlots;
-                const bool has_s = t + 2 < T;                        // S(t+2) goes out in the same burst as PV(t)
+                const bool has_s = t + 2 < T;                        // S(t+2) of a half goes out behind its P V(t)
                 const uint32_t sq_k = has_s ? seq_k(ld0, t + 2) : 0u, slot_k = sq_k % kSlots;
                 ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
                 if (ok && has_s) ok = wait_for(&bars->full[slot_k], (sq_k / kSlots) & 1u, bars, a.status_word);
-                if (ok) ok = wait_for(&bars->p_ready[g], cg & 1u, bars, a.status_word);
-                if (ok && t > 0) ok = wait_for(&bars->turn[g], turns++ & 1u, bars, a.status_word);
-                if (!ok) break;
-                tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t v_lo = ring_lo + slot * (kSlotBytes >> 4);
+#pragma unroll 1
+                for (int half = 0; half < 2 && ok; ++half) {
+                    ok = wait_for(&bars->p_ready[g][half], cg & 1u, bars, a.status_word);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (lane == 0) {
+                        const uint32_t v_lo = ring_lo + slot * (kSlotBytes >> 4) + (uint32_t)half * (8192u >> 4), d_p = d_s + (uint32_t)half * 64u;
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) {                     // 32 keys at a time: high and low parts of the weights
-                        const uint64_t v_desc = pack64(v_lo + (uint32_t)ks * (4096u >> 4), hi);
-                        umma_f8_ts(d_o, d_s + (uint32_t)ks * 8u, v_desc, idesc_hi, ks > 0 || t > 1);
-                        umma_f8_ts(d_o, d_s + 32u + (uint32_t)ks * 8u, v_desc, idesc_lo, 1u);
+                        for (int ks = 0; ks < 2; ++ks) {                 // 32 keys at a time: high and low parts of the weights
+                            const uint64_t v_desc = pack64(v_lo + (uint32_t)ks * (4096u >> 4), hi);
+                            umma_f8_ts(d_o, d_p + (uint32_t)ks * 8u, v_desc, idesc_hi, ks > 0 || half > 0 || t > 1);
+                            umma_f8_ts(d_o, d_p + 16u + (uint32_t)ks * 8u, v_desc, idesc_lo, 1u);
+                        }
+                        umma_commit(&bars->pv_done[g][half]);
+                        if (half) umma_commit(&bars->empty[slot]);
+                        if (has_s) {
+                            mma_s(slot_k, half);
+                            if (half) umma_commit(&bars->empty[slot_k]);
+                        }
                     }
-                    if (has_s) mma_s(slot_k);
-                    umma_commit(&bars->pv_done[g]);
-                    umma_commit(&bars->empty[slot]);
-                    if (has_s) umma_commit(&bars->empty[slot_k]);
-                    if (t + 1 < T) mbar_arrive(&bars->turn[g ^ 1]);
+                    __syncwarp();
                 }
-                __syncwarp();
+                if (!ok) break;
             }
             ld0 += 2u * T;
             ++units_done;
@@ -429,24 +433,27 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             float m_used = -CUDART_INF_F, l = 0.f;
             float v_ref = 0.f;                                             // power of two that V's scales are taken relative to
 
-            // One tile's share of this thread: kCols keys.
-            auto tile = [&](int t, auto cols_c) -> bool {
+            float v_unit = 0.f, v_corr = 1.f;
+            // Half a tile's share of this thread: kCols keys.
+            auto step = [&](int t, int half, auto cols_c) -> bool {
                 constexpr int kCols = decltype(cols_c)::value;
-                const int c0 = kCols == 64 ? copy * 64 : 0;                // first key of the tile that is this thread's
+                const int c0 = half * 64 + (kCols == 32 ? copy * 32 : 0);  // first key of the tile that is this thread's
                 const int key0 = (un.tile_begin + t) * kTileKeys;
                 const uint32_t ti = ld0 / 2 + t;
                 const float* const sc = s_scale + (ti & (kScaleTiles - 1)) * 32;
-                if (!wait_for(&bars->scales[ti & (kScaleTiles - 1)], (ti / kScaleTiles) & 1u, bars, a.status_word)) return false;
-                // V's scales relative to a power of two that follows the largest one seen: a factor below 2
-                const float sv_top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sc[16 + (lane & 15)])));
-                float v_corr = 1.f;
-                if (sv_top >= 2.f * v_ref) {
-                    const float ref = __uint_as_float(max(__float_as_uint(sv_top) & 0x7f800000u, 0x0c800000u));   // at least 2^-102
-                    v_corr = v_ref / ref;
-                    v_ref = ref;
+                v_corr = 1.f;
+                if (half == 0) {
+                    if (!wait_for(&bars->scales[ti & (kScaleTiles - 1)], (ti / kScaleTiles) & 1u, bars, a.status_word)) return false;
+                    // V's scales relative to a power of two that follows the largest one seen: a factor below 2
+                    const float sv_top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sc[16 + (lane & 15)])));
+                    if (sv_top >= 2.f * v_ref) {
+                        const float ref = __uint_as_float(max(__float_as_uint(sv_top) & 0x7f800000u, 0x0c800000u));   // at least 2^-102
+                        v_corr = v_ref / ref;
+                        v_ref = ref;
+                    }
+                    v_unit = kWeightTop / 256.f / v_ref;                   // (split_weights wants x / 256)
                 }
-                const float v_unit = kWeightTop / 256.f / v_ref;           // (split_weights wants x / 256)
-                if (!wait_for(&bars->s_ready[grp], cgm & 1u, bars, a.status_word)) return false;
+                if (!wait_for(&bars->s_ready[grp][half], cgm & 1u, bars, a.status_word)) return false;
                 tc_fence_after();
                 // the thread's part of the row of S comes into registers once
                 uint32_t r[kCols];
@@ -458,11 +465,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                     // d + a is tree slot a (visible when a is the row's slot or an ancestor; the ancestor mask has no bit
                     // at or above num_nodes, so keys past the request's end are out).
                     const int d = pl - key0 - c0;                          // < kCols here
-                    unsigned long long lo, hi;
-                    if (d >= 64) { lo = ~0ull; hi = ((1ull << (d - 64)) - 1ull) | (anc << (d - 64)); }
-                    else if (d > 0) { lo = ((1ull << d) - 1ull) | (anc << d); hi = anc >> (64 - d); }
-                    else { lo = d > -64 ? anc >> (-d) : 0ull; hi = 0ull; }
-                    const uint32_t w[4] = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+                    const unsigned long long see = d > 0 ? ((1ull << d) - 1ull) | (anc << d) : d > -64 ? anc >> (-d) : 0ull;
+                    const uint32_t w[2] = {(uint32_t)see, (uint32_t)(see >> 32)};
 #pragma unroll
                     for (int e = 0; e < kCols; ++e)
                         if (!((w[e >> 5] >> (e & 31)) & 1u)) r[e] = 0xff800000u;     // -inf
@@ -483,7 +487,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                     m_used = mx;
                     rescale = true;
                 }
-                rescale = rescale && t > grp;                              // O of this group holds earlier tiles of the unit
+                rescale = rescale && (t > grp || half > 0);                // O of this group holds earlier keys of the unit
                 corr *= v_corr;
                 const float neg_m = m_used == -CUDART_INF_F ? 0.f : -m_used;
                 // p = exp2(s * scales - m) goes into the sum as it is; p * (V's scale) goes to the tensor cores as a high
@@ -509,7 +513,9 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 }
                 l += ((l4[0].x + l4[0].y) + (l4[1].x + l4[1].y)) + ((l4[2].x + l4[2].y) + (l4[3].x + l4[3].y));
                 if (__any_sync(0xffffffffu, rescale)) {
-                    // (S of this tile was committed behind the group's last P V product: O is stable)
+                    // O is stable once the products of the half before are through
+                    if (!wait_for(&bars->pv_done[grp][half ^ 1], (half ? cgm : cgm - 1) & 1u, bars, a.status_word)) return false;
+                    tc_fence_after();
                     const float f = rescale ? corr : 1.f;
 #pragma unroll 1                                                           // (rare: kept small)
                     for (int c = 0; c < 8; ++c) {
@@ -521,36 +527,39 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                         tmem_st16(tO + c * 16, o);
                     }
                 }
-                const uint32_t at = tS + (uint32_t)(c0 >> 2);
-                if constexpr (kCols == 128) { tmem_st32(at, ph); tmem_st32(at + 32, pw); }
+                const uint32_t at = tS + (uint32_t)half * 64u;
+                if constexpr (kCols == 64) { tmem_st16(at, ph); tmem_st16(at + 16, pw); }
                 else {
-                    tmem_st16(at, ph); tmem_st16(at + 32, pw);
-                    const uint32_t z = tS + (uint32_t)((copy ^ 1) << 4);   // the other copy's keys weigh nothing in these lanes
-                    tmem_zero16(z); tmem_zero16(z + 32);
+                    tmem_st8(at + copy * 8, ph); tmem_st8(at + 16 + copy * 8, pw);
+                    const uint32_t z = at + (uint32_t)((copy ^ 1) << 3);   // the other copy's keys weigh nothing in these lanes
+                    tmem_zero8(z); tmem_zero8(z + 16);
                 }
                 tmem_wait_st();
                 return true;
             };
             for (int t = grp; t < T && ok; t += 2, ++cgm) {
-                if (warp_valid) ok = twice ? tile(t, std::integral_constant<int, 64>()) : tile(t, std::integral_constant<int, 128>());
-                else { ok = wait_for(&bars->s_ready[grp], cgm & 1u, bars, a.status_word); tc_fence_after(); }
-                if (!ok) break;
-                // the unit's last tile may hold rows past the request's last key: zero their V (P is exactly 0 there,
-                // but 0 x NaN garbage would still poison the product)
-                const int key0 = (un.tile_begin + t) * kTileKeys;
-                if (key0 + kTileKeys > L) {
-                    const uint32_t sq = seq_v(ld0, t, T), slot = sq % kSlots;
-                    ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
+#pragma unroll 1
+                for (int half = 0; half < 2 && ok; ++half) {
+                    if (warp_valid) ok = twice ? step(t, half, std::integral_constant<int, 32>()) : step(t, half, std::integral_constant<int, 64>());
+                    else { ok = wait_for(&bars->s_ready[grp][half], cgm & 1u, bars, a.status_word); tc_fence_after(); }
                     if (!ok) break;
-                    if (row >= L - key0) {
-                        const uint32_t base = sRing + slot * kSlotBytes + (uint32_t)row * 128u;
+                    // the unit's last tile may hold rows past the request's last key: zero their V (P is exactly 0 there,
+                    // but 0 x NaN garbage would still poison the product)
+                    const int key0 = (un.tile_begin + t) * kTileKeys;
+                    if (half == 0 && key0 + kTileKeys > L) {
+                        const uint32_t sq = seq_v(ld0, t, T), slot = sq % kSlots;
+                        ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
+                        if (!ok) break;
+                        if (row >= L - key0) {
+                            const uint32_t base = sRing + slot * kSlotBytes + (uint32_t)row * 128u;
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) st_shared16(base + c * 16u, 0, 0, 0, 0);
+                            for (int c = 0; c < 8; ++c) st_shared16(base + c * 16u, 0, 0, 0, 0);
+                        }
+                        fence_async_proxy();
                     }
-                    fence_async_proxy();
+                    tc_fence_before();
+                    warp_arrive(&bars->p_ready[grp][half], lane);
                 }
-                tc_fence_before();
-                warp_arrive(&bars->p_ready[grp], lane);
             }
             if (!ok) break;
             if (row_scale != row_scale) l = row_scale;                     // NaN or infinity among the row's queries
@@ -560,9 +569,9 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             warp_arrive(&bars->stats_ready, lane);
             if (grp == 0) {
                 // epilogue: both groups' last products, then the merge of (max, sum, O) over groups and copies, and the store
-                ok = wait_for(&bars->pv_done[0], (cgm - 1) & 1u, bars, a.status_word) &&
+                ok = wait_for(&bars->pv_done[0][1], (cgm - 1) & 1u, bars, a.status_word) &&
                      wait_for(&bars->stats_ready, units_done & 1u, bars, a.status_word);
-                if (ok && theirs > 0) ok = wait_for(&bars->pv_done[1], (cg_other + theirs - 1) & 1u, bars, a.status_word);
+                if (ok && theirs > 0) ok = wait_for(&bars->pv_done[1][1], (cg_other + theirs - 1) & 1u, bars, a.status_word);
                 if (!ok) break;
                 tc_fence_after();
                 if (warp_valid) {
