@@ -239,7 +239,8 @@ __device__ __forceinline__ bool next_unit(const FusedPlan* pl, Cursor& c, int B,
 // and launch, straight from a cold instruction cache, so its cost is its length: it reads only the two numbers per
 // request the plan depends on (the parent arrays are checked by the warps that use them, unit by unit), keeps to
 // 32-bit arithmetic and rolled loops, and has two block barriers on the contiguous path and five on the other.
-template <int kMaxChunks = kFusedMaxChunks>
+// kUnitCost: times the cost that contiguous_unit_cost gives a unit (a kernel whose tiles are cheaper pays more of them).
+template <int kMaxChunks = kFusedMaxChunks, int kUnitCost = 1>
 __device__ __noinline__ static void make(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ num_nodes,
                                         int B, int N, int Hkv, int G, int page_size, int max_pages,
                                         FusedPlanScratch* sc, FusedPlan* pl, int* status_word) {
@@ -303,7 +304,7 @@ __device__ __noinline__ static void make(const int32_t* __restrict__ prefix_len,
         }
         __syncthreads();
         const int t_all = pl->t_all, n_used = pl->n_used;
-        const int unit_cost = contiguous_unit_cost(rows_max);
+        const int unit_cost = kUnitCost * contiguous_unit_cost(rows_max);
         for (int x = tid; x <= n_used; x += kFusedThreads)
             sc->cut[x] = contiguous_cut(x, n_used, t_all, pairs, unit_cost, pl->tiles, sc->weight, pl->u.start, sc->live_before, B, Hkv);
         __syncthreads();

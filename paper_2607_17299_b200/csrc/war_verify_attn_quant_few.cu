@@ -42,6 +42,9 @@ constexpr int kSoftWarps = 4 * kGroups;
 constexpr int kWarpLoadK = kSoftWarps, kWarpMma = kSoftWarps + 1, kWarpLoadV = kSoftWarps + 3;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kMaxRows = 32;
+// What a unit costs in the split, times the bf16 kernel's tiles: with 32 rows a boundary takes as long as some fifteen tiles of
+// 32 KB (64 requests of 8 slots 468 -> 447 us, 20 requests 158 -> 152; with 16 rows it made 326 us 332).
+template <int kRp> constexpr int kUnitCostOf = kRp == 32 ? 3 : 1;
 // The largest scaled weight is 2^kRescaleThreshold (a stale maximum) * 2 (V's scale against its reference) * kWeightTop = 448,
 // the largest e4m3 value.
 constexpr float kRescaleThreshold = 3.0f;          // log2 units
@@ -196,7 +199,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
     }
     if (kFused) {
         // this CTA's units, worked out here (the ring is idle until the first unit starts)
-        fused_plan::make<kMaxChunks>(a.prefix_len, a.num_nodes, a.B, a.N, a.Hkv, a.G, a.page_size, a.max_pages,
+        fused_plan::make<kMaxChunks, kUnitCostOf<kRp>>(a.prefix_len, a.num_nodes, a.B, a.N, a.Hkv, a.G, a.page_size, a.max_pages,
                          (FusedPlanScratch*)(smem + kOffRing), (FusedPlan*)(smem + kOffFused), a.status_word);
     }
     if (kFused) fence_async_proxy();                       // the plan's scratch is about to be overwritten by tensor copies
