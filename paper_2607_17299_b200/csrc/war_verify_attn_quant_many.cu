@@ -14,10 +14,14 @@
 // tensor map (d, token, head, page) with the pool's own strides, one copy per (page, head).  The scales of a tile travel
 // with it, sixteen 4-byte asynchronous copies for K and for V, so that no softmax warp waits for global memory.
 //
-// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 605 us, 2.6 TB/s and 656 TFLOP/s.  Bound by the
-// chain of a tile, S -> maximum -> exponentials and 8-bit parts -> P, about 4900 cycles in either of the two groups (11 instructions
-// an element) against the 1200 of its sixteen products; TMEM has no room for a third group's S next to two O.  Sixteen softmax
-// warps, two threads a row, took 754 us: what they gain in overlap they lose in registers and in agreeing on a maximum.
+// A tile is worked on in halves of 64 keys: while a group's softmax warps have one half, P V and the next tile's S of the other
+// are on the tensor cores, so the next S is ready when they come to it (whole tiles: 605 us below).
+//
+// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 583 us, 2.7 TB/s and 681 TFLOP/s of the two
+// products (each operand in two parts: twice that on the pipe).  Bound by the softmax warps: 11 instructions an element, two
+// warps a scheduler, half of the issue slots used.  TMEM has no room for a third group's S next to two O.  Sixteen softmax
+// warps, two threads a row, were slower in lockstep (754 us) and with the reference handed from half to half (639 us): what
+// they gain in overlap they lose in instructions for agreeing on it and in registers.
 #include <type_traits>
 #include "war_attn_quant_sm100_parts.cuh"
 
@@ -44,9 +48,9 @@ constexpr int kOffStats = kOffBar + 512;
 constexpr int kOffScales = kOffStats + 3 * 256 * 4;        // [tile of the CTA & 15][K, V][8-key group]
 constexpr int kOffFused = kOffScales + 2048;
 constexpr int kSmemBytes = kOffFused + 768 + 1024;
-// Scales are kept for 16 tiles.  While a tile y is unfinished its V slot stays taken, and so do the slots of every later V
-// and of every K beyond y + 2 (bursts take turns: a later product waits for y's): with kSlots slots no producer is past
-// y + 2 + kSlots.
+// Scales are kept for 16 tiles.  While a tile y is unfinished, the slots of V of y, y + 2, y + 4 ... and of K of y + 2, y + 4 ...
+// stay taken once they are loaded (one issuer serves these tiles in order): half of the loads from there on, so with kSlots
+// slots no producer gets past y + 2 + kSlots.
 constexpr int kScaleTiles = 16;
 static_assert(2 + kSlots < kScaleTiles, "scales of an unfinished tile stay");
 constexpr int kMaxChunks = kSlots * kSlotBytes / 1024;    // the merge needs two rows of every chunk in the ring
@@ -159,7 +163,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
-    // columns: [0,128) S/P of group 0, [128,256) S/P of group 1, [256,384) O of group 0, [384,512) O of group 1
+    // columns: [0,128) S/P of group 0, a half tile in each half, [128,256) S/P of group 1, [256,384) O of group 0, [384,512) O of group 1
 
     // register hand-over between warpgroups: the third warpgroup gives registers up, the softmax warpgroups take them
     // (each instruction is executed by all four warps of its warpgroup, and the role code stays inside that branch)
@@ -331,8 +335,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     } else {
         // ------------------------------------------------------------------ softmax groups, one thread per row
         // With at most 64 rows in the block the rows stand twice among the 128 lanes, and a copy takes only half of the keys,
-        // with its own maximum and its own O: the weights of the other keys are zero in its lanes.  So a thread has 128 or 64
-        // keys of a row, and all four schedulers work.
+        // with its own maximum and its own O: the weights of the other keys are zero in its lanes.  So a thread has 64 or 32
+        // keys of a row at a time, and all four schedulers work.
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int grp = warp >> 2, quad = warp & 3;
         const int row = quad * 32 + lane;                            // TMEM lane
