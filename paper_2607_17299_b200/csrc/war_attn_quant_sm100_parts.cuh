@@ -1,7 +1,6 @@
 // Parts of the two tensor-core kernels over the 8-bit cache (library-internal): copies, MMA and TMEM wrappers, bounded waits,
 // kernel arguments, tensor maps.
 #pragma once
-#include <mutex>
 #include "war_quant.cuh"
 #include "war_attn_quant.cuh"
 #include "war_attn_sm100_parts.cuh"
@@ -159,42 +158,6 @@ bool make_pool_map(CUtensorMap* map, const void* pool, long long num_pages, int 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The tensor maps of a call depend only on the pools' addresses and shapes, so the last few are kept (by value: a map holds
-// an address and strides, nothing of the contents).
-struct PoolMapKey {
-    const void *k, *v; long long num_pages, s[6]; int Hkv, page_size, dev;
-    bool operator==(const PoolMapKey& o) const {
-        for (int i = 0; i < 6; ++i) if (s[i] != o.s[i]) return false;
-        return k == o.k && v == o.v && num_pages == o.num_pages && Hkv == o.Hkv && page_size == o.page_size && dev == o.dev;
-    }
-};
-struct PoolMaps { PoolMapKey key; CUtensorMap k_map, v_map; bool used; };
-constexpr int kMapCacheEntries = 8;
-std::mutex g_map_lock;
-PoolMaps g_map_cache[kMapCacheEntries];
-
-bool pool_maps(const PoolMapKey& key, CUtensorMap* k_map, CUtensorMap* v_map) {
-    std::lock_guard<std::mutex> g(g_map_lock);
-    for (int e = 0; e < kMapCacheEntries; ++e) {
-        if (g_map_cache[e].used && g_map_cache[e].key == key) {
-            const PoolMaps hit = g_map_cache[e];
-            for (int m = e; m > 0; --m) g_map_cache[m] = g_map_cache[m - 1];
-            g_map_cache[0] = hit;
-            *k_map = hit.k_map; *v_map = hit.v_map;
-            return true;
-        }
-    }
-    PoolMaps fresh;
-    fresh.key = key; fresh.used = true;
-    if (!make_pool_map(&fresh.k_map, key.k, key.num_pages, key.Hkv, key.page_size, key.s) ||
-        !make_pool_map(&fresh.v_map, key.v, key.num_pages, key.Hkv, key.page_size, key.s + 3))
-        return false;
-    for (int m = kMapCacheEntries - 1; m > 0; --m) g_map_cache[m] = g_map_cache[m - 1];
-    g_map_cache[0] = fresh;
-    *k_map = fresh.k_map; *v_map = fresh.v_map;
-    return true;
-}
-
 int log2_of(int x) {
     int s = 0;
     while ((1 << s) < x) ++s;
@@ -204,11 +167,11 @@ int log2_of(int x) {
 // What both kernels are launched with; false: the pools have no tensor map.
 inline bool quant_kernel_args(const void* q, const AttnQuantPools& pools, const int32_t* page_table, const int32_t* prefix_len,
                               const int32_t* num_nodes, const int32_t* parent, const war_attn_params_t* p, const AttnWorkspace& w,
-                              bool fused, int dev, void* out, float* lse, int* status_word, QuantKernelArgs* a, CUtensorMap* k_map,
+                              bool fused, void* out, float* lse, int* status_word, QuantKernelArgs* a, CUtensorMap* k_map,
                               CUtensorMap* v_map) {
-    PoolMapKey key{pools.k, pools.v, p->num_pages, {}, p->Hkv, p->page_size, dev};
-    for (int i = 0; i < 3; ++i) { key.s[i] = pools.ks[i]; key.s[3 + i] = pools.vs[i]; }
-    if (!pool_maps(key, k_map, v_map)) return false;
+    if (!make_pool_map(k_map, pools.k, p->num_pages, p->Hkv, p->page_size, pools.ks) ||
+        !make_pool_map(v_map, pools.v, p->num_pages, p->Hkv, p->page_size, pools.vs))
+        return false;
     a->q = (const __nv_bfloat16*)q; a->page_table = page_table; a->prefix_len = prefix_len;
     a->out = (__nv_bfloat16*)out; a->lse = lse; a->status_word = status_word; a->w = w; a->pools = pools;
     a->num_pages = p->num_pages; a->scale_log2 = p->scale * kLog2e;

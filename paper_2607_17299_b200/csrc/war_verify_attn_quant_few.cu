@@ -818,7 +818,7 @@ war_status_t war_attn_quant_launch_few(const void* q, const AttnQuantPools& pool
     if (rows > kMaxRows) return WAR_ERR_UNSUPPORTED;
     CUtensorMap k_map, v_map;
     QuantKernelArgs a;
-    if (!quant_kernel_args(q, pools, page_table, prefix_len, num_nodes, parent, p, w, fused, dev, out, lse, status_word, &a, &k_map, &v_map))
+    if (!quant_kernel_args(q, pools, page_table, prefix_len, num_nodes, parent, p, w, fused, out, lse, status_word, &a, &k_map, &v_map))
         return WAR_ERR_UNSUPPORTED;
     const auto kernel = rows <= 16 ? (fused ? attn_quant_few_kernel<true, 16> : attn_quant_few_kernel<false, 16>)
                                    : (fused ? attn_quant_few_kernel<true, 32> : attn_quant_few_kernel<false, 32>);

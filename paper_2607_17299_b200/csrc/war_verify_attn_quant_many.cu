@@ -17,11 +17,12 @@
 // A tile is worked on in halves of 64 keys: while a group's softmax warps have one half, P V and the next tile's S of the other
 // are on the tensor cores, so the next S is ready when they come to it (whole tiles: 605 us below).
 //
-// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 583 us, 2.7 TB/s and 681 TFLOP/s of the two
+// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 590 us, 2.7 TB/s and 673 TFLOP/s of the two
 // products (each operand in two parts: twice that on the pipe).  Bound by the softmax warps: 11 instructions an element, two
 // warps a scheduler, half of the issue slots used.  TMEM has no room for a third group's S next to two O.  Sixteen softmax
 // warps, two threads a row, were slower in lockstep (754 us) and with the reference handed from half to half (639 us): what
 // they gain in overlap they lose in instructions for agreeing on it and in registers.
+#include <mutex>
 #include <type_traits>
 #include "war_attn_quant_sm100_parts.cuh"
 
@@ -778,7 +779,7 @@ war_status_t war_attn_quant_launch_many(const void* q, const AttnQuantPools& poo
     if (grid <= 0) return WAR_ERR_CUDA;
     CUtensorMap k_map, v_map;
     QuantKernelArgs a;
-    if (!quant_kernel_args(q, pools, page_table, prefix_len, num_nodes, parent, p, w, fused, dev, out, lse, status_word, &a, &k_map, &v_map))
+    if (!quant_kernel_args(q, pools, page_table, prefix_len, num_nodes, parent, p, w, fused, out, lse, status_word, &a, &k_map, &v_map))
         return WAR_ERR_UNSUPPORTED;
     if (fused) attn_quant_many_kernel<true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
     else attn_quant_many_kernel<false><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
