@@ -18,7 +18,7 @@
 // which the rows alone (no penalties, biases, masks) 45 (131 MB, 2.9 TB/s: two thread blocks' tables fill an SM, the start of
 // a row has no bar yet, and 512 blocks go through in two waves), counting the contexts about 25 and looking candidates up the
 // rest; looking every value up, as a first version did, took 449.  All values of 32 requests of 32 slots and 131071
-// float32 logits: 400 us for 1.09 GB (2.7 TB/s), 240 without penalties; there the arithmetic, about 280 instructions for 128
+// float32 logits: 400 us for 1.09 GB (2.7 TB/s), 202 without penalties, biases and masks; there the arithmetic, about 280 instructions for 128
 // values, is the bound.  One slot of 8 requests: 9.7 us, a launch and four dependent reads.
 #include <cuda_bf16.h>
 #include <cooperative_groups.h>
@@ -397,6 +397,9 @@ war_target_kernel(const TargetArgs a) {
                 }
             }
         } else {
+            // the next piece's lines come to L2 meanwhile (without penalties, biases and masks 240 -> 202 us at the size above)
+            const int next = first + kSegment + lane * (128 / (int)sizeof(T));
+            if (lane * 128 < kSegment * (int)sizeof(T) && next < v1) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + next));
             // (rolled, three loads ahead: unrolled, its code no longer stays in the instruction cache)
             uint4 in0 = fetch(0), in1 = fetch(1), in2 = fetch(2);
             load_mask();
