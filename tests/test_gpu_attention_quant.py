@@ -169,6 +169,20 @@ def test_one_key_takes_all_and_zero_queries(war):
     c.check(*c.run(war))
 
 
+@pytest.mark.parametrize("N,B", [(3, 6), (24, 6), (3, 70)])
+def test_requests_without_slots(war, N, B):
+    """num_nodes 0: the request's rows of out and lse stay as they are, whatever its prefix."""
+    rng = np.random.default_rng(92)
+    c = Case(92, "e4m3", rng.integers(0, 900, B).tolist(), N, 8, 2, 16, 16, full=True)
+    c.nn[1::3] = 0
+    c.dnn = torch.from_numpy(c.nn).to(DEV)
+    out, lse = c.run(war)
+    c.check(out, lse, [i for i in range(B) if c.nn[i] > 0])
+    for i in range(1, B, 3):
+        assert (out[i] == 7.0).all() and (lse[i] == 7.0).all()
+    assert war.war_device_status() == 0
+
+
 @pytest.mark.parametrize("kernel", [0, 1])
 @pytest.mark.parametrize("N", [4, 8, 24])                       # 16, 32 and 96 query rows
 def test_many_small_weights(war, N, kernel):

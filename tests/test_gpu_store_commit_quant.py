@@ -165,6 +165,15 @@ def test_store_rotations(war, kv, rot, interleaved):
     assert war.war_device_status() == 0
 
 
+def test_store_many_requests_and_none(war):
+    """More requests than thread blocks fit the GPU, some without a slot."""
+    s = Store(29, "e5m2", [k % 50 for k in range(400)], 2, 3, 1, 16, 16, 32)
+    s.nn[::7] = 0
+    s.run(war)
+    s.check(skip=range(0, 400, 7))
+    assert war.war_device_status() == 0
+
+
 @pytest.mark.parametrize("kw", [dict(pow2=False), dict(zero=True), dict(magnitude=1e-30), dict(magnitude=1e30), dict(magnitude=300.0)])
 def test_store_scales(war, kw):
     """Old scales that are no powers of two, rows of zeros, rows far smaller and far larger than what the block holds."""

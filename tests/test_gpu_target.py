@@ -158,6 +158,13 @@ def test_rows_that_are_hard_to_dismiss(war, kind, dtype):
     c.check(war)
 
 
+def test_requests_without_slots_and_many_requests(war):
+    c = Case(48, 700, 2, 300, "bf16")
+    c.nn[::3] = 0
+    c.check(war)
+    assert (c.run(war)[::3] == -1).all()
+
+
 def test_logits_far_apart(war):
     """Requests 2^32 elements apart, in and out."""
     c = Case(46, 2, 3, 4001, "bf16")
