@@ -95,7 +95,7 @@ struct SoftmaxShared {
     float m[kGroups][kMaxRows], neg_m[kGroups][kMaxRows], corr[kGroups][kMaxRows];
     union {
         float sum[kGroups][4][kMaxRows]; // [group][warp]: the row sums at the end of a unit,
-        int most[kGroups][4][kMaxRows];  // a tile's row maxima before
+        float most[kGroups][4][kMaxRows];  // a tile's row maxima before
     };
     alignas(16) float f[kGroups][kMaxRows];          // factors of the groups' O in the epilogue
     float v_unit[kGroups];               // what a group's O is relative to
@@ -540,32 +540,22 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                     const int4 w = *reinterpret_cast<const int4*>(word);
                     viol = (w.x | w.y | w.z | w.w) != 0;
                     if (!viol) break;
-                    // ---- the tile's row maxima (of S * scales, read again), and new references for all rows.  Rolled tightly: code
-                    // that runs this rarely comes from L2, at some 40 cycles an instruction.
-#pragma unroll 1
-                    for (int r = 0; r < kRp; r += 4) {
-                        uint32_t v[4];
-                        tmem_ld4(tS + r, v);
-                        tmem_wait_ld();
-                        const float4 rs = *reinterpret_cast<const float4*>(&sh->row_scale[r]);
-                        const float z[4] = {rs.x, rs.y, rs.z, rs.w};
+                    // ---- the tile's row maxima (of S * scales, read again), and new references for all rows
+                    if constexpr (kRp == 32) tmem_ld32(tS, reinterpret_cast<uint32_t*>(x));
+                    else tmem_ld16(tS, reinterpret_cast<uint32_t*>(x));
+                    tmem_wait_ld();
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            int o = (see >> (r + q)) & 1u ? __float_as_int(__uint_as_float(v[q]) * (z[q] * ks)) : (int)0xff800000;
-                            o ^= (o >> 31) & 0x7fffffff;                   // ordered as whole numbers
-                            o = __reduce_max_sync(0xffffffffu, o);
-                            if (lane == q) sh->most[grp][quad][r + q] = o;
-                        }
-                    }
+                    for (int r = 0; r < kRp; ++r) x[r] = (see >> r) & 1u ? x[r] * (sh->row_scale[r] * ks) : -CUDART_INF_F;
+                    const float most = reduce_rows(x, lane, [](float p, float q) { return fmaxf(p, q); });
+                    if (lane < kRp) sh->most[grp][quad][lane] = most;
                     warp_arrive(&bars->vote[grp], lane);
                     ok = wait_for(&bars->vote[grp], votes++ & 1u, bars, a.status_word);
                     if (!ok) break;
                     if (tid_g < kRp) {
                         const int r = tid_g;
-                        int o = max(max(sh->most[grp][0][r], sh->most[grp][1][r]), max(sh->most[grp][2][r], sh->most[grp][3][r]));
-                        o ^= (o >> 31) & 0x7fffffff;
+                        const float o = fmaxf(fmaxf(sh->most[grp][0][r], sh->most[grp][1][r]), fmaxf(sh->most[grp][2][r], sh->most[grp][3][r]));
                         // (a margin, so that the next one is further off; -inf stays -inf; a NaN row keeps its reference)
-                        const float old = sh->m[grp][r], now = fmaxf(__int_as_float(o) + kMargin, old);
+                        const float old = sh->m[grp][r], now = fmaxf(o + kMargin, old);
                         sh->m[grp][r] = now;
                         sh->neg_m[grp][r] = now == -CUDART_INF_F ? kNoMax : -now;
                         sh->corr[grp][r] = now == old ? 1.f : exp2f(old - now);             // 0 when nothing was accumulated yet
