@@ -404,47 +404,36 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                 ok = wait_for(&bars->epi_done, (units_done - 1) & 1u, bars, a.status_word);
                 if (!ok) break;
             }
-            // Queries, by group 0, four threads a row.  A row's largest magnitude fixes a power of two that puts it into
+            // Queries, sixteen threads a row, eight dims each.  A row's largest magnitude fixes a power of two that puts it into
             // [128, 256); the scaled row is the sum of a high part, rounded to e4m3, and a low part, the remainder rounded to
             // e4m3: exact for elements above 2^-9 of the largest.
-            if (grp == 0 && tid < 4 * kRp) {
-                const int r = tid >> 2, quarter = tid & 3;
+            if (tid < 16 * kRp) {
+                const int r = tid >> 4, piece = tid & 15;
                 const bool in_tree = r < R;
                 const int q_row = (i * a.N + (in_tree ? r / a.G : 0)) * a.Hq + un.kvh * a.G + (in_tree ? r % a.G : 0);
-                const uint4* src = reinterpret_cast<const uint4*>(a.q + (size_t)q_row * 128) + quarter * 4;
-                uint32_t top = 0;                                           // bf16 magnitudes compare as integers
+                const uint4 x = *(reinterpret_cast<const uint4*>(a.q + (size_t)q_row * 128) + piece);
+                uint32_t top = in_tree ? max(max(mag2(x.x), mag2(x.y)), max(mag2(x.z), mag2(x.w))) : 0u;     // bf16 magnitudes compare as integers
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint4 x = src[c];
-                    top = max(top, max(max(mag2(x.x), mag2(x.y)), max(mag2(x.z), mag2(x.w))));
-                }
-                if (!in_tree) top = 0;
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
                 const int e = (int)(top >> 7);                              // biased exponent of the largest
                 const uint32_t up = !in_tree ? 0u : top == 0 ? 127u : (uint32_t)min(254 + 7 - e, 254);  // 2^(7 - exponent); rows that are none: 0
                 const float f = __uint_as_float(up << 23);
-                if (quarter == 0) {
+                if (piece == 0) {
                     sh->row_scale[r] = top >= 0x7f80u ? CUDART_NAN_F : in_tree ? a.scale_log2 / f : 0.f;
                     sh->q_row[r] = q_row;
                 }
-                const uint32_t dst = sQ + (uint32_t)r * 128u;
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {                               // 8 dims at a time (again, from L1)
-                    const uint4 x = src[c];
-                    const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
-                    uint32_t h2[4], l2[4];
+                const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
+                uint32_t h2[4], l2[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float lo = __uint_as_float(w4[k] << 16) * f, hi = __uint_as_float(w4[k] & 0xffff0000u) * f;
-                        h2[k] = quant::encode2(lo, hi, kKvE4M3);
-                        const float2 back = quant::decode2(h2[k], kKvE4M3);
-                        l2[k] = quant::encode2(lo - back.x, hi - back.y, kKvE4M3);
-                    }
-                    const uint32_t at = dst + (uint32_t)(((quarter * 2 + (c >> 1)) ^ (r & 7)) << 4) + (c & 1) * 8u;
-                    st_shared8(at, h2[0] | (h2[1] << 16), h2[2] | (h2[3] << 16));
-                    st_shared8(at + kRp * 128u, l2[0] | (l2[1] << 16), l2[2] | (l2[3] << 16));
+                for (int k = 0; k < 4; ++k) {
+                    const float lo = __uint_as_float(w4[k] << 16) * f, hi = __uint_as_float(w4[k] & 0xffff0000u) * f;
+                    h2[k] = quant::encode2(lo, hi, kKvE4M3);
+                    const float2 back = quant::decode2(h2[k], kKvE4M3);
+                    l2[k] = quant::encode2(lo - back.x, hi - back.y, kKvE4M3);
                 }
+                const uint32_t at = sQ + (uint32_t)r * 128u + (uint32_t)(((piece >> 1) ^ (r & 7)) << 4) + (piece & 1) * 8u;
+                st_shared8(at, h2[0] | (h2[1] << 16), h2[2] | (h2[3] << 16));
+                st_shared8(at + kRp * 128u, l2[0] | (l2[1] << 16), l2[2] | (l2[3] << 16));
             }
             // A malformed tree: nothing is written for the request.
             bool tree_ok = true;
@@ -639,24 +628,20 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
             if (!ok) break;
             tc_fence_after();
             const bool split = un.n_chunks != 1;
-            if (tid_g < 8 && grp * 8 < kRp) {                            // the rows this group stores
-                const int r = grp * 8 + tid_g;
-                float M = -CUDART_INF_F;
-                for (int g = 0; g < kGroups; ++g) M = fmaxf(M, sh->m[g][r]);
-                float sum = 0.f;
-#pragma unroll 1
-                for (int g = 0; g < kGroups; ++g) {
-                    const float m = sh->m[g][r];
-                    const float w = m == -CUDART_INF_F ? 0.f : exp2f(m - M);
-                    sum += ((sh->sum[g][0][r] + sh->sum[g][1][r]) + (sh->sum[g][2][r] + sh->sum[g][3][r])) * w;
-                    sh->f[g][r] = w * sh->v_unit[g];
-                }
+            static_assert(kGroups * 8 == 32, "a lane for every group of eight rows");
+            if (quad == 0 && grp * 8 < kRp) {                            // the eight rows this group stores, a lane per row and group
+                const int g = lane >> 3, r = grp * 8 + (lane & 7);
+                const float m = sh->m[g][r];
+                float M = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 16));
+                const float w = m == -CUDART_INF_F ? 0.f : exp2f(m - M);
+                float sum = ((sh->sum[g][0][r] + sh->sum[g][1][r]) + (sh->sum[g][2][r] + sh->sum[g][3][r])) * w;
+                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
                 if (sh->row_scale[r] != sh->row_scale[r]) sum = CUDART_NAN_F;           // NaN or infinity among the queries
-                if (!split) {
-                    const float norm = sum == 0.f ? 0.f : 1.f / sum;
-                    for (int g = 0; g < kGroups; ++g) sh->f[g][r] *= norm;
-                }
-                if (tree_ok && r < R) {
+                const float norm = split ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+                sh->f[g][r] = w * sh->v_unit[g] * norm;
+                if (g == 0 && tree_ok && r < R) {
                     if (!split) {
                         if (a.lse) a.lse[sh->q_row[r]] = (M + log2f(sum)) * kLn2;
                     } else {
