@@ -17,8 +17,8 @@
 // A tile is 16 KB of K and 16 KB of V, rows of 128 bytes in the 128-byte swizzle, for either memory order: one tensor map
 // (d, token, head, page) with the pool's own strides, one copy per (page, head).
 //
-// Bound by HBM for 16 rows and fewer (64 requests of about 14000 keys, 8 kv heads, 1.82 GB: 329 us, 5.5 TB/s); for 32 rows the
-// exponentials and conversions of the softmax warps add up to more (447 us, 4.1 TB/s).  Single tokens (8 requests of 4096
+// Bound by HBM for 16 rows and fewer (64 requests of about 14000 keys, 8 kv heads, 1.82 GB: 327 us, 5.6 TB/s); for 32 rows the
+// exponentials and conversions of the softmax warps add up to more (420 us, 4.3 TB/s).  Single tokens (8 requests of 4096
 // keys, 67 MB): 30 us, of which planning takes 5 and the merge of split requests 6.  A row per lane, as for more rows, takes
 // 600 us and more for 32 rows; three slots fewer in the ring 10 % more.
 #include <cuda.h>

@@ -15,9 +15,9 @@
 // with it, sixteen 4-byte asynchronous copies for K and for V, so that no softmax warp waits for global memory.
 //
 // A tile is worked on in halves of 64 keys: while a group's softmax warps have one half, P V and the next tile's S of the other
-// are on the tensor cores, so the next S is ready when they come to it (whole tiles: 605 us below).
+// are on the tensor cores, so the next S is ready when they come to it (571 us against 598 with whole tiles, same GPU).
 //
-// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 590 us, 2.7 TB/s and 673 TFLOP/s of the two
+// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 575 us, 2.7 TB/s and 690 TFLOP/s of the two
 // products (each operand in two parts: twice that on the pipe).  Bound by the softmax warps: 11 instructions an element, two
 // warps a scheduler, half of the issue slots used.  TMEM has no room for a third group's S next to two O.  Sixteen softmax
 // warps, two threads a row, were slower in lockstep (754 us) and with the reference handed from half to half (639 us): what
