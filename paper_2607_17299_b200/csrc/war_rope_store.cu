@@ -8,8 +8,8 @@
 // again fell on the wrong side of a code's border); everything else is 32-bit arithmetic with one rounding at the end.
 //
 // Nothing here computes much: each value is read once and written once, and what matters is that every SM has rows to
-// move.  A thread block works for one request: it fills a table of (c, s) for the request's slots (shared by all heads
-// and both roles), and its warps then take tasks,
+// move.  A thread block works for one request: it fills a table of (c, s) for the depths of the request's tree (shared
+// by slots, heads and both roles), and its warps then take tasks,
 //   rows    one slot, up to kHeadsPerTask heads: eight lanes a row, two groups of eight elements (16 bytes) a lane, chosen so
 //           that an element and its partner are the same lane's; the lane's (c, s) stay in registers over the heads
 //   blocks  (8-bit pools) one head's K or V rows of one scale block: largest magnitude first, then the scale, the
@@ -153,8 +153,8 @@ __device__ __forceinline__ void rotate(Row& r, const Turn& t, const float2* tabl
 template <int kv, int kMode>
 __global__ void __launch_bounds__(kThreads, 2)
 war_rope_store_kernel(const StoreArgs a, const int parts) {
-    extern __shared__ __align__(16) float2 s_table[];                     // [N][half]
-    __shared__ int s_depth[kMaxSlots];
+    extern __shared__ __align__(16) float2 s_table[];                     // [depth, up to N of them][half]
+    __shared__ int s_depth[kMaxSlots], s_levels;
     __shared__ float s_scratch[kMode == kOdd ? kWarps : 1][4][128];
     const int b = blockIdx.x, part = blockIdx.y;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, side = lane >> 3;
@@ -178,6 +178,8 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
                 p0 = p0 >= 32 ? q01 : q00; p1 = p1 >= 32 ? q11 : q10;
             }
             s_depth[lane] = d0; s_depth[lane + 32] = d1;
+            const int deepest = __reduce_max_sync(0xffffffffu, max(d0, d1));
+            if (lane == 0) s_levels = deepest + 1;
         }
     }
     __syncthreads();
@@ -237,9 +239,9 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
     // the first task's values arrive while the table is filled
     int task = part * kWarps + warp;
     if (task < tasks) fetch_task(task);
-    for (int x = tid; x < n * a.half; x += kThreads) {
+    for (int x = tid; x < s_levels * a.half; x += kThreads) {
         const int j = x / a.half, i = x - j * a.half;
-        const double turns = (double)(pl + s_depth[j]) * ((double)a.inv_freq[i] * 0.15915494309189533577);
+        const double turns = (double)(pl + j) * ((double)a.inv_freq[i] * 0.15915494309189533577);
         double s, c;
         sincospi(2.0 * (turns - rint(turns)), &s, &c);
         s_table[j * a.half + table_at<kMode>(i, a.half)] = make_float2((float)(c * (double)a.factor), (float)(s * (double)a.factor));
@@ -251,7 +253,7 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
         if (!first) fetch_task(task);
         if (task >= block_tasks) {
             const int r = task - block_tasks, j = r / chunks, h0 = (r - j * chunks) * kHeadsPerTask;
-            const float2* table = s_table + j * a.half;
+            const float2* table = s_table + s_depth[j] * a.half;
             const Turn turn = load_turn<kMode>(table, at);
             const int h1 = min(h0 + kHeadsPerTask, heads);
 #pragma unroll
@@ -301,7 +303,7 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
             auto turned = [&](const Raw& raw, int j) -> Row {
                 Row r = widen(raw);
                 if (!which) {
-                    const float2* table = s_table + min(j + side, j1 - 1) * a.half;
+                    const float2* table = s_table + s_depth[min(j + side, j1 - 1)] * a.half;
                     rotate<kMode>(r, load_turn<kMode>(table, at), table, at);
                 }
                 return r;
