@@ -16,10 +16,10 @@
 //           re-encoding of older rows if the scale has grown, and the new rows (turned again from the kept input)
 // and the request's tasks are dealt over several thread blocks when there are few requests.
 //
-// Measured: 128 requests of 64 slots, 64 + 8 heads, bf16 pool (336 MB): 63 us, 5.3 TB/s (sixteen lanes a row with the partner
-// fetched by shuffle took 93).  256 requests of 8 slots, 32 + 8 heads, e4m3 pool (46 MB): 19 us (37 before); there the work is
-// in the scale blocks, which pass their values twice, and in the table's 64-bit functions, a seventh of all instructions.  One
-// slot of 8 requests: 4.7 us, the chain of dependent reads.
+// Measured: 128 requests of 64 slots, 64 + 8 heads, bf16 pool (336 MB): 59 us, 5.7 TB/s (sixteen lanes a row with the partner
+// fetched by shuffle took 93).  256 requests of 8 slots, 32 + 8 heads, e4m3 pool (46 MB): 18.5 us (37 before); there the
+// issue slots are the bound, most of them in the scale blocks, which pass their values twice.  One slot of 8 requests: 4.5 us, the
+// chain of dependent reads.
 #include <cuda_bf16.h>
 #include <math.h>
 #include "war_common.cuh"
@@ -49,7 +49,15 @@ struct StoreArgs {
     long long num_pages;
     float factor;
     int N, Hq, Hkv, page_size, max_pages, half, interleaved, block, blocks_per_page;
+    int chunks;                               // row tasks of a slot
+    uint32_t hkv_magic, chunks_magic;         // for quotient()
+    int page_shift, block_shift;              // logarithms of page_size (-1: no power of two) and block (8-bit pools)
 };
+
+// n / d for 0 <= n < 2^32 / d by a product with floor(2^32 / d) + 1 (a division by a run-time number is some 25 instructions, and
+// a task has six); magic 0: a division.
+__host__ __device__ __forceinline__ uint32_t magic_of(int d) { return d > 1 && d <= 4096 ? (uint32_t)((1ull << 32) / d + 1) : 0u; }
+__device__ __forceinline__ int quotient(int n, int d, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)n, magic) : n / d; }
 
 struct Raw { uint4 a, b; };                   // a lane's two groups of a row
 struct Row { float a[8], b[8]; };
@@ -194,11 +202,12 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
         return;
     }
     const int32_t* pt = a.page_table + (size_t)b * a.max_pages;
-    const int first_block = pl / a.block;
-    const int blocks = kv == kKvBf16 ? 0 : (pl + n - 1) / a.block - first_block + 1;
+    const int first_block = kv == kKvBf16 ? 0 : pl >> a.block_shift;
+    const int blocks = kv == kKvBf16 ? 0 : ((pl + n - 1) >> a.block_shift) - first_block + 1;
     const int block_tasks = 2 * a.Hkv * blocks;
     const int heads = a.Hq + (kv == kKvBf16 ? 2 * a.Hkv : 0);             // heads the row tasks cover: q, then k and v of a bf16 pool
-    const int chunks = (heads + kHeadsPerTask - 1) / kHeadsPerTask;
+    const int chunks = a.chunks;
+    auto page_index = [&](int pos) -> int { return a.page_shift >= 0 ? pos >> a.page_shift : pos / a.page_size; };
     const int tasks = block_tasks + n * chunks;
     const Place at = place<kMode>(lane, a.half, a.interleaved, s_scratch[kMode == kOdd ? warp : 0][side]);
 
@@ -229,11 +238,11 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
     };
     auto fetch_task = [&](int task) {
         if (task >= block_tasks) {
-            const int r = task - block_tasks, j = r / chunks;
+            const int r = task - block_tasks, j = quotient(r, chunks, a.chunks_magic);
             fetch_heads(j, (r - j * chunks) * kHeadsPerTask);
         } else {
-            const int pos0 = (first_block + (task >> 1) / a.Hkv) * a.block;
-            fetch_rows(task & 1, (task >> 1) % a.Hkv, max(0, pos0 - pl), min(n, pos0 + a.block - pl));
+            const int t = quotient(task >> 1, a.Hkv, a.hkv_magic), pos0 = (first_block + t) << a.block_shift;
+            fetch_rows(task & 1, (task >> 1) - t * a.Hkv, max(0, pos0 - pl), min(n, pos0 + a.block - pl));
         }
     };
     // the first task's values arrive while the table is filled
@@ -252,7 +261,7 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
     for (bool first = true; task < tasks; task += parts * kWarps, first = false) {
         if (!first) fetch_task(task);
         if (task >= block_tasks) {
-            const int r = task - block_tasks, j = r / chunks, h0 = (r - j * chunks) * kHeadsPerTask;
+            const int r = task - block_tasks, j = quotient(r, chunks, a.chunks_magic), h0 = (r - j * chunks) * kHeadsPerTask;
             const float2* table = s_table + s_depth[j] * a.half;
             const Turn turn = load_turn<kMode>(table, at);
             const int h1 = min(h0 + kHeadsPerTask, heads);
@@ -269,7 +278,8 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
                     dst = a.q_out + (((size_t)b * a.N + j) * a.Hq + h) * 128;
                 } else {
                     const int pos = pl + j;
-                    const long long page = pt[pos / a.page_size];
+                    const int pi = page_index(pos);
+                    const long long page = pt[pi];
                     if (page < 0 || page >= a.num_pages) {
                         if (at.s == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
                         continue;
@@ -277,7 +287,7 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
                     const bool is_k = h < a.Hq + a.Hkv;
                     const long long* st = is_k ? a.kp : a.vp;
                     const int kh = h - a.Hq - (is_k ? 0 : a.Hkv);
-                    dst = reinterpret_cast<__nv_bfloat16*>(is_k ? a.kpool : a.vpool) + page * st[0] + kh * st[1] + (long long)(pos % a.page_size) * st[2];
+                    dst = reinterpret_cast<__nv_bfloat16*>(is_k ? a.kpool : a.vpool) + page * st[0] + kh * st[1] + (long long)(pos - pi * a.page_size) * st[2];
                 }
                 *reinterpret_cast<uint4*>(dst + at.a) = in[u].a;
                 *reinterpret_cast<uint4*>(dst + at.b) = in[u].b;
@@ -286,18 +296,19 @@ war_rope_store_kernel(const StoreArgs a, const int parts) {
         }
         if constexpr (kv != kKvBf16) {
             // ---- one scale block of one head's K or V
-            const int which = task & 1, h = (task >> 1) % a.Hkv, t = (task >> 1) / a.Hkv;
-            const int pos0 = (first_block + t) * a.block;
+            const int t = quotient(task >> 1, a.Hkv, a.hkv_magic), which = task & 1, h = (task >> 1) - t * a.Hkv;
+            const int pos0 = (first_block + t) << a.block_shift;
             const int j0 = max(0, pos0 - pl), j1 = min(n, pos0 + a.block - pl);
-            const long long page = pt[pos0 / a.page_size];
+            const int pi = page_index(pos0);
+            const long long page = pt[pi];
             if (page < 0 || page >= a.num_pages) {
                 if (lane == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
                 continue;
             }
             const long long* ps = which ? a.vp : a.kp;
-            const int row0 = pos0 % a.page_size;
+            const int row0 = pos0 - pi * a.page_size;
             uint8_t* dst = (which ? a.vpool : a.kpool) + page * ps[0] + h * ps[1] + (long long)row0 * ps[2];
-            float* scale = (which ? a.vscale : a.kscale) + (page * a.Hkv + h) * a.blocks_per_page + row0 / a.block;
+            float* scale = (which ? a.vscale : a.kscale) + (page * a.Hkv + h) * a.blocks_per_page + (row0 >> a.block_shift);
             const int old = min(max(pl - pos0, 0), a.block);              // rows of earlier tokens in the block
             const float s_old = old > 0 ? *scale : 0.f;
             auto turned = [&](const Raw& raw, int j) -> Row {
@@ -416,8 +427,13 @@ extern "C" war_status_t war_rope_store(const void* d_q, const void* d_k, const v
     a.half = p->rot_dim / 2; a.interleaved = p->interleaved;
     a.block = p->kv_type == kKvBf16 ? p->page_size : p->scale_block;
     a.blocks_per_page = p->page_size / a.block;
+    a.page_shift = -1; a.block_shift = 0;
+    for (int k = 0; k < 30; ++k) if (p->page_size == 1 << k) a.page_shift = k;
+    while (p->kv_type != kKvBf16 && 1 << a.block_shift < a.block) ++a.block_shift;
     // how many thread blocks share a request: enough to fill the GPU, no more than there are tasks
     const long long heads = p->Hq + (p->kv_type == kKvBf16 ? 2ll * p->Hkv : 0);
+    a.chunks = (int)((heads + kHeadsPerTask - 1) / kHeadsPerTask);
+    a.hkv_magic = magic_of(p->Hkv); a.chunks_magic = magic_of(a.chunks);
     const long long tasks = (p->kv_type == kKvBf16 ? 0 : 2ll * p->Hkv * ((p->N + a.block - 2) / a.block + 1)) +
                             (long long)p->N * ((heads + kHeadsPerTask - 1) / kHeadsPerTask);
     long long parts = kResident / p->B;
