@@ -31,7 +31,7 @@ struct CommitArgs {
     int* status_word;
     long long ks[3], vs[3];                   // pool strides (page, head, token) in elements
     long long num_pages;
-    int N, P, Hkv, page_size, max_pages, block, blocks_per_page;
+    int N, P, Hkv, page_size, max_pages, block, block_shift, blocks_per_page;     // block: a power of two
 };
 
 __global__ void __launch_bounds__(kThreads)
@@ -62,8 +62,8 @@ war_commit_quant_kernel(const CommitArgs a, const int kv) {
 
     if (running && !wrong && k > 0) {
         const int32_t* pt = a.page_table + (size_t)b * a.max_pages;
-        const int fb = (pl + 1) / a.block;                                // first block that can receive a row
-        const int n_blocks = (pl + last) / a.block - fb + 1;              // blocks that hold sources or destinations: at most 10
+        const int fb = (pl + 1) >> a.block_shift;                                // first block that can receive a row
+        const int n_blocks = ((pl + last) >> a.block_shift) - fb + 1;              // blocks that hold sources or destinations: at most 10
         // lane l: page and place of block fb + l
         long long page = -1;
         if (lane < n_blocks) page = pt[(int)((long long)(fb + lane) * a.block / a.page_size)];
@@ -74,19 +74,19 @@ war_commit_quant_kernel(const CommitArgs a, const int kv) {
             const int which = task & 1, h = task >> 1;
             const long long* st = which ? a.vs : a.ks;
             uint8_t* pool = which ? a.vpool : a.kpool;
-            float* scale_p = (which ? a.vscale : a.kscale) + ((page_ok ? page : 0) * a.Hkv + h) * a.blocks_per_page + row_in_page / a.block;
+            float* scale_p = (which ? a.vscale : a.kscale) + ((page_ok ? page : 0) * a.Hkv + h) * a.blocks_per_page + (row_in_page >> a.block_shift);
             const float scale = page_ok && lane < n_blocks ? *scale_p : 0.f;
             const long long base = page_ok ? page * st[0] + h * st[1] + (long long)row_in_page * st[2] : -1;
             // new scale of every receiving block: the largest among the blocks its live rows come from
-            float s_new = lane == 0 && (pl + 1) % a.block != 0 ? scale : 0.f;        // rows up to the root stay where they are
+            float s_new = lane == 0 && ((pl + 1) & (a.block - 1)) != 0 ? scale : 0.f;        // rows up to the root stay where they are
             for (int d = 0; d < k; ++d) {
-                const int from = (pl + slot_of(d)) / a.block - fb, to = (pl + 1 + d) / a.block - fb;
+                const int from = ((pl + slot_of(d)) >> a.block_shift) - fb, to = ((pl + 1 + d) >> a.block_shift) - fb;
                 const float s = __shfl_sync(0xffffffffu, scale, from);               // (0 for a block whose page is bad)
                 if (lane == to) s_new = fmaxf(s_new, s);
             }
             if (!(s_new > 0.f)) s_new = scale;
             // rows that stay in a block whose scale has grown: those up to the root, and accepted slots already in place
-            const int t_last = (pl + k) / a.block - fb;
+            const int t_last = ((pl + k) >> a.block_shift) - fb;
             for (int t = 0; t <= t_last; ++t) {
                 const float so = __shfl_sync(0xffffffffu, scale, t), sn = __shfl_sync(0xffffffffu, s_new, t);
                 const long long at = __shfl_sync(0xffffffffu, base, t);
@@ -116,7 +116,7 @@ war_commit_quant_kernel(const CommitArgs a, const int kv) {
                     const int d = d0 + 4 * u + (lane >> 3), dc = min(d, k - 1);
                     const int slot = slot_of(dc);
                     const int src = pl + slot, dst = pl + 1 + dc;
-                    const int from = src / a.block - fb, to = dst / a.block - fb;
+                    const int from = (src >> a.block_shift) - fb, to = (dst >> a.block_shift) - fb;
                     const long long from_at = __shfl_sync(0xffffffffu, base, from);
                     const float so = __shfl_sync(0xffffffffu, scale, from), sn = __shfl_sync(0xffffffffu, s_new, to);
                     to_at[u] = __shfl_sync(0xffffffffu, base, to);
@@ -192,6 +192,8 @@ extern "C" war_status_t war_commit_quant(const int32_t* d_ids, const int32_t* d_
     a.prefix_len = d_prefix_len; a.tail = d_tail; a.tail_len = d_tail_len; a.status_word = status_word;
     for (int i = 0; i < 3; ++i) { a.ks[i] = p->k_strides[i]; a.vs[i] = p->v_strides[i]; }
     a.num_pages = p->num_pages; a.N = p->N; a.P = p->P; a.Hkv = p->Hkv; a.page_size = p->page_size; a.max_pages = p->max_pages_per_req;
+    a.block_shift = 0;
+    while (1 << a.block_shift < q->scale_block) ++a.block_shift;
     a.block = q->scale_block; a.blocks_per_page = p->page_size / q->scale_block;
     int parts = (2 * p->Hkv + kWarps - 1) / kWarps;                       // a warp per (head, K or V), at most eight blocks
     if (parts > 8) parts = 8;
