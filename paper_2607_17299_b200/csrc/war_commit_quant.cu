@@ -70,6 +70,10 @@ war_commit_quant_kernel(const CommitArgs a, const int kv) {
         const bool page_ok = page >= 0 && page < a.num_pages;
         if (lane < n_blocks && !page_ok && part == 0 && warp == 0) war_set_device_status(a.status_word, WAR_ERR_BAD_PAGE);
         const int row_in_page = lane < n_blocks ? (int)((long long)(fb + lane) * a.block % a.page_size) : 0;
+        const int t_last = ((pl + k) >> a.block_shift) - fb;              // last block that receives a row
+        // lane l: source and destination block of the path's slots l and l + 32
+        const int from0 = lane < k ? ((pl + s0) >> a.block_shift) - fb : 0, to0 = lane < k ? ((pl + 1 + lane) >> a.block_shift) - fb : -1;
+        const int from1 = lane + 32 < k ? ((pl + s1) >> a.block_shift) - fb : 0, to1 = lane + 32 < k ? ((pl + 33 + lane) >> a.block_shift) - fb : -1;
         for (int task = part * kWarps + warp; task < 2 * a.Hkv; task += parts * kWarps) {
             const int which = task & 1, h = task >> 1;
             const long long* st = which ? a.vs : a.ks;
@@ -79,14 +83,15 @@ war_commit_quant_kernel(const CommitArgs a, const int kv) {
             const long long base = page_ok ? page * st[0] + h * st[1] + (long long)row_in_page * st[2] : -1;
             // new scale of every receiving block: the largest among the blocks its live rows come from
             float s_new = lane == 0 && ((pl + 1) & (a.block - 1)) != 0 ? scale : 0.f;        // rows up to the root stay where they are
-            for (int d = 0; d < k; ++d) {
-                const int from = ((pl + slot_of(d)) >> a.block_shift) - fb, to = ((pl + 1 + d) >> a.block_shift) - fb;
-                const float s = __shfl_sync(0xffffffffu, scale, from);               // (0 for a block whose page is bad)
-                if (lane == to) s_new = fmaxf(s_new, s);
+            const float a0 = __shfl_sync(0xffffffffu, scale, from0), a1 = __shfl_sync(0xffffffffu, scale, from1);    // (0 for a block whose page is bad)
+            for (int t = 0; t <= t_last; ++t) {
+                // (scales are not negative: ordered as whole numbers)
+                const uint32_t m = max(to0 == t && a0 > 0.f ? __float_as_uint(a0) : 0u, to1 == t && a1 > 0.f ? __float_as_uint(a1) : 0u);
+                const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, m));
+                if (lane == t) s_new = fmaxf(s_new, top);
             }
             if (!(s_new > 0.f)) s_new = scale;
             // rows that stay in a block whose scale has grown: those up to the root, and accepted slots already in place
-            const int t_last = ((pl + k) >> a.block_shift) - fb;
             for (int t = 0; t <= t_last; ++t) {
                 const float so = __shfl_sync(0xffffffffu, scale, t), sn = __shfl_sync(0xffffffffu, s_new, t);
                 const long long at = __shfl_sync(0xffffffffu, base, t);
