@@ -175,6 +175,14 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
         un.slot = u; un.slot_base = 0; un.slot_stride = 0; un.bump = 0;
         return true;
     };
+    // A load has landed.  Parities tell a phase from the next one only, and whoever waits here does not see every load of a slot:
+    // if another issuer's load before this is still on its way, its phase would pass for this one.  So that one has to be
+    // consumed first.  (It has been issued by then: the caller has seen a later load of its producer land, or the unit
+    // before is through; so the load before that is consumed and the wait on `empty` cannot take one phase for another.)
+    auto landed = [&](uint32_t sq) -> bool {
+        const uint32_t slot = sq % kSlots, phase = (sq / kSlots) & 1u;
+        return wait_for(&bars->empty[slot], phase ^ 1u, bars, a.status_word) && wait_for(&bars->full[slot], phase, bars, a.status_word);
+    };
     const int pages_per_tile = kTileKeys / a.page_size;
     const uint32_t page_bytes = (uint32_t)a.page_size * 128u;
 
@@ -324,7 +332,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
             ok = wait_for(&bars->q_ready, units_done & 1u, bars, a.status_word);
             for (int g = w; g < kGroups && g < T && ok; g += 2) {
                 const uint32_t sq = seq_k(ld0, g), slot = sq % kSlots;
-                ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
+                ok = landed(sq);
                 if (!ok) break;
                 tc_fence_after();
                 if (lane == 0) mma_s(g, slot);
@@ -336,8 +344,8 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                 const bool has_s = t + kGroups < T;                      // the group's next S goes out in the same burst as PV(t)
                 const uint32_t sq_k = seq_k(ld0, t + kGroups), slot_k = sq_k % kSlots;
                 const uint32_t done = g >= 2 ? tiles_done[1]++ : tiles_done[0]++;
-                ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
-                if (ok && has_s) ok = wait_for(&bars->full[slot_k], (sq_k / kSlots) & 1u, bars, a.status_word);
+                ok = landed(sq);
+                if (ok && has_s) ok = landed(sq_k);
                 if (ok) ok = wait_for(&bars->p_ready[g], done & 1u, bars, a.status_word);
                 if (!ok) break;
                 tc_fence_after();
@@ -593,7 +601,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                 // 0 x NaN garbage would still poison the product)
                 if (key0 + kTileKeys > L) {
                     const uint32_t sq = seq_v(ld0, t, T), slot = sq % kSlots;
-                    ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
+                    ok = landed(sq);
                     if (!ok) break;
                     if (key >= L - key0) {
                         const uint32_t base = sRing + slot * kSlotBytes + (uint32_t)key * 128u;

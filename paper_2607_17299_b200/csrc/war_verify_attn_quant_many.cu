@@ -131,6 +131,14 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         un.slot = u; un.slot_base = 0; un.slot_stride = 0; un.bump = 0;
         return true;
     };
+    // A load has landed.  Parities tell a phase from the next one only, and whoever waits here does not see every load of a slot:
+    // if another issuer's load before this is still on its way, its phase would pass for this one.  So that one has to be
+    // consumed first.  (It has been issued by then: the caller has seen a later load of its producer land, or the unit
+    // before is through; so the load before that is consumed and the wait on `empty` cannot take one phase for another.)
+    auto landed = [&](uint32_t sq) -> bool {
+        const uint32_t slot = sq % kSlots, phase = (sq / kSlots) & 1u;
+        return wait_for(&bars->empty[slot], phase ^ 1u, bars, a.status_word) && wait_for(&bars->full[slot], phase, bars, a.status_word);
+    };
     const int pages_per_tile = kTileKeys / a.page_size;
     const uint32_t page_bytes = (uint32_t)a.page_size * 128u;
 
@@ -281,7 +289,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             ok = wait_for(&bars->q_ready, units_done & 1u, bars, a.status_word);
             if (ok && g < T) {
                 const uint32_t sq = seq_k(ld0, g), slot = sq % kSlots;
-                ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
+                ok = landed(sq);
                 if (ok) {
                     tc_fence_after();
                     if (lane == 0) { mma_s(slot, 0); mma_s(slot, 1); umma_commit(&bars->empty[slot]); }
@@ -292,8 +300,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 const uint32_t sq = seq_v(ld0, t, T), slot = sq % kSlots;
                 const bool has_s = t + 2 < T;                        // S(t+2) of a half goes out behind its P V(t)
                 const uint32_t sq_k = has_s ? seq_k(ld0, t + 2) : 0u, slot_k = sq_k % kSlots;
-                ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
-                if (ok && has_s) ok = wait_for(&bars->full[slot_k], (sq_k / kSlots) & 1u, bars, a.status_word);
+                ok = landed(sq);
+                if (ok && has_s) ok = landed(sq_k);
 #pragma unroll 1
                 for (int half = 0; half < 2 && ok; ++half) {
                     ok = wait_for(&bars->p_ready[g][half], cg & 1u, bars, a.status_word);
@@ -546,14 +554,19 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
 #pragma unroll 1
                 for (int half = 0; half < 2 && ok; ++half) {
                     if (warp_valid) ok = twice ? step(t, half, std::integral_constant<int, 32>()) : step(t, half, std::integral_constant<int, 64>());
-                    else { ok = wait_for(&bars->s_ready[grp][half], cgm & 1u, bars, a.status_word); tc_fence_after(); }
+                    else {
+                        const uint32_t ti = ld0 / 2 + t;                   // (its scales as well: no phase of theirs is passed over)
+                        ok = wait_for(&bars->scales[ti & (kScaleTiles - 1)], (ti / kScaleTiles) & 1u, bars, a.status_word) &&
+                             wait_for(&bars->s_ready[grp][half], cgm & 1u, bars, a.status_word);
+                        tc_fence_after();
+                    }
                     if (!ok) break;
                     // the unit's last tile may hold rows past the request's last key: zero their V (P is exactly 0 there,
                     // but 0 x NaN garbage would still poison the product)
                     const int key0 = (un.tile_begin + t) * kTileKeys;
                     if (half == 0 && key0 + kTileKeys > L) {
                         const uint32_t sq = seq_v(ld0, t, T), slot = sq % kSlots;
-                        ok = wait_for(&bars->full[slot], (sq / kSlots) & 1u, bars, a.status_word);
+                        ok = landed(sq);
                         if (!ok) break;
                         if (row >= L - key0) {
                             const uint32_t base = sRing + slot * kSlotBytes + (uint32_t)row * 128u;
