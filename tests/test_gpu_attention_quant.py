@@ -280,3 +280,35 @@ def test_no_lse_and_empty_batch(war):
     c.dnn.zero_()
     out, lse = c.run(war)
     assert (out == 7).all() and (lse == 7).all() and war.war_device_status() == 0
+
+
+@pytest.mark.parametrize("N,B,page", [(3, 33, 32), (24, 8, 16)])
+def test_long_units_give_the_same_bits_again_and_again(war, N, B, page):
+    """Units of hundreds of tiles over a gigabyte of scattered pages, launched back to back: loads come late and out of order, and
+    no launch may use one before it is there."""
+    Hq, Hkv, L = 8, 2, 54648
+    g = torch.Generator(DEV).manual_seed(93)
+    pages = -(-(L + N) // page)
+    table = torch.randperm(B * pages, generator=g, device=DEV).to(torch.int32).view(B, pages)
+    k, v = (torch.randint(0, 0x78, (B * pages, page, Hkv, 128), generator=g, device=DEV, dtype=torch.uint8).view(torch.float8_e4m3fn).permute(0, 2, 1, 3)
+            for _ in range(2))
+    ks, vs = (torch.full((B * pages, Hkv, 1), 2.0 ** -8, device=DEV) for _ in range(2))
+    q = torch.randn((B, N, Hq, 128), generator=g, device=DEV).to(torch.bfloat16)
+    nn, prefix = torch.full((B,), N, dtype=torch.int32, device=DEV), torch.full((B,), L, dtype=torch.int32, device=DEV)
+    parent = (torch.arange(N, device=DEV, dtype=torch.int32) - 1).expand(B, N).contiguous()
+    params = war.attn_quant_params(q, k, v, ks, vs, table, 0.05)
+    ws, out, lse = war.new_quant_workspace(params, DEV), torch.zeros_like(q), torch.zeros((B, N, Hq), device=DEV)
+    call = lambda: war.war_verify_attn_quant(q, k, v, ks, vs, table, prefix, nn, parent, params, ws, out, lse)
+    call()
+    torch.cuda.synchronize()
+    first = out.clone(), lse.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(10):
+            call()
+    for _ in range(5):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    assert war.war_device_status() == 0
