@@ -35,6 +35,7 @@ constexpr int kResident = 148 * 2;            // thread blocks that a B200 holds
 // How a lane's elements are laid out: kSplit (a pair is half the rotation apart), kAdjacent (a pair is two neighbours), both
 // where the rotation covers whole lanes; kOdd takes every other rot_dim, through shared memory.
 constexpr int kSplit = 0, kAdjacent = 1, kOdd = 2;
+constexpr int kScratchRow = 136;              // floats from row to row: four rows' neighbours in different banks
 
 struct StoreArgs {
     const __nv_bfloat16 *q, *k, *v;
@@ -88,7 +89,7 @@ struct Place {
     int s, a, b;                              // lane of the row (0 to 7); first elements of its groups
     int half, interleaved;
     bool turns;                               // its elements rotate (kSplit, kAdjacent)
-    float* scratch;                           // 128 floats of this row's eight lanes (kOdd)
+    float* scratch;                           // kScratchRow floats of this row's eight lanes (kOdd)
 };
 template <int kMode>
 __device__ __forceinline__ Place place(int lane, int half, int interleaved, float* scratch) {
@@ -98,8 +99,9 @@ __device__ __forceinline__ Place place(int lane, int half, int interleaved, floa
     p.turns = p.s < g;
     const bool split = kMode == kSplit && p.turns;
     // kSplit: group s and the one half the rotation later; lanes past the rotation share the groups behind it: 2 * s and 2 * s + 1
-    p.a = split ? 8 * p.s : 16 * p.s;
-    p.b = split ? 8 * p.s + half : 16 * p.s + 8;
+    // kOdd: the lanes' groups side by side, in both halves of the head
+    p.a = split || kMode == kOdd ? 8 * p.s : 16 * p.s;
+    p.b = split ? 8 * p.s + half : kMode == kOdd ? 64 + 8 * p.s : 16 * p.s + 8;
     return p;
 }
 
@@ -143,10 +145,15 @@ __device__ __forceinline__ void rotate(Row& r, const Turn& t, const float2* tabl
         }
     } else {
         __syncwarp();
+        float4* const a4 = reinterpret_cast<float4*>(p.scratch + p.a);
+        float4* const b4 = reinterpret_cast<float4*>(p.scratch + p.b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { p.scratch[p.a + i] = r.a[i]; p.scratch[p.b + i] = r.b[i]; }
+        for (int i = 0; i < 2; ++i) {
+            a4[i] = make_float4(r.a[4 * i], r.a[4 * i + 1], r.a[4 * i + 2], r.a[4 * i + 3]);
+            b4[i] = make_float4(r.b[4 * i], r.b[4 * i + 1], r.b[4 * i + 2], r.b[4 * i + 3]);
+        }
         __syncwarp();
-#pragma unroll 1
+#pragma unroll 2
         for (int k = p.s; k < p.half; k += 8) {
             const float2 cs = table[k];
             float* x = p.scratch + (p.interleaved ? 2 * k : k);
@@ -154,7 +161,11 @@ __device__ __forceinline__ void rotate(Row& r, const Turn& t, const float2* tabl
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { r.a[i] = p.scratch[p.a + i]; r.b[i] = p.scratch[p.b + i]; }
+        for (int i = 0; i < 2; ++i) {
+            const float4 x = a4[i], y = b4[i];
+            r.a[4 * i] = x.x; r.a[4 * i + 1] = x.y; r.a[4 * i + 2] = x.z; r.a[4 * i + 3] = x.w;
+            r.b[4 * i] = y.x; r.b[4 * i + 1] = y.y; r.b[4 * i + 2] = y.z; r.b[4 * i + 3] = y.w;
+        }
     }
 }
 
@@ -163,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 war_rope_store_kernel(const StoreArgs a, const int parts) {
     extern __shared__ __align__(16) float2 s_table[];                     // [depth, up to N of them][half]
     __shared__ int s_depth[kMaxSlots], s_levels;
-    __shared__ float s_scratch[kMode == kOdd ? kWarps : 1][4][128];
+    __shared__ __align__(16) float s_scratch[kMode == kOdd ? kWarps : 1][4][kScratchRow];
     const int b = blockIdx.x, part = blockIdx.y;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, side = lane >> 3;
     const int n = a.num_nodes[b], pl = a.prefix_len[b];
