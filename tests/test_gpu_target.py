@@ -158,6 +158,17 @@ def test_rows_that_are_hard_to_dismiss(war, kind, dtype):
     c.check(war)
 
 
+@pytest.mark.parametrize("V", [8000, 7770, 8096])
+def test_tables_around_the_shared_memory_limit(war, V):
+    """A slice whose tables come to just below, about and just above the 48 KB that a launch has to ask for, the kernel's own variables
+    included."""
+    for W in range(V, V + 64, 32):
+        c = Case(49, 1, 1, 4 * W, "bf16", ctx=30, bias=2)
+        c.check(war)
+    c = Case(50, 120, 1, 4 * V, "bf16", ctx=30, bias=2, mask=None)          # four slices
+    c.check(war)
+
+
 def test_requests_without_slots_and_many_requests(war):
     c = Case(48, 700, 2, 300, "bf16")
     c.nn[::3] = 0
