@@ -122,8 +122,8 @@ __device__ __forceinline__ uint32_t mag2(uint32_t w) { return max(w & 0x7fffu, (
 // Four scaled weights (two pairs, each divided by 256) as high (e4m3) and low (e5m2) codes, four of each.  The pipe that
 // holds the 8-bit conversions is the busiest but one here, so both codes are cut out of halves: a half of x / 256 holds in
 // its bits 7 to 14 the e4m3 code of x (the two exponent biases differ by 8), rounded by adding half a step before the cut;
-// the remainder is exact, and its e5m2 code is a half's upper byte, rounded the same way.  Together they hold x to 2^-8 of
-// itself, or to 2^-17 for the smallest.
+// the remainder is exact, and its e5m2 code is a half's upper byte, rounded the same way.  Together they hold x to 2^-7.8 of
+// itself, or to 2^-13.8 where it is below 2^-6 (the high part's step is 2^-9 there, and the low part holds the rest to 2^-3).
 __device__ __forceinline__ void split_weights(float2 x01, float2 x23, uint32_t& high, uint32_t& low) {
     asm("{\n.reg .b32 y0, y1, h0, h1, d0, d1, s0, s1;\n"
         "cvt.rn.f16x2.f32 y0, %3, %2;\n"
@@ -143,6 +143,12 @@ __device__ __forceinline__ void split_weights(float2 x01, float2 x23, uint32_t& 
         "prmt.b32 %0, s0, s1, 0x7531;\n"
         "prmt.b32 %1, d0, d1, 0x7531;\n}\n"
         : "=r"(high), "=r"(low) : "f"(x01.x), "f"(x01.y), "f"(x23.x), "f"(x23.y), "r"(0x5c005c00u));
+}
+
+// from the scales of a group's first tile, one a lane
+__device__ __forceinline__ float v_reference(float scale) {
+    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(scale));         // (not negative: ordered as integers)
+    return top == 0 || top >= 0x21800000u ? kVRefLarge : kVRefSmall;                      // (2^-60)
 }
 
 // A pool as (d, token, head, page) with its own strides and a box of one (page, head).

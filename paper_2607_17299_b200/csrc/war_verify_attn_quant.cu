@@ -16,7 +16,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kTile = 32;
 constexpr int kSub = 16;
 
-// One thread per query row; K and V codes are staged as halves (every code is one), their scales beside them.
+// One thread per query row; K and V codes are staged as halves (every code is one), their scales beside them, and V's
+// logarithms (see war_attn_quant.cuh).
 __global__ void __launch_bounds__(128)
 attn_quant_simple_kernel(const __nv_bfloat16* __restrict__ q, const AttnQuantPools pools, const int32_t* __restrict__ page_table,
                          const int32_t* __restrict__ prefix_len, int N, int Hq, int Hkv, int G, int page_size, int max_pages,
@@ -24,7 +25,7 @@ attn_quant_simple_kernel(const __nv_bfloat16* __restrict__ q, const AttnQuantPoo
                          float* __restrict__ lse, int* status_word) {
     __shared__ __align__(16) uint32_t sK[kTile][64];
     __shared__ __align__(16) uint32_t sV[kTile][64];
-    __shared__ float s_scale[2][kTile];
+    __shared__ float s_scale[2][kTile], s_lv[kTile];
     __shared__ int s_unit;
     const int tid = threadIdx.x;
     while (true) {
@@ -82,7 +83,10 @@ attn_quant_simple_kernel(const __nv_bfloat16* __restrict__ q, const AttnQuantPoo
                 uint32_t* dst = &(which ? sV : sK)[row][piece * 4];
                 dst[0] = quant::decode2_half(val.x & 0xffffu, pools.kv); dst[1] = quant::decode2_half(val.x >> 16, pools.kv);
                 dst[2] = quant::decode2_half(val.y & 0xffffu, pools.kv); dst[3] = quant::decode2_half(val.y >> 16, pools.kv);
-                if (piece == 0) s_scale[which][row] = sc;
+                if (piece == 0) {
+                    s_scale[which][row] = sc;
+                    if (which) s_lv[row] = v_log(v_relative(sc, kVRefLarge));
+                }
             }
             __syncthreads();
             if (!active) continue;
@@ -103,7 +107,7 @@ attn_quant_simple_kernel(const __nv_bfloat16* __restrict__ q, const AttnQuantPoo
                     }
                     const bool vis = pos < pl || (pos < k_end && ((anc >> (pos - pl)) & 1ull));
                     s[kk] = vis ? a * s_scale[0][sub + kk] * scale_log2 : -CUDART_INF_F;
-                    tmax = fmaxf(tmax, s[kk]);
+                    tmax = fmaxf(tmax, s[kk] + s_lv[sub + kk]);
                 }
                 if (tmax == -CUDART_INF_F) continue;
                 const float m_new = fmaxf(m, tmax);
@@ -128,8 +132,9 @@ attn_quant_simple_kernel(const __nv_bfloat16* __restrict__ q, const AttnQuantPoo
             }
         }
         if (active) {
+            const float down = normal_sum(m, l);
             if (un.n_chunks == 1) {
-                const float inv = 1.f / l;
+                const float inv = down / l;
                 __nv_bfloat162* dst = reinterpret_cast<__nv_bfloat162*>(out + qrow * 128);
 #pragma unroll
                 for (int d = 0; d < 64; ++d) dst[d] = __floats2bfloat162_rn(acc[2 * d] * inv, acc[2 * d + 1] * inv);
@@ -137,7 +142,7 @@ attn_quant_simple_kernel(const __nv_bfloat16* __restrict__ q, const AttnQuantPoo
             } else {
                 float* po = w.part_o + ((size_t)u * w.rows + tid) * 128;
 #pragma unroll
-                for (int d = 0; d < 128; ++d) po[d] = acc[d];
+                for (int d = 0; d < 128; ++d) po[d] = acc[d] * down;
                 w.part_ml[((size_t)u * w.rows + tid) * 2] = m;
                 w.part_ml[((size_t)u * w.rows + tid) * 2 + 1] = l;
             }

@@ -5,7 +5,8 @@
 //
 //   S = K Qh' + K Ql'      128 keys x the rows; q (scaled by a power of two per row) = Qh + Ql, both e4m3
 //   p = exp2(S * (row's constant * K's scale of the key's block) - the row's reference)
-//   O' += V' Ph + V' Pl    128 dims x the rows; p * (V's scale of the key's block) = Ph + Pl, e4m3 and e5m2
+//   O' += V' Ph + V' Pl    128 dims x the rows; p * (V's scale of the key's block) = Ph + Pl, e4m3 and e5m2; the row's
+//                          reference follows these, not the p alone (see war_attn_quant.cuh)
 //
 // So a softmax thread has one key and all rows, and a tile of 128 keys costs sixteen products of 16 or 32 columns, each bound
 // by the 4 KB of K or V that it reads from shared memory.  Rows' maxima lie across the lanes: a tile is worked out relative
@@ -45,10 +46,9 @@ constexpr int kMaxRows = 32;
 // What a unit costs in the split, times the bf16 kernel's tiles: with 32 rows a boundary takes as long as some fifteen tiles of
 // 32 KB (64 requests of 8 slots 468 -> 447 us, 20 requests 158 -> 152; with 16 rows it made 326 us 332).
 template <int kRp> constexpr int kUnitCostOf = kRp == 32 ? 3 : 1;
-// The largest scaled weight is 2^kRescaleThreshold (a stale maximum) * 2 (V's scale against its reference) * kWeightTop = 448,
-// the largest e4m3 value.
+// The largest weight is 2^kRescaleThreshold (a stale reference) * kWeightTop = 448, the largest e4m3 value.
 constexpr float kRescaleThreshold = 3.0f;          // log2 units
-constexpr float kWeightTop = 28.f;
+constexpr float kWeightTop = 56.f;
 constexpr float kMargin = 1.f;                      // a new reference lies this far above the maximum
 constexpr float kNoMax = 1e30f;                     // stands for minus the maximum of a row that has seen no key yet
 
@@ -462,7 +462,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
             ok = wait_for(&bars->q_ready, units_done & 1u, bars, a.status_word);
             if (!ok) break;
 
-            float v_ref = 0.f;                                             // power of two that V's scales are taken relative to
+            float v_ref = 1.f;                                             // power of two that V's scales are taken relative to
             float l[kRp];
 #pragma unroll
             for (int r = 0; r < kRp; ++r) l[r] = 0.f;
@@ -473,15 +473,8 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                 ok = wait_for(&bars->scales[ti & (kScaleTiles - 1)], (ti / kScaleTiles) & 1u, bars, a.status_word);
                 if (!ok) break;
                 const float ks = sc[key >> 3];
-                // V's scales relative to a power of two that follows the largest one seen: a factor below 2
-                const float sv_top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sc[16 + (lane & 15)])));
-                float v_corr = 1.f;
-                if (sv_top >= 2.f * v_ref) {
-                    const float ref = __uint_as_float(max(__float_as_uint(sv_top) & 0x7f800000u, 0x0c800000u));   // at least 2^-102
-                    v_corr = v_ref / ref;
-                    v_ref = ref;
-                }
-                const float vs = sc[16 + (key >> 3)] * (kWeightTop / 256.f / v_ref);       // (split_weights wants x / 256)
+                if (t == grp) v_ref = v_reference(sc[16 + (lane & 15)]);
+                const float vs = v_relative(sc[16 + (key >> 3)], v_ref) * (kWeightTop / 256.f);       // (split_weights wants x / 256)
                 // Which rows see this thread's key: all (prefix), none (past the request's end), or those with the key's
                 // tree slot among their ancestors.
                 uint32_t see = ~0u;
@@ -498,8 +491,8 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                 tc_fence_after();
 
                 // x = S * (row's and key's scales) - the row's reference, -inf where the row does not see the key; p = exp2(x).
-                // If some x of the group is above 2^kRescaleThreshold the references are renewed and all is worked out again;
-                // the group's four warps tell each other while the exponentials are under way.
+                // If some x + lv (p with V's scale, what the tensor cores get) of the group is above kRescaleThreshold the references
+                // are renewed and all is worked out again; the group's four warps tell each other while the exponentials are under way.
                 float x[kRp];
                 const float2 ks2 = make_float2(ks, ks);
                 bool viol = false;
@@ -525,7 +518,8 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                         float top[2] = {-CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
                         for (int r = 0; r < kRp; r += 4) { top[0] = max3(top[0], x[r], x[r + 1]); top[1] = max3(top[1], x[r + 2], x[r + 3]); }
-                        const bool mine = __any_sync(0xffffffffu, fmaxf(top[0], top[1]) > kRescaleThreshold);
+                        const float lv = v_log(vs * (256.f / kWeightTop));
+                        const bool mine = __any_sync(0xffffffffu, fmaxf(top[0], top[1]) + lv > kRescaleThreshold);
                         if (lane == 0) word[quad] = mine;
                         warp_arrive(&bars->vote[grp], lane);
                     }
@@ -537,12 +531,13 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                     const int4 w = *reinterpret_cast<const int4*>(word);
                     viol = (w.x | w.y | w.z | w.w) != 0;
                     if (!viol) break;
-                    // ---- the tile's row maxima (of S * scales, read again), and new references for all rows
+                    // ---- the tile's row maxima (of S * scales + lv, read again), and new references for all rows
                     if constexpr (kRp == 32) tmem_ld32(tS, reinterpret_cast<uint32_t*>(x));
                     else tmem_ld16(tS, reinterpret_cast<uint32_t*>(x));
                     tmem_wait_ld();
+                    const float lv = v_log(vs * (256.f / kWeightTop));
 #pragma unroll
-                    for (int r = 0; r < kRp; ++r) x[r] = (see >> r) & 1u ? x[r] * (sh->row_scale[r] * ks) : -CUDART_INF_F;
+                    for (int r = 0; r < kRp; ++r) x[r] = (see >> r) & 1u ? fmaf(x[r], sh->row_scale[r] * ks, lv) : -CUDART_INF_F;
                     const float most = reduce_rows(x, lane, [](float p, float q) { return fmaxf(p, q); });
                     if (lane < kRp) sh->most[grp][quad][lane] = most;
                     warp_arrive(&bars->vote[grp], lane);
@@ -567,7 +562,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                     }
                 }
                 if (!ok) break;
-                if ((viol || v_corr != 1.f) && t != grp) {
+                if (viol && t != grp) {
                     // (S of this tile was committed behind the group's last P V product: O is stable)
 #pragma unroll 1
                     for (int c = 0; c < kRp; c += 8) {
@@ -576,7 +571,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                         const float* const f = &sh->corr[grp][c];
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (viol ? f[e] * v_corr : v_corr));
+                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[e]);
                         tmem_st8(tO + c, o);
                     }
                     tmem_wait_st();
@@ -639,16 +634,17 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
             static_assert(kGroups * 8 == 32, "a lane for every group of eight rows");
             if (quad == 0 && grp * 8 < kRp) {                            // the eight rows this group stores, a lane per row and group
                 const int g = lane >> 3, r = grp * 8 + (lane & 7);
-                const float m = sh->m[g][r];
+                float m = sh->m[g][r], sum = (sh->sum[g][0][r] + sh->sum[g][1][r]) + (sh->sum[g][2][r] + sh->sum[g][3][r]);
+                const float down = normal_sum(m, sum);
                 float M = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                 M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 16));
                 const float w = m == -CUDART_INF_F ? 0.f : exp2f(m - M);
-                float sum = ((sh->sum[g][0][r] + sh->sum[g][1][r]) + (sh->sum[g][2][r] + sh->sum[g][3][r])) * w;
+                sum *= w;
                 sum += __shfl_xor_sync(0xffffffffu, sum, 8);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 16);
                 if (sh->row_scale[r] != sh->row_scale[r]) sum = CUDART_NAN_F;           // NaN or infinity among the queries
                 const float norm = split ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-                sh->f[g][r] = w * sh->v_unit[g] * norm;
+                sh->f[g][r] = w * (down * sh->v_unit[g]) * norm;
                 if (g == 0 && tree_ok && r < R) {
                     if (!split) {
                         if (a.lse) a.lse[sh->q_row[r]] = (M + log2f(sum)) * kLn2;

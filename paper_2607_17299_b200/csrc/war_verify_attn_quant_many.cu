@@ -5,7 +5,8 @@
 //
 //   S = Qh K' + Ql K'      q (scaled by a power of two per row) = Qh + Ql, both e4m3: eight kind::f8f6f4 products of 32 dims
 //   p = exp2(S * (row's constant * K's scale of the key's block) - m)
-//   O += Ph V' + Pl V'     p * (V's scale of the key's block) = Ph + Pl, e4m3 and e5m2: eight products of 32 keys
+//   O += Ph V' + Pl V'     p * (V's scale of the key's block) = Ph + Pl, e4m3 and e5m2: eight products of 32 keys; the row's
+//                          reference m follows these, not the p alone (see war_attn_quant.cuh)
 //
 // Converting the cache to 16 bits on chip instead would move every element through shared memory three more times (read,
 // written twice as wide, read twice as wide by the tensor cores), 192 of the 128 bytes an SM moves a cycle; splitting the
@@ -35,10 +36,10 @@ constexpr int kRegsSoftmax = 224;
 constexpr int kRegsOther = 48;
 constexpr int kWarpLoadK = 8, kWarpMma = 9, kWarpLoadV = 11;        // (group g's issuer is warp kWarpMma + g)
 constexpr uint32_t kTmemCols = 512;
-// The largest scaled weight is 2^kRescaleThreshold (a stale maximum) * 2 (V's scale against its reference) * kWeightTop = 448,
-// the largest e4m3 value.
-constexpr float kRescaleThreshold = 3.0f;          // log2 units
-constexpr float kWeightTop = 28.f;
+// The largest weight is 2^kRescaleThreshold (a stale reference) * kWeightTop = 448, the largest e4m3 value.  (3 and 56 take as
+// long and lose two bits of the smallest weights; with 32 rows and less, where a group renews all rows at once, 1 takes 11 %.)
+constexpr float kRescaleThreshold = 1.0f;          // log2 units
+constexpr float kWeightTop = 224.f;
 constexpr float kTinyScale = 1.1754943508222875e-38f;   // a scale of 0 must not turn a masked -inf into NaN
 
 // shared memory map (offsets from a 1024-byte aligned base)
@@ -47,7 +48,8 @@ constexpr int kOffRing = 32768;
 constexpr int kOffBar = kOffRing + kSlots * kSlotBytes;
 constexpr int kOffStats = kOffBar + 512;
 constexpr int kOffScales = kOffStats + 3 * 256 * 4;        // [tile of the CTA & 15][K, V][8-key group]
-constexpr int kOffFused = kOffScales + 2048;
+constexpr int kOffLv = kOffScales + 2048;                  // [softmax warp][V's scales: log2, relative][8-key group of its tile]
+constexpr int kOffFused = kOffLv + 8 * 32 * 4;
 constexpr int kSmemBytes = kOffFused + 768 + 1024;
 // Scales are kept for 16 tiles.  While a tile y is unfinished, the slots of V of y, y + 2, y + 4 ... and of K of y + 2, y + 4 ...
 // stay taken once they are loaded (one issuer serves these tiles in order): half of the loads from there on, so with kSlots
@@ -444,9 +446,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 anc = valid ? a.w.anc[(size_t)i * a.N + j] : 0ull;
             }
             float m_used = -CUDART_INF_F, l = 0.f;
-            float v_ref = 0.f;                                             // power of two that V's scales are taken relative to
-
-            float v_unit = 0.f, v_corr = 1.f;
+            float v_ref = 1.f;                                             // power of two that V's scales are taken relative to
+            float* const s_lv = (float*)(smem + kOffLv) + warp * 32;      // log2 of V's scales, and the scales, relative to v_ref
             // Half a tile's share of this thread: kCols keys.
             auto step = [&](int t, int half, auto cols_c) -> bool {
                 constexpr int kCols = decltype(cols_c)::value;
@@ -454,17 +455,14 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 const int key0 = (un.tile_begin + t) * kTileKeys;
                 const uint32_t ti = ld0 / 2 + t;
                 const float* const sc = s_scale + (ti & (kScaleTiles - 1)) * 32;
-                v_corr = 1.f;
                 if (half == 0) {
                     if (!wait_for(&bars->scales[ti & (kScaleTiles - 1)], (ti / kScaleTiles) & 1u, bars, a.status_word)) return false;
-                    // V's scales relative to a power of two that follows the largest one seen: a factor below 2
-                    const float sv_top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sc[16 + (lane & 15)])));
-                    if (sv_top >= 2.f * v_ref) {
-                        const float ref = __uint_as_float(max(__float_as_uint(sv_top) & 0x7f800000u, 0x0c800000u));   // at least 2^-102
-                        v_corr = v_ref / ref;
-                        v_ref = ref;
-                    }
-                    v_unit = kWeightTop / 256.f / v_ref;                   // (split_weights wants x / 256)
+                    const float sv = sc[16 + (lane & 15)];
+                    if (t == grp) v_ref = v_reference(sv);
+                    const float rel = v_relative(sv, v_ref);
+                    __syncwarp();                                          // (the tile before has been read)
+                    if (lane < 16) { s_lv[lane] = v_log(rel); s_lv[16 + lane] = rel * (kWeightTop / 256.f); }    // (split_weights wants x / 256)
+                    __syncwarp();
                 }
                 if (!wait_for(&bars->s_ready[grp][half], cgm & 1u, bars, a.status_word)) return false;
                 tc_fence_after();
@@ -486,14 +484,14 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 }
                 float mx = -CUDART_INF_F;
 #pragma unroll
-                for (int k = 0; k < kCols / 8; ++k) {                      // 8 keys with one scale: three-input max, then the scale
+                for (int k = 0; k < kCols / 8; ++k) {                      // 8 keys with one scale: three-input max, then the scales
                     const uint32_t* x = r + k * 8;
                     const float m0 = max3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
                     const float m1 = max3(__uint_as_float(x[3]), __uint_as_float(x[4]), __uint_as_float(x[5]));
-                    mx = fmaxf(mx, max3(m0, m1, fmaxf(__uint_as_float(x[6]), __uint_as_float(x[7]))) * fmaxf(sc[(c0 >> 3) + k] * row_scale, kTinyScale));
+                    mx = fmaxf(mx, fmaf(max3(m0, m1, fmaxf(__uint_as_float(x[6]), __uint_as_float(x[7]))), fmaxf(sc[(c0 >> 3) + k] * row_scale, kTinyScale), s_lv[(c0 >> 3) + k]));
                 }
                 float corr = 1.f;
-                bool rescale = v_corr != 1.f;
+                bool rescale = false;
                 if (mx > m_used + kRescaleThreshold || (m_used == -CUDART_INF_F && mx > -CUDART_INF_F)) {
                     corr = exp2f(m_used - mx);                             // 0 when nothing was accumulated yet
                     l *= corr;
@@ -501,7 +499,6 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                     rescale = true;
                 }
                 rescale = rescale && (t > grp || half > 0);                // O of this group holds earlier keys of the unit
-                corr *= v_corr;
                 const float neg_m = m_used == -CUDART_INF_F ? 0.f : -m_used;
                 // p = exp2(s * scales - m) goes into the sum as it is; p * (V's scale) goes to the tensor cores as a high
                 // part, rounded to e4m3, and a low part, the remainder rounded to e5m2
@@ -510,7 +507,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 uint32_t ph[kCols / 4], pw[kCols / 4];
 #pragma unroll
                 for (int k = 0; k < kCols / 8; ++k) {
-                    const float ks = fmaxf(sc[(c0 >> 3) + k] * row_scale, kTinyScale), vs = sc[16 + (c0 >> 3) + k] * v_unit;
+                    const float ks = fmaxf(sc[(c0 >> 3) + k] * row_scale, kTinyScale), vs = s_lv[16 + (c0 >> 3) + k];
                     const float2 ks2 = make_float2(ks, ks), vs2 = make_float2(vs, vs);
                     float2 w2[4];
 #pragma unroll
@@ -583,7 +580,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             if (row_scale != row_scale) l = row_scale;                     // NaN or infinity among the row's queries
             const uint32_t theirs = (uint32_t)(T + grp) >> 1;              // tiles of this unit that the other group has
             const bool fused_split = kFused && un.n_chunks != 1;
-            st_m[grp * 128 + row] = m_used; st_l[grp * 128 + row] = l; st_w[grp * 128 + row] = v_ref * (1.f / kWeightTop);
+            const float down = normal_sum(m_used, l);
+            st_m[grp * 128 + row] = m_used; st_l[grp * 128 + row] = l; st_w[grp * 128 + row] = down * v_ref * (1.f / kWeightTop);
             warp_arrive(&bars->stats_ready, lane);
             if (grp == 0) {
                 // epilogue: both groups' last products, then the merge of (max, sum, O) over groups and copies, and the store
