@@ -632,6 +632,10 @@ def war_target(d_logits: torch.Tensor, d_num_nodes: torch.Tensor, d_ids: Optiona
     every slot into d_target [B, N] (what war_accept takes), the processed logits into d_out where it is given.
     d_mask: int32 words [B, N, ceil(V / 32)], unit stride along the words; expand() shares one mask."""
     f32, i32, i64 = torch.float32, torch.int32, torch.int64
+    if d_ctx is None and not (d_repetition is None and d_presence is None and d_frequency is None):
+        raise ValueError("penalties need d_ctx (an empty tensor where all contexts are empty)")
+    if d_bias_ids is not None and d_bias_val is not None and d_bias_ids.shape != d_bias_val.shape:
+        raise ValueError("d_bias_ids and d_bias_val must be of one length")
     p = _target_params(_layout(d_logits), _layout(d_out), None if d_mask is None else (None, d_mask.shape, d_mask.stride()), d_target.shape,
                        tuple(None if t is None else t.shape for t in (d_ids, d_parent)),
                        tuple(None if t is None else t.shape for t in (d_num_nodes, d_prompt_len, d_repetition, d_presence, d_frequency)),
