@@ -479,7 +479,7 @@ war_status_t war_verify_attn_quant(const void* d_q, const void* d_kpool, const v
  * NULL: 1, 0, 0) contexts and trees are not read and may be NULL; without ids and parent (both or none) paths do not count.
  * Bias lists: d_bias_off int64 [B+1], entries behind each other; all three arrays or none; at most 65 534 entries a request.
  * d_mask: words by strides (request, slot); stride 0 shares a mask.  B <= 65535, N <= 64, V <= 262144.
- * A malformed tree (WAR_ERR_BAD_TREE), or offsets that decrease or hold 2^31 tokens or too many bias entries, or a context
+ * A malformed tree (WAR_ERR_BAD_TREE), or offsets that are negative, decrease or hold 2^31 tokens or too many bias entries, or a context
  * without d_ctx (NULL will do where all contexts are empty; WAR_ERR_INVALID_ARG), give -1 for all of the request's slots and leave its rows of d_out.  One launch, no workspace. */
 typedef struct {
     const int32_t* d_ctx; const int64_t* d_ctx_off; const int32_t* d_prompt_len;

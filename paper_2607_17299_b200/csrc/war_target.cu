@@ -184,7 +184,7 @@ war_target_kernel(const TargetArgs a) {
     if (a.bias_off) { e0 = a.bias_off[b]; e1 = a.bias_off[b + 1]; }
     int bad = 0;
     if (n_in < 0 || n_in > a.N) bad = WAR_ERR_BAD_TREE;
-    if (c1 < c0 || c1 - c0 >= (1ll << 31) || e1 < e0 || e1 - e0 > kMaxBias) bad = WAR_ERR_INVALID_ARG;
+    if (c0 < 0 || c1 < c0 || c1 - c0 >= (1ll << 31) || e0 < 0 || e1 < e0 || e1 - e0 > kMaxBias) bad = WAR_ERR_INVALID_ARG;
     if (c1 > c0 && !a.ctx) bad = WAR_ERR_INVALID_ARG;
     for (int x = tid; x < bit_words + 1; x += kThreads) rare[x] = 0;
     const uint4 zero = make_uint4(0, 0, 0, 0);                            // (W is a multiple of 32)

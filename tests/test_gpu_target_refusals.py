@@ -50,3 +50,14 @@ def test_no_tokens_at_all(war):
     assert code == 0 and war.war_device_status() == 0
     np.testing.assert_array_equal(got, want)
     np.testing.assert_array_equal(c.run(war), want)              # an empty tensor has no address
+
+
+@pytest.mark.parametrize("which", ["d_ctx_off", "d_bias_off"])
+def test_negative_offsets(war, which):
+    c = Case(63, 3, 4, 500, "bf16", mask=None, bias=6)
+    want = c.want()[1]
+    off = (c.off if which == "d_ctx_off" else c.boff).copy()
+    off[0] = -2
+    got = c.run(war, **{which: dev(off)})
+    assert (got[0] == -1).all() and war.war_device_status() == 1
+    np.testing.assert_array_equal(got[1:], want[1:])
