@@ -652,12 +652,17 @@ def war_target(d_logits: torch.Tensor, d_num_nodes: torch.Tensor, d_ids: Optiona
 
 
 @_by_layout
-def _commit_params(ids, tail, table, k_pool, v_pool, k_scale, v_scale) -> CommitQuantParams:
+def _commit_params(ids, per_slot, per_request, tail, table, k_pool, v_pool, k_scale, v_scale) -> CommitQuantParams:
+    if len(ids) != 2 or len(tail) != 2 or len(table) != 2:
+        raise ValueError("d_ids must be [B, N], d_tail [B, P], page_table [B, max_pages]")
     q = CommitQuantParams()
     q.kv_type, q.scale_block = _pool_layout(k_pool, v_pool, k_scale, v_scale)
     p = q.commit
     p.B, p.N = ids
     p.P = tail[1]
+    for shape, want in ((per_slot, (p.B, p.N)), (tail[:1], (p.B,)), (table[:1], (p.B,))) + tuple((x, (p.B,)) for x in per_request):
+        if tuple(shape) != want:
+            raise ValueError(f"expected shape {want}, got {tuple(shape)}")
     p.num_pages, p.Hkv, p.page_size, p.D = k_pool[1]
     p.max_pages_per_req = table[1]
     p.k_strides[:], p.v_strides[:] = k_pool[2], v_pool[2]
@@ -667,8 +672,10 @@ def _commit_params(ids, tail, table, k_pool, v_pool, k_scale, v_scale) -> Commit
 def war_commit_quant(d_ids: torch.Tensor, d_accept_len: torch.Tensor, d_accept_path: torch.Tensor, d_bonus: torch.Tensor,
                      k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page_table: torch.Tensor,
                      d_prefix_len: torch.Tensor, d_tail: torch.Tensor, d_tail_len: torch.Tensor) -> None:
-    """war_commit for a float8_e4m3fn / float8_e5m2 cache; pools and scales are updated in place."""
-    q = _commit_params(d_ids.shape, d_tail.shape, page_table.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
+    """war_commit for a float8_e4m3fn / float8_e5m2 cache; pools and scales are updated in place.  d_ids and d_accept_path [B, N],
+    d_accept_len, d_bonus, d_prefix_len and d_tail_len [B], d_tail [B, P], page_table [B, max_pages]."""
+    q = _commit_params(d_ids.shape, d_accept_path.shape, (d_accept_len.shape, d_bonus.shape, d_prefix_len.shape, d_tail_len.shape), d_tail.shape,
+                       page_table.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
     code = _lib.war_commit_quant(_ptr(d_ids, torch.int32), _ptr(d_accept_len, torch.int32), _ptr(d_accept_path, torch.int32),
                                  _ptr(d_bonus, torch.int32), _address(k_pool), _address(v_pool), _address(k_scale), _address(v_scale),
                                  _ptr(page_table, torch.int32), C.byref(q),

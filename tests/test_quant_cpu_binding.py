@@ -37,3 +37,26 @@ def test_bias_lists_are_of_one_length(war, length):
         war.war_target(**target_args(d_bias_val=torch.zeros(length)))
     with pytest.raises(ValueError, match="CUDA"):
         war.war_target(**target_args())
+
+
+def commit_args(**over):
+    B, N, P = 3, 5, 8
+    pool = lambda: torch.zeros((12, 2, 16, 128), dtype=torch.uint8).view(torch.float8_e4m3fn)
+    one = lambda *shape: torch.zeros(shape, **i32)
+    a = dict(d_ids=one(B, N), d_accept_len=one(B), d_accept_path=one(B, N), d_bonus=one(B), k_pool=pool(), v_pool=pool(),
+             k_scale=torch.ones((12, 2, 1)), v_scale=torch.ones((12, 2, 1)), page_table=one(B, 4), d_prefix_len=one(B), d_tail=one(B, P),
+             d_tail_len=one(B))
+    return {**a, **over}
+
+
+@pytest.mark.parametrize("name,shape", [("d_accept_len", (2,)), ("d_accept_len", (3, 1)), ("d_accept_path", (3, 4)), ("d_accept_path", (2, 5)),
+                                        ("d_accept_path", (15,)), ("d_bonus", (4,)), ("d_prefix_len", (2,)), ("d_tail_len", (2,)),
+                                        ("d_tail", (2, 8)), ("d_tail", (8,)), ("page_table", (2, 4)), ("page_table", (12,)), ("d_ids", (15,))])
+def test_commit_shapes(war, name, shape):
+    with pytest.raises(ValueError, match="expected shape|d_ids must be"):
+        war.war_commit_quant(**commit_args(**{name: torch.zeros(shape, **i32)}))
+
+
+def test_commit_shapes_that_belong_together(war):
+    with pytest.raises(ValueError, match="CUDA"):                # nothing but the device is wrong
+        war.war_commit_quant(**commit_args())
