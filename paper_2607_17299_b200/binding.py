@@ -584,11 +584,36 @@ def new_quant_workspace(params: AttnQuantParams, device) -> torch.Tensor:
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
+@_by_layout
+def _attn_quant_call(q, table, prefix, nodes, parent, out, lse, k_pool, v_pool, k_scale, v_scale, scale, kernel) -> Tuple[bytes, int]:
+    """What attn_quant_params gives for these tensors, as bytes, and the workspace's size; checks that they belong together."""
+    kv, block = _pool_layout(k_pool, v_pool, k_scale, v_scale)
+    if len(q) != 4 or len(table) != 2:
+        raise ValueError("d_q must be [B, N, Hq, D], d_page_table [B, max_pages]")
+    B, N, Hq, D = q
+    num_pages, Hkv, pg, pool_D = k_pool[1]
+    for shape, want in ((table[:1], (B,)), (prefix, (B,)), (nodes, (B,)), (parent, (B, N)), (out, (B, N, Hq, D)), (lse, (B, N, Hq)), ((D,), (pool_D,))):
+        if shape is not None and tuple(shape) != want:
+            raise ValueError(f"expected shape {want}, got {tuple(shape)}")
+    p = AttnQuantParams()
+    a = p.attn
+    a.B, a.N, a.Hq, a.Hkv, a.D, a.page_size, a.max_pages_per_req, a.kernel, a.num_pages, a.scale = B, N, Hq, Hkv, D, pg, table[1], kernel, num_pages, scale
+    a.k_strides[:], a.v_strides[:] = k_pool[2], v_pool[2]
+    p.kv_type, p.scale_block = kv, block
+    return bytes(p), war_verify_attn_quant_workspace_bytes(p)
+
+
 def war_verify_attn_quant(d_q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
                           d_page_table: torch.Tensor, d_prefix_len: torch.Tensor, d_num_nodes: torch.Tensor, d_parent: torch.Tensor,
                           params: AttnQuantParams, d_workspace: torch.Tensor, d_out: torch.Tensor, d_lse: Optional[torch.Tensor]) -> None:
     """war_verify_attn over a float8_e4m3fn / float8_e5m2 cache; params from attn_quant_params for these tensors."""
-    if d_workspace.numel() * d_workspace.element_size() < war_verify_attn_quant_workspace_bytes(params):
+    a = params.attn
+    described, workspace = _attn_quant_call(d_q.shape, d_page_table.shape, d_prefix_len.shape, d_num_nodes.shape, d_parent.shape, d_out.shape,
+                                            None if d_lse is None else d_lse.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale),
+                                            _layout(v_scale), a.scale, a.kernel)
+    if described != bytes(params):
+        raise ValueError("params do not describe these tensors (see attn_quant_params)")
+    if d_workspace.numel() * d_workspace.element_size() < workspace:
         raise ValueError("workspace is smaller than war_verify_attn_quant_workspace_bytes")
     code = _lib.war_verify_attn_quant(_ptr(d_q, torch.bfloat16), _strided(k_pool, 4, torch.float8_e4m3fn, torch.float8_e5m2),
                                       _strided(v_pool, 4, torch.float8_e4m3fn, torch.float8_e5m2), _ptr(k_scale, torch.float32),
