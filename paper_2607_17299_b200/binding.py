@@ -467,6 +467,15 @@ def _address(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+def _stream_of(*tensors: Optional[torch.Tensor]) -> int:
+    """The current stream, for a call whose tensors are all on its device."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"the call runs on the current device, cuda:{device}, but a tensor is on cuda:{t.get_device()}")
+    return _stream()
+
+
 def _is_contiguous(t) -> bool:
     """As Tensor.is_contiguous, of a _layout."""
     step = 1
@@ -558,7 +567,8 @@ def war_rope_store(d_q: Optional[torch.Tensor], d_k: torch.Tensor, d_v: torch.Te
     code = _lib.war_rope_store(_address(d_q), _address(d_k), _address(d_v), _ptr(d_inv_freq, torch.float32), _ptr(page_table, torch.int32),
                                _ptr(d_prefix_len, torch.int32), _ptr(d_num_nodes, torch.int32), _ptr(d_parent, torch.int32), C.byref(p),
                                _address(k_pool), _address(v_pool), _address(k_scale), _address(v_scale), _ptr(d_q_out, torch.bfloat16),
-                               _stream())
+                               _stream_of(d_q, d_k, d_v, d_inv_freq, page_table, d_prefix_len, d_num_nodes, d_parent, k_pool, v_pool,
+                                          k_scale, v_scale, d_q_out))
     _check("war_rope_store", code)
 
 
@@ -619,7 +629,9 @@ def war_verify_attn_quant(d_q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch
                                       _strided(v_pool, 4, torch.float8_e4m3fn, torch.float8_e5m2), _ptr(k_scale, torch.float32),
                                       _ptr(v_scale, torch.float32), _ptr(d_page_table, torch.int32), _ptr(d_prefix_len, torch.int32),
                                       _ptr(d_num_nodes, torch.int32), _ptr(d_parent, torch.int32), C.byref(params), _ptr(d_workspace),
-                                      _ptr(d_out, torch.bfloat16), _ptr(d_lse, torch.float32), _stream())
+                                      _ptr(d_out, torch.bfloat16), _ptr(d_lse, torch.float32),
+                                      _stream_of(d_q, k_pool, v_pool, k_scale, v_scale, d_page_table, d_prefix_len, d_num_nodes, d_parent,
+                                                 d_workspace, d_out, d_lse))
     _check("war_verify_attn_quant", code)
 
 
@@ -672,7 +684,9 @@ def war_target(d_logits: torch.Tensor, d_num_nodes: torch.Tensor, d_ids: Optiona
         inputs.d_bias_off = inputs.d_bias_ids = inputs.d_bias_val = None             # (an empty tensor has no address)
     code = _lib.war_target(_strided(d_logits, 3, torch.bfloat16, f32), _ptr(d_num_nodes, i32), _ptr(d_ids, i32), _ptr(d_parent, i32),
                            C.byref(inputs), C.byref(p), _ptr(d_target, i32),
-                           None if d_out is None else _strided(d_out, 3, torch.bfloat16, f32), _stream())
+                           None if d_out is None else _strided(d_out, 3, torch.bfloat16, f32),
+                           _stream_of(d_logits, d_num_nodes, d_ids, d_parent, d_target, d_ctx, d_ctx_off, d_prompt_len, d_repetition,
+                                      d_presence, d_frequency, d_bias_off, d_bias_ids, d_bias_val, d_mask, d_out))
     _check("war_target", code)
 
 
@@ -704,5 +718,7 @@ def war_commit_quant(d_ids: torch.Tensor, d_accept_len: torch.Tensor, d_accept_p
     code = _lib.war_commit_quant(_ptr(d_ids, torch.int32), _ptr(d_accept_len, torch.int32), _ptr(d_accept_path, torch.int32),
                                  _ptr(d_bonus, torch.int32), _address(k_pool), _address(v_pool), _address(k_scale), _address(v_scale),
                                  _ptr(page_table, torch.int32), C.byref(q),
-                                 _ptr(d_prefix_len, torch.int32), _ptr(d_tail, torch.int32), _ptr(d_tail_len, torch.int32), _stream())
+                                 _ptr(d_prefix_len, torch.int32), _ptr(d_tail, torch.int32), _ptr(d_tail_len, torch.int32),
+                                 _stream_of(d_ids, d_accept_len, d_accept_path, d_bonus, k_pool, v_pool, k_scale, v_scale, page_table,
+                                            d_prefix_len, d_tail, d_tail_len))
     _check("war_commit_quant", code)

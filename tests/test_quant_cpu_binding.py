@@ -101,3 +101,15 @@ def test_attention_params_of_other_tensors(war):
     a["params"].attn.kernel = 2                                  # the caller's own choices stay
     with pytest.raises(ValueError, match="CUDA"):
         war.war_verify_attn_quant(**a)
+
+
+def test_tensors_on_another_device_than_the_current_one(war, monkeypatch):
+    class On:
+        def __init__(self, device):
+            self.get_device = lambda: device
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(war, "_stream", lambda: 77)
+    assert war._stream_of(On(1), None, On(1)) == 77
+    for where in ((On(0),), (On(1), On(0)), (None, On(1), On(2))):
+        with pytest.raises(ValueError, match="current device, cuda:1"):
+            war._stream_of(*where)
