@@ -434,12 +434,12 @@ war_status_t war_rope_frequencies(const war_rope_freq_params_t* params, float* h
 /* ------------------------------------------------------------------------------------------------
  * Verification attention over a cache held in 8 bits: war_verify_attn with K[c,:] = kscale * kcode[c,:] and
  * V[c,:] = vscale * vcode[c,:], the scales those of c's block of scale_block tokens and kv head (see war_rope_store; here they
- * need not be powers of two).  Half the bytes of the bf16 cache, and the codes go to the tensor
- * cores as they are: q and the softmax weights are each split into two 8-bit parts whose products are summed in 32 bits,
- * so no precision of the bf16 queries is lost (elements below 2^-9 of a row's largest are held to 2^-18 of it).  A weight
- * times its V scale, w = p * vscale, is held to 2^-7.8 of itself or, the small ones, to 2^-18.6 of the largest w among the keys that
- * its row sees; scales below 2^-60 count as 2^-60 in that comparison (as they are, down to 2^-120, where a run of 128 keys begins
- * with such), and V scales above 2^125 (2^65 after such keys) count as that.
+ * need not be powers of two).  Half the bytes of the bf16 cache, and the codes go to the tensor cores as they are: q and the
+ * softmax weights are each split into two 8-bit parts whose products are summed in 32 bits,
+ * so no precision of the bf16 queries is lost (elements below 2^-9 of a row's largest are held to 2^-17 of it).  A weight
+ * times its V scale, w = p * vscale, is held to 2^-7.8 of itself or, the small ones, to 2^-18.6 of the largest w among the
+ * keys that its row sees.  V scales below 2^-60 count as 2^-60 in that comparison, and V scales above 2^125 as 2^125 altogether (where
+ * all scales of the first 128 keys that a thread block takes are below 2^-60, these bounds are 2^-120 and 2^65 for its keys).
  * Arguments, masks, outputs, untouched rows, workspace rules and limits as in war_verify_attn, and:
  *   kv_type 1 (e4m3) or 2 (e5m2); scales float32 [num_pages, Hkv, page_size / scale_block], scale_block 8 .. page_size
  *   pools by strides: unit stride along d, the others multiples of 16 bytes, the base on 16 bytes
