@@ -15,8 +15,6 @@ constexpr float kSmallestScale = 7.8886090522101181e-31f;      // 2^-100: its re
 #ifdef __CUDACC__
 namespace quant {
 
-__device__ __forceinline__ float most(int kv) { return kv == kKvE4M3 ? 448.f : 57344.f; }
-
 // The smallest power of two s with a <= most * s, at least kSmallestScale; 0 for a = 0.  a >= 0; infinity counts as the
 // largest finite number.  Both types' largest value is 1.75 * 2^k (k = 8 or 15), so only a's exponent and the comparison
 // of its fraction with 0.75 matter: exact.
