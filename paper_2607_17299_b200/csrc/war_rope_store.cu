@@ -23,6 +23,7 @@
 #include <cuda_bf16.h>
 #include <math.h>
 #include "war_common.cuh"
+#include "war_attn_plan.cuh"
 #include "war_quant.cuh"
 
 namespace {
@@ -31,7 +32,7 @@ constexpr int kMaxSlots = 64;
 constexpr int kThreads = 384;
 constexpr int kWarps = kThreads / 32;
 constexpr int kHeadsPerTask = 8;
-constexpr int kResident = 148 * 2;            // thread blocks that a B200 holds at a time
+constexpr int kResident = 2;                  // thread blocks that an SM holds at a time
 // How a lane's elements are laid out: kSplit (a pair is half the rotation apart), kAdjacent (a pair is two neighbours), both
 // where the rotation covers whole lanes; kOdd takes every other rot_dim, through shared memory.
 constexpr int kSplit = 0, kAdjacent = 1, kOdd = 2;
@@ -447,7 +448,9 @@ extern "C" war_status_t war_rope_store(const void* d_q, const void* d_k, const v
     a.hkv_magic = magic_of(p->Hkv); a.chunks_magic = magic_of(a.chunks);
     const long long tasks = (p->kv_type == kKvBf16 ? 0 : 2ll * p->Hkv * ((p->N + a.block - 2) / a.block + 1)) +
                             (long long)p->N * ((heads + kHeadsPerTask - 1) / kHeadsPerTask);
-    long long parts = kResident / p->B;
+    const int n_sm = war_attn_sm_count();
+    if (n_sm <= 0) return WAR_ERR_CUDA;
+    long long parts = n_sm * kResident / p->B;
     if (parts > (tasks + kWarps - 1) / kWarps) parts = (tasks + kWarps - 1) / kWarps;
     if (parts < 1) parts = 1;
     const int mode = p->rot_dim % 16 != 0 ? kOdd : p->interleaved ? kAdjacent : kSplit;

@@ -23,6 +23,7 @@
 #include <cuda_bf16.h>
 #include <cooperative_groups.h>
 #include "war_common.cuh"
+#include "war_attn_plan.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -578,7 +579,8 @@ extern "C" war_status_t war_target(const void* d_logits, const int32_t* d_num_no
     // Slices of whole mask words, at most eight, at least four segments each (with two, 99
     // requests of 29 slots and 8266 tokens take 106 us, with four 90, with eight 116), so many that the requests fill the GPU (two thread
     // blocks an SM, 1.5 waves of them: 256 requests of 32000 tokens take 90 us with two slices, 106 with three); rows are dealt to more clusters of a request only if that leaves room: each counts the context again.
-    const int resident = 2 * 148;
+    const int n_sm = war_attn_sm_count(), resident = 2 * n_sm;
+    if (n_sm <= 0) return WAR_ERR_CUDA;
     const int most = (p->V + kSegment * 4 - 1) / (kSegment * 4), least = (p->V + kMaxSlice - 1) / kMaxSlice;
     int slices = (resident * 3 / 2 + p->B - 1) / p->B;
     slices = slices > most ? most : slices;
