@@ -6,8 +6,8 @@
 // type's smallest normal number.
 //
 // A step moves a few kilobytes a request, so what counts is the length of the chain page table -> scale -> row -> write
-// and the number of launches (8 requests of up to 16 slots 7.0 us, 256 of up to 32 slots 11.3 us, 6 MB; one launch, where
-// war_commit makes two).  One cluster of thread blocks per request: its warps take one (head, K or V) each, lanes
+// and the number of launches (8 requests of up to 16 slots 7.0 us, 256 of up to 32 slots 11.3 us, 6 MB, the kernel alone; one
+// launch, where war_commit makes two).  One cluster of thread blocks per request: its warps take one (head, K or V) each, lanes
 // hold the scales of the blocks that can be involved (at most ten in a row), sixteen rows are in flight at a time; after a
 // cluster barrier (everybody has read prefix_len) the first block advances the context.
 #include <cooperative_groups.h>

@@ -17,9 +17,9 @@
 // and the request's tasks are dealt over several thread blocks when there are few requests.
 //
 // Measured: 128 requests of 64 slots, 64 + 8 heads, bf16 pool (336 MB): 59 us, 5.7 TB/s (sixteen lanes a row with the partner
-// fetched by shuffle took 93).  256 requests of 8 slots, 32 + 8 heads, e4m3 pool (46 MB): 18.5 us (37 before); there the
-// issue slots are the bound, most of them in the scale blocks, which pass their values twice.  One slot of 8 requests: 4.5 us, the
-// chain of dependent reads.
+// fetched by shuffle took 93).  256 requests of 8 slots, 32 + 8 heads, e4m3 pool (46 MB): 17 to 18.5 us (37 before); no unit is at
+// its limit there (issue slots 54 %, DRAM 13 %, 28 % of the warps resident): a warp's four to six tasks follow each other, each a chain
+// of dependent instructions, and scale blocks pass their values twice.  One slot of 8 requests: 4.6 us, the chain of dependent reads.
 #include <cuda_bf16.h>
 #include <math.h>
 #include "war_common.cuh"

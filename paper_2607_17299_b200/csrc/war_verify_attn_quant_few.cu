@@ -18,10 +18,11 @@
 // A tile is 16 KB of K and 16 KB of V, rows of 128 bytes in the 128-byte swizzle, for either memory order: one tensor map
 // (d, token, head, page) with the pool's own strides, one copy per (page, head).
 //
-// Bound by HBM for 16 rows and fewer (64 requests of about 14000 keys, 8 kv heads, 1.82 GB: 327 us, 5.6 TB/s); for 32 rows the
-// exponentials and conversions of the softmax warps add up to more (420 us, 4.3 TB/s).  Single tokens (8 requests of 4096
-// keys, 67 MB): 30 us, of which planning takes 5 and the merge of split requests 6.  A row per lane, as for more rows, takes
-// 600 us and more for 32 rows; three slots fewer in the ring 10 % more.
+// Measured next to the bf16 kernel on the same keys and GPU (64 requests of 4096 to 32768 keys, 8 kv heads, 2.02 GB of codes): 16
+// rows 368 us (5.5 TB/s, near HBM's bound) against 588, 32 rows 442 to 472 us (4.3 to 4.6 TB/s) against 591.  With 32 rows no unit is
+// at its limit (issue slots 42 %, tensor pipe 12 %, DRAM 47 % over 16 requests): the softmax warps' chain is the longest.
+// Single tokens (8 requests of 4096 keys, 67 MB): 31 us against 34, of which planning takes 5 and the merge of split requests 6.
+// A row per lane, as for more rows, takes 600 us and more for 32 rows; three slots fewer in the ring 10 % more.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -44,7 +45,7 @@ constexpr int kWarpLoadK = kSoftWarps, kWarpMma = kSoftWarps + 1, kWarpLoadV = k
 constexpr uint32_t kTmemCols = 512;
 constexpr int kMaxRows = 32;
 // What a unit costs in the split, times the bf16 kernel's tiles: with 32 rows a boundary takes as long as some fifteen tiles of
-// 32 KB (64 requests of 8 slots 468 -> 447 us, 20 requests 158 -> 152; with 16 rows it made 326 us 332).
+// 32 KB (64 requests of 8 slots 468 -> 447 us when it came in, 20 requests 158 -> 152; with 16 rows it made 326 us 332).
 template <int kRp> constexpr int kUnitCostOf = kRp == 32 ? 3 : 1;
 // The largest weight is 2^kRescaleThreshold (a stale reference) * kWeightTop = 448, the largest e4m3 value.
 constexpr float kRescaleThreshold = 3.0f;          // log2 units

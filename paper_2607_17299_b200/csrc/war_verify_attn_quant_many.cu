@@ -8,9 +8,10 @@
 //   O += Ph V' + Pl V'     p * (V's scale of the key's block) = Ph + Pl, e4m3 and e5m2: eight products of 32 keys; the row's
 //                          reference m follows these, not the p alone (see war_attn_quant.cuh)
 //
-// Converting the cache to 16 bits on chip instead would move every element through shared memory three more times (read,
-// written twice as wide, read twice as wide by the tensor cores), 192 of the 128 bytes an SM moves a cycle; splitting the
-// small operands keeps the tensor work of the bf16 kernel per key (sixteen products of 64 cycles a tile) and its precision.
+// Splitting the small operands keeps the tensor work of the bf16 kernel per key (sixteen products of 64 cycles a tile).  Converting the
+// cache to 16 bits on chip instead would move every element through shared memory three more times (read, written twice as
+// wide, read twice as wide by the tensor cores): 192 KB a tile, 1500 cycles, above the 1400 that HBM needs for a tile but
+// below the 3400 that this kernel takes; it has not been tried here.
 // A tile of 128 keys is 16 KB of K and 16 KB of V, rows of 128 bytes in the 128-byte swizzle, for either memory order: one
 // tensor map (d, token, head, page) with the pool's own strides, one copy per (page, head).  The scales of a tile travel
 // with it, sixteen 4-byte asynchronous copies for K and for V, so that no softmax warp waits for global memory.
@@ -18,9 +19,12 @@
 // A tile is worked on in halves of 64 keys: while a group's softmax warps have one half, P V and the next tile's S of the other
 // are on the tensor cores, so the next S is ready when they come to it (571 us against 598 with whole tiles, same GPU).
 //
-// Measured: 32 requests of 16K to 32K keys, 128 rows per kv head (1.57 GB): 575 us, 2.7 TB/s and 690 TFLOP/s of the two
-// products (each operand in two parts: twice that on the pipe).  Bound by the softmax warps: 11 instructions an element, two
-// warps a scheduler, half of the issue slots used.  TMEM has no room for a third group's S next to two O.  Sixteen softmax
+// Measured next to the bf16 kernel on the same keys and GPU: this one is the slower one, with half the bytes.  32 requests of 16K to
+// 32K keys, 128 rows per kv head (1.60 GB): 577 us against 499; 64 requests, 64 rows (2.02 GB): 624 against 594; 4 requests of up to
+// 131072 keys, 96 rows, e5m2 (0.40 GB): 197 against 156; 128 requests, 512 rows in four row blocks (1.19 GB): 1980 against 1310.
+// 577 us are 2.8 TB/s and 700 TFLOP/s of the two products (each operand in two parts: twice that on the pipe).  Bound by the
+// softmax warps: 11 instructions an element, two warps a scheduler, 47 % of the issue slots and 30 % of the tensor pipe used (8
+// requests).  TMEM has no room for a third group's S next to two O.  Sixteen softmax
 // warps, two threads a row, were slower in lockstep (754 us) and with the reference handed from half to half (639 us): what
 // they gain in overlap they lose in instructions for agreeing on it and in registers.
 #include <mutex>
