@@ -33,6 +33,9 @@ constexpr float kLeastLv = -85.f;
 constexpr float kVRefLarge = 33554432.f, kVRefSmall = 2.9103830456733704e-11f;
 __device__ __forceinline__ float v_relative(float scale, float v_ref) { return fminf(scale, v_ref * 0x1p100f) * (1.f / v_ref); }
 __device__ __forceinline__ float v_log(float relative) { return fmaxf(__log2f(relative), kLeastLv); }
+// A sum whose reference grows by 2^d, given 2^(-d / 2): d may be 185 (from the least lv to the most), where 2^-d is no 32-bit number
+// any more but the sum of p up to 2^88 times that is.
+__device__ __forceinline__ float half_step(float sum, float root) { return sum * root * root; }
 // A group's (reference, sum) with the sum between 1 and 2: such references are logarithms of sums and can be compared between
 // groups and parts, whatever scales they were worked out with.  Returns the power of two that the sum was multiplied by.
 __device__ __forceinline__ float normal_sum(float& m, float& sum) {

@@ -111,10 +111,10 @@ attn_quant_simple_kernel(const __nv_bfloat16* __restrict__ q, const AttnQuantPoo
                 }
                 if (tmax == -CUDART_INF_F) continue;
                 const float m_new = fmaxf(m, tmax);
-                const float corr = exp2f(m - m_new);
-                l *= corr;
+                const float corr = exp2f(0.5f * (m - m_new));
+                l = half_step(l, corr);
 #pragma unroll
-                for (int d = 0; d < 128; ++d) acc[d] *= corr;
+                for (int d = 0; d < 128; ++d) acc[d] = half_step(acc[d], corr);
                 m = m_new;
 #pragma unroll
                 for (int kk = 0; kk < kSub; ++kk) {

@@ -551,7 +551,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                         const float old = sh->m[grp][r], now = fmaxf(o + kMargin, old);
                         sh->m[grp][r] = now;
                         sh->neg_m[grp][r] = now == -CUDART_INF_F ? kNoMax : -now;
-                        sh->corr[grp][r] = now == old ? 1.f : exp2f(old - now);             // 0 when nothing was accumulated yet
+                        sh->corr[grp][r] = now == old ? 1.f : exp2f(0.5f * (old - now));    // 0 when nothing was accumulated yet; see half_step
                     }
                     warp_arrive(&bars->vote[grp], lane);
                     ok = wait_for(&bars->vote[grp], votes++ & 1u, bars, a.status_word);
@@ -559,7 +559,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
 #pragma unroll
                     for (int r = 0; r < kRp; r += 4) {
                         const float4 c4 = *reinterpret_cast<const float4*>(&sh->corr[grp][r]);
-                        l[r] *= c4.x; l[r + 1] *= c4.y; l[r + 2] *= c4.z; l[r + 3] *= c4.w;
+                        l[r] = half_step(l[r], c4.x); l[r + 1] = half_step(l[r + 1], c4.y); l[r + 2] = half_step(l[r + 2], c4.z); l[r + 3] = half_step(l[r + 3], c4.w);
                     }
                 }
                 if (!ok) break;
@@ -572,7 +572,7 @@ attn_quant_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                         const float* const f = &sh->corr[grp][c];
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[e]);
+                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(half_step(__uint_as_float(o[e]), f[e]));
                         tmem_st8(tO + c, o);
                     }
                     tmem_wait_st();

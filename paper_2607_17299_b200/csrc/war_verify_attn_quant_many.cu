@@ -497,8 +497,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 float corr = 1.f;
                 bool rescale = false;
                 if (mx > m_used + kRescaleThreshold || (m_used == -CUDART_INF_F && mx > -CUDART_INF_F)) {
-                    corr = exp2f(m_used - mx);                             // 0 when nothing was accumulated yet
-                    l *= corr;
+                    corr = exp2f(0.5f * (m_used - mx));                    // 0 when nothing was accumulated yet; see half_step
+                    l = half_step(l, corr);
                     m_used = mx;
                     rescale = true;
                 }
@@ -537,7 +537,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                         tmem_ld16(tO + c * 16, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(half_step(__uint_as_float(o[e]), f));
                         tmem_st16(tO + c * 16, o);
                     }
                 }

@@ -165,3 +165,19 @@ def test_scales_from_tiny_to_huge(war, N, low, high):
     place(c)
     for kernel in (1, 0, 2):
         check(c, *c.run(war, kernel), whole=False)
+
+
+@pytest.mark.parametrize("N", ROWS)
+@pytest.mark.parametrize("first,rest", [(-90, -8), (-110, 60), (-61, -59)])
+@pytest.mark.parametrize("prefix", [700, 9000])
+def test_contexts_that_begin_with_tiny_scales(war, N, first, rest, prefix):
+    """The first 200 keys have small scales, the others large ones: some tiles begin a group's or a thread block's share with scales below
+    2^-60, others do not, and the parts meet."""
+    c = Case(57, "e4m3", [prefix], N, 4, 1, 16, 8, dirty=False, full=True)
+    dots = np.random.default_rng(58).standard_normal(prefix + N)
+    set_keys(c, dots)
+    c.sv[:] = 2.0 ** rest
+    scales_at(c, range(0, 200, 8), 2.0 ** first, 8)
+    place(c)
+    for kernel in (1, 0, 2):
+        check(c, *c.run(war, kernel))
