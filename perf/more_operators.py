@@ -466,7 +466,7 @@ def _compact_own(s, war):
     pages = _buffers(s, war)
     if "ws" not in s:
         s["ws"] = war.new_compact_workspace(pages)
-    war.war_pages_compact(pages, s["ws"], s["copies"], s["n_copies"], s["word"])
+    war.war_pages_compact(pages, s["case"]["page"], s["ws"], s["copies"], s["n_copies"], s["word"])
     war.war_pages_copy(s["copies"], s["n_copies"], s["k_pool"], s["v_pool"], s["k_scale"], s["v_scale"])
     return s["word"], s["n_copies"]
 
