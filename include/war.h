@@ -20,6 +20,10 @@
  *   war_verify_attn_quant                war_verify_attn over a cache held in 8 bits with a scale per block and head
  *   war_target                           penalties, biases and grammar masks on the logits: the tokens war_accept compares with
  *   war_commit_quant                     war_commit for the 8-bit cache
+ *   war_pages_grow / _fork / _free       pages for the next step, requests that become copies of others, finished requests
+ *   war_pages_compact / _copy            used pages to the front of the pool; the copies that fork and compaction ask for
+ *   war_prefix_groups                    which requests share how much of their prefix
+ *   war_verify_attn_shared(_quant)       war_verify_attn(_quant) with the shared prefix of a group computed once for all members
  *
  * Conventions shared by every call
  *   - Pointers named d_* are DEVICE pointers, h_* are HOST pointers.  The caller owns every buffer it
@@ -509,6 +513,92 @@ war_status_t war_commit_quant(const int32_t* d_ids, const int32_t* d_accept_len,
                               const int32_t* d_bonus, void* d_kpool, void* d_vpool, float* d_kscale, float* d_vscale,
                               const int32_t* d_page_table, const war_commit_quant_params_t* params, int32_t* d_prefix_len,
                               int32_t* d_tail, int32_t* d_tail_len, war_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Pages.  Synchronous rollouts run every prompt several times (paper Section 5.3 reports rollouts of four and eight), so requests share
+ * cache pages; the calls above leave it to the caller who holds which.  These calls keep the books of one pool, all in device memory:
+ *   d_refs [num_pages]        table entries that hold the page
+ *   d_free [ceil(num_pages / 32)]   bit page % 32 of word page / 32 is set iff refs is 0 (no bits behind the last page)
+ *   d_page_table [B, max_pages_per_req], d_held [B]   the first held[b] entries of row b are in use
+ * A new pool has refs and held 0 and all bits of its pages set.  The pages of all layers go by one table: a list of copies
+ * int32 [n, 3] = (from, to, rows) is given to war_pages_copy once per layer.  Results do not depend on timing: pages are given
+ * out from the lowest free one up, to the requests in order.  B <= 4096, num_pages <= 2^30.  One launch each; nothing is allocated.
+ * Books that contradict themselves (a page outside the pool, more entries than refs counts, held outside [0, max_pages_per_req]) record
+ * WAR_ERR_BAD_PAGE; such entries are left out.
+ *
+ * war_pages_grow: room for the next step.  A running request (d_tail_len NULL, or tail_len[b] >= 0) gets pages for positions below
+ *   prefix_len[b] + N.  It is served iff the pool has all pages wanted by the requests up to and with it.
+ *   granted[b] = 1: it has its room (also where it needed nothing); 0: it is not running or nothing was changed for it.  A request whose
+ *   room is beyond max_pages_per_req is not served and records WAR_ERR_BAD_PAGE.
+ * war_pages_fork: request b with src[b] = s >= 0, s != b, becomes a copy of request s as it was before the call; others (src[b] = -1 or b)
+ *   stay.  All copies are made at once, so requests may swap.  Its prefix_len, tail window and tail_len are those of s (see war_commit); the
+ *   full pages of the prefix are shared; the page that is partly filled (prefix_len % page_size rows) becomes a fresh one and a line of
+ *   d_copies, except that the lowest request that takes an s which is itself replaced gets s's page, if nobody else holds it.
+ *   What b held before is given back; entries behind the new ones are -1; pages of s behind its prefix (its tree's) are not shared:
+ *   war_pages_grow follows.  d_copies has room for B lines, in the order of the requests; d_n_copies int32.  *d_ok = 1; or 0 and nothing is changed
+ *   where the pool has too few free pages (those given back by the call itself do not count).  A source that is not running, is
+ *   no request or holds fewer pages than its prefix: WAR_ERR_INVALID_ARG, and b stays as it is.
+ * war_pages_free: requests with done[b] != 0 give their pages back (shared ones stay with their other holders): held = 0, their entries -1,
+ *   tail_len = -1 where d_tail_len is given.
+ * war_pages_compact: the i-th highest used page moves to the i-th lowest free one while it lies above it, at most max_copies of them (the
+ *   highest first, so that calls can share the work); tables, refs and bits follow, d_copies lists the moves (whole pages) in this order.
+ *   *d_top: no page at or above it is in use.  d_workspace: war_pages_compact_workspace_bytes(num_pages), 4-byte aligned, any contents.
+ * war_pages_copy: rows [0, rows) of page `from` to page `to` for every line, K and V, all heads, and the scales of the blocks that hold
+ *   them.  A page that is written stands on one line only.  *d_n_copies lines, at most max_copies.  Pools by strides: unit stride
+ *   along d, the others multiples of 16 bytes.  Bad page ids are skipped (WAR_ERR_BAD_PAGE).
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t* d_refs; uint32_t* d_free; int32_t* d_page_table; int32_t* d_held;
+    int32_t B, page_size, max_pages_per_req, reserved;
+    int64_t num_pages;
+} war_pages_t;
+war_status_t war_pages_grow(const war_pages_t* pages, int32_t N, const int32_t* d_prefix_len, const int32_t* d_tail_len,
+                            int32_t* d_granted, war_stream_t stream);
+war_status_t war_pages_fork(const war_pages_t* pages, const int32_t* d_src, int32_t P, int32_t* d_prefix_len, int32_t* d_tail,
+                            int32_t* d_tail_len, int32_t* d_copies, int32_t* d_n_copies, int32_t* d_ok, war_stream_t stream);
+war_status_t war_pages_free(const war_pages_t* pages, const int32_t* d_done, int32_t* d_tail_len, war_stream_t stream);
+size_t war_pages_compact_workspace_bytes(int64_t num_pages);
+war_status_t war_pages_compact(const war_pages_t* pages, void* d_workspace, int32_t max_copies, int32_t* d_copies, int32_t* d_n_copies,
+                               int32_t* d_top, war_stream_t stream);
+typedef struct {
+    int32_t Hkv, D, page_size, kv_type, scale_block, reserved;          /* scale_block is ignored for bf16 */
+    int64_t num_pages;
+    int64_t kpool_strides[4], vpool_strides[4];                         /* [page, head, token, d] in elements */
+} war_pages_copy_params_t;
+war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d_n_copies, int32_t max_copies, void* d_kpool, void* d_vpool,
+                            float* d_kscale, float* d_vscale, const war_pages_copy_params_t* params, war_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Shared prefixes.
+ * war_prefix_groups: which running requests (d_tail_len NULL, or tail_len >= 0) share their prefix, read off the page tables.  Requests
+ * whose prefixes have the same full page at position min_shared - 1 are a group: leader[b] = the lowest of them, shared_len[b] =
+ * page_size times the number of leading full pages that all of them have in common with the leader.  min_shared lies behind what all requests share
+ * anyway (a system prompt), if that is no group worth making.  A request without such a page, alone with it, or of a group that has
+ * less than min_shared in common: leader[b] = b, shared_len[b] = 0.  Changes only when pages do (fork, grow, free, compaction).
+ *
+ * war_verify_attn_shared, war_verify_attn_shared_quant: war_verify_attn and war_verify_attn_quant, arguments, results, untouched
+ * rows and workspace rules as there, for requests in groups.  leader[b] names the group (leader[leader[b]] must be itself);
+ * shared_len[leader] says how many leading tokens its members share (rounded down to whole pages; at most any member's prefix_len): their K and
+ * V are read once, through the table of the group's lowest request with num_nodes > 0, and multiplied with the queries of all members.
+ * Requests with num_nodes = 0 do not count as members, and a group with one member is a request for itself, whatever its shared_len.
+ * A member whose leader or shared_len breaks these rules records WAR_ERR_INVALID_ARG and its rows are left as they are.
+ * kernel must be 0; B * N * Hq < 2^29.  Three launches.  Pages of the shared prefix are taken from one table: tables that differ there
+ * give the results of that one.
+ * ------------------------------------------------------------------------------------------------ */
+war_status_t war_prefix_groups(const int32_t* d_page_table, const int32_t* d_prefix_len, const int32_t* d_tail_len, int32_t B,
+                               int32_t page_size, int32_t max_pages_per_req, int32_t min_shared, int32_t* d_leader, int32_t* d_shared_len,
+                               war_stream_t stream);
+size_t war_verify_attn_shared_workspace_bytes(const war_attn_params_t* params);
+war_status_t war_verify_attn_shared(const void* d_q, const void* d_kpool, const void* d_vpool, const int32_t* d_page_table,
+                                    const int32_t* d_prefix_len, const int32_t* d_num_nodes, const int32_t* d_parent,
+                                    const int32_t* d_leader, const int32_t* d_shared_len, const war_attn_params_t* params,
+                                    void* d_workspace, void* d_out, float* d_lse, war_stream_t stream);
+size_t war_verify_attn_shared_quant_workspace_bytes(const war_attn_quant_params_t* params);
+war_status_t war_verify_attn_shared_quant(const void* d_q, const void* d_kpool, const void* d_vpool, const float* d_kscale,
+                                          const float* d_vscale, const int32_t* d_page_table, const int32_t* d_prefix_len,
+                                          const int32_t* d_num_nodes, const int32_t* d_parent, const int32_t* d_leader,
+                                          const int32_t* d_shared_len, const war_attn_quant_params_t* params, void* d_workspace,
+                                          void* d_out, float* d_lse, war_stream_t stream);
 
 /* Diagnostic, no counterpart in the paper: exercises the bounded waits of the attention kernel without the kernel.
  * Every wait inside the tensor-core kernel (on a tile that has not arrived, on a result that is not ready) gives up

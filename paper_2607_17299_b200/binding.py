@@ -10,7 +10,7 @@ import ctypes as C
 import functools
 import math
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
 import torch
@@ -31,7 +31,9 @@ EXPORTS = ["war_index_build", "war_index_append", "war_index_append_async", "war
            "war_index_import", "war_index_info", "war_index_destroy", "war_draft", "war_draft_scored_workspace_bytes", "war_draft_scored", "war_draft_local", "war_draft_pick",
            "war_verify_attn_workspace_bytes", "war_verify_attn", "war_verify_attn_noalloc", "war_accept", "war_commit", "war_device_status",
            "war_rope_store", "war_rope_frequencies", "war_verify_attn_quant_workspace_bytes", "war_verify_attn_quant", "war_target",
-           "war_commit_quant",
+           "war_commit_quant", "war_pages_grow", "war_pages_fork", "war_pages_free", "war_pages_compact_workspace_bytes", "war_pages_compact",
+           "war_pages_copy", "war_prefix_groups", "war_verify_attn_shared_workspace_bytes", "war_verify_attn_shared",
+           "war_verify_attn_shared_quant_workspace_bytes", "war_verify_attn_shared_quant",
            "war_selftest_bounded_wait",
            "war_status_string"]
 
@@ -722,3 +724,262 @@ def war_commit_quant(d_ids: torch.Tensor, d_accept_len: torch.Tensor, d_accept_p
                                  _stream_of(d_ids, d_accept_len, d_accept_path, d_bonus, k_pool, v_pool, k_scale, v_scale, page_table,
                                             d_prefix_len, d_tail, d_tail_len))
     _check("war_commit_quant", code)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# pages and shared prefixes
+# ---------------------------------------------------------------------------------------------------------------
+class Pages(NamedTuple):
+    """The books of a paged cache, int32 CUDA tensors (see include/war.h): refs [num_pages], free [ceil(num_pages / 32)] (bits),
+    page_table [B, max_pages], held [B].  new_pages makes those of an empty pool."""
+    refs: torch.Tensor
+    free: torch.Tensor
+    page_table: torch.Tensor
+    held: torch.Tensor
+
+
+class PagesBooks(C.Structure):
+    _fields_ = [("d_refs", C.c_void_p), ("d_free", C.c_void_p), ("d_page_table", C.c_void_p), ("d_held", C.c_void_p), ("B", C.c_int32),
+                ("page_size", C.c_int32), ("max_pages_per_req", C.c_int32), ("reserved", C.c_int32), ("num_pages", C.c_int64)]
+
+
+class PagesCopyParams(C.Structure):
+    _fields_ = [("Hkv", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32), ("kv_type", C.c_int32), ("scale_block", C.c_int32),
+                ("reserved", C.c_int32), ("num_pages", C.c_int64), ("kpool_strides", C.c_int64 * 4), ("vpool_strides", C.c_int64 * 4)]
+
+
+_lib.war_pages_grow.restype = C.c_int
+_lib.war_pages_grow.argtypes = [C.POINTER(PagesBooks), C.c_int32] + [C.c_void_p] * 4
+_lib.war_pages_fork.restype = C.c_int
+_lib.war_pages_fork.argtypes = [C.POINTER(PagesBooks), C.c_void_p, C.c_int32] + [C.c_void_p] * 7
+_lib.war_pages_free.restype = C.c_int
+_lib.war_pages_free.argtypes = [C.POINTER(PagesBooks)] + [C.c_void_p] * 3
+_lib.war_pages_compact_workspace_bytes.restype = C.c_size_t
+_lib.war_pages_compact_workspace_bytes.argtypes = [C.c_int64]
+_lib.war_pages_compact.restype = C.c_int
+_lib.war_pages_compact.argtypes = [C.POINTER(PagesBooks), C.c_void_p, C.c_int32] + [C.c_void_p] * 4
+_lib.war_pages_copy.restype = C.c_int
+_lib.war_pages_copy.argtypes = [C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 4 + [C.POINTER(PagesCopyParams), C.c_void_p]
+_lib.war_prefix_groups.restype = C.c_int
+_lib.war_prefix_groups.argtypes = [C.c_void_p] * 3 + [C.c_int32] * 4 + [C.c_void_p] * 3
+_lib.war_verify_attn_shared_workspace_bytes.restype = C.c_size_t
+_lib.war_verify_attn_shared_workspace_bytes.argtypes = [C.POINTER(AttnParams)]
+_lib.war_verify_attn_shared.restype = C.c_int
+_lib.war_verify_attn_shared.argtypes = [C.c_void_p] * 9 + [C.POINTER(AttnParams)] + [C.c_void_p] * 4
+_lib.war_verify_attn_shared_quant_workspace_bytes.restype = C.c_size_t
+_lib.war_verify_attn_shared_quant_workspace_bytes.argtypes = [C.POINTER(AttnQuantParams)]
+_lib.war_verify_attn_shared_quant.restype = C.c_int
+_lib.war_verify_attn_shared_quant.argtypes = [C.c_void_p] * 11 + [C.POINTER(AttnQuantParams)] + [C.c_void_p] * 4
+
+
+def new_pages(num_pages: int, B: int, max_pages: int, device) -> Pages:
+    """The books of an empty pool for B requests of at most max_pages pages."""
+    free = np.zeros(-(-num_pages // 32) * 32, np.uint8)
+    free[:num_pages] = 1
+    words = torch.from_numpy(np.packbits(free, bitorder="little").view(np.int32))
+    zeros = functools.partial(torch.zeros, dtype=torch.int32, device=device)
+    return Pages(zeros(num_pages), words.to(device), torch.full((B, max_pages), -1, dtype=torch.int32, device=device), zeros(B))
+
+
+@_by_layout
+def _pages_shapes(refs, free, table, held) -> Tuple[int, int, int]:
+    if len(refs) != 1 or len(table) != 2 or tuple(held) != (table[0],) or tuple(free) != (-(-refs[0] // 32),):
+        raise ValueError("pages must be refs [num_pages], free [ceil(num_pages / 32)], page_table [B, max_pages], held [B]")
+    return table[0], table[1], refs[0]
+
+
+def _books(pages: Pages, page_size: int) -> PagesBooks:
+    refs, free, table, held = pages
+    B, width, num_pages = _pages_shapes(refs.shape, free.shape, table.shape, held.shape)
+    i32 = torch.int32
+    return PagesBooks(_ptr(refs, i32), _ptr(free, i32), _ptr(table, i32), _ptr(held, i32), B, page_size, width, 0, num_pages)
+
+
+def _same_shape(want, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.shape != want:
+            raise ValueError(f"expected shape {tuple(want)}, got {tuple(t.shape)}")
+
+
+def _copy_list(d_copies: torch.Tensor, least: int) -> int:
+    if d_copies.dim() != 2 or d_copies.shape[1] != 3 or d_copies.shape[0] < least:
+        raise ValueError(f"d_copies must be int32 [n, 3] with n >= {least}")
+    return d_copies.shape[0]
+
+
+def war_pages_grow(pages: Pages, N: int, page_size: int, d_prefix_len: torch.Tensor, d_tail_len: Optional[torch.Tensor],
+                   d_granted: torch.Tensor) -> None:
+    """Pages for positions below prefix_len + N of every running request; d_granted [B]: 1 where a request has its room."""
+    i32 = torch.int32
+    books = _books(pages, page_size)
+    _same_shape(pages.held.shape, d_prefix_len, d_tail_len, d_granted)
+    code = _lib.war_pages_grow(C.byref(books), N, _ptr(d_prefix_len, i32), _ptr(d_tail_len, i32), _ptr(d_granted, i32),
+                               _stream_of(*pages, d_prefix_len, d_tail_len, d_granted))
+    _check("war_pages_grow", code)
+
+
+def war_pages_fork(pages: Pages, d_src: torch.Tensor, page_size: int, d_prefix_len: torch.Tensor, d_tail: torch.Tensor,
+                   d_tail_len: torch.Tensor, d_copies: torch.Tensor, d_n_copies: torch.Tensor, d_ok: torch.Tensor) -> None:
+    """Request b becomes a copy of request d_src[b] (-1 or b: stays); d_copies int32 [>= B, 3] and d_n_copies [1] for
+    war_pages_copy, once per layer; d_ok [1]: 0 where the pool had too few pages and nothing was changed."""
+    i32 = torch.int32
+    books = _books(pages, page_size)
+    _same_shape(pages.held.shape, d_src, d_prefix_len, d_tail_len)
+    if d_tail.dim() != 2 or d_tail.shape[0] != pages.held.shape[0] or d_n_copies.numel() != 1 or d_ok.numel() != 1:
+        raise ValueError("d_tail must be [B, P], d_n_copies and d_ok one number each")
+    _copy_list(d_copies, pages.held.shape[0])
+    code = _lib.war_pages_fork(C.byref(books), _ptr(d_src, i32), d_tail.shape[1], _ptr(d_prefix_len, i32), _ptr(d_tail, i32),
+                               _ptr(d_tail_len, i32), _ptr(d_copies, i32), _ptr(d_n_copies, i32), _ptr(d_ok, i32),
+                               _stream_of(*pages, d_src, d_prefix_len, d_tail, d_tail_len, d_copies, d_n_copies, d_ok))
+    _check("war_pages_fork", code)
+
+
+def war_pages_free(pages: Pages, d_done: torch.Tensor, d_tail_len: Optional[torch.Tensor] = None) -> None:
+    """Requests with d_done[b] != 0 give their pages back and, where d_tail_len is given, stop running (tail_len = -1)."""
+    i32 = torch.int32
+    books = _books(pages, 1)
+    _same_shape(pages.held.shape, d_done, d_tail_len)
+    _check("war_pages_free", _lib.war_pages_free(C.byref(books), _ptr(d_done, i32), _ptr(d_tail_len, i32),
+                                                 _stream_of(*pages, d_done, d_tail_len)))
+
+
+def new_compact_workspace(pages: Pages) -> torch.Tensor:
+    n = int(_lib.war_pages_compact_workspace_bytes(pages.refs.numel()))
+    if n == 0:
+        raise WarError("war_pages_compact_workspace_bytes", 6)
+    return torch.empty(n, dtype=torch.uint8, device=pages.refs.device)
+
+
+def war_pages_compact(pages: Pages, page_size: int, d_workspace: torch.Tensor, d_copies: torch.Tensor, d_n_copies: torch.Tensor,
+                      d_top: torch.Tensor) -> None:
+    """Moves used pages to the front of the pool, as many as d_copies int32 [n, 3] has lines for; d_n_copies [1], and d_top [1]: no
+    page at or above it is in use.  Workspace from new_compact_workspace."""
+    i32 = torch.int32
+    books = _books(pages, page_size)
+    if d_workspace.numel() * d_workspace.element_size() < _lib.war_pages_compact_workspace_bytes(pages.refs.numel()):
+        raise ValueError("workspace is smaller than war_pages_compact_workspace_bytes")
+    if d_n_copies.numel() != 1 or d_top.numel() != 1:
+        raise ValueError("d_n_copies and d_top are one number each")
+    code = _lib.war_pages_compact(C.byref(books), _ptr(d_workspace), _copy_list(d_copies, 0), _ptr(d_copies, i32), _ptr(d_n_copies, i32),
+                                  _ptr(d_top, i32), _stream_of(*pages, d_workspace, d_copies, d_n_copies, d_top))
+    _check("war_pages_compact", code)
+
+
+@_by_layout
+def _copy_params(k_pool, v_pool, k_scale, v_scale) -> PagesCopyParams:
+    q = PagesCopyParams()
+    q.kv_type, q.scale_block = _pool_layout(k_pool, v_pool, k_scale, v_scale)
+    q.num_pages, q.Hkv, q.page_size, q.D = k_pool[1]
+    q.kpool_strides[:], q.vpool_strides[:] = k_pool[2], v_pool[2]
+    return q
+
+
+def war_pages_copy(d_copies: torch.Tensor, d_n_copies: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
+                   k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None) -> None:
+    """Applies a list of copies (war_pages_fork, war_pages_compact) to one layer's cache: bf16, or 8-bit with its scales."""
+    q = _copy_params(_layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
+    code = _lib.war_pages_copy(_ptr(d_copies, torch.int32), _ptr(d_n_copies, torch.int32), _copy_list(d_copies, 0), _address(k_pool),
+                               _address(v_pool), _address(k_scale), _address(v_scale), C.byref(q),
+                               _stream_of(d_copies, d_n_copies, k_pool, v_pool, k_scale, v_scale))
+    _check("war_pages_copy", code)
+
+
+def war_prefix_groups(d_page_table: torch.Tensor, d_prefix_len: torch.Tensor, d_tail_len: Optional[torch.Tensor], page_size: int,
+                      min_shared: int, d_leader: torch.Tensor, d_shared_len: torch.Tensor) -> None:
+    """Groups of running requests that share at least min_shared tokens of their prefix: d_leader [B], d_shared_len [B]."""
+    i32 = torch.int32
+    if d_page_table.dim() != 2:
+        raise ValueError("d_page_table must be [B, max_pages]")
+    _same_shape(d_page_table.shape[:1], d_prefix_len, d_tail_len, d_leader, d_shared_len)
+    code = _lib.war_prefix_groups(_ptr(d_page_table, i32), _ptr(d_prefix_len, i32), _ptr(d_tail_len, i32), d_page_table.shape[0], page_size,
+                                  d_page_table.shape[1], min_shared, _ptr(d_leader, i32), _ptr(d_shared_len, i32),
+                                  _stream_of(d_page_table, d_prefix_len, d_tail_len, d_leader, d_shared_len))
+    _check("war_prefix_groups", code)
+
+
+def war_verify_attn_shared_workspace_bytes(params: AttnParams) -> int:
+    return int(_lib.war_verify_attn_shared_workspace_bytes(C.byref(params)))
+
+
+def war_verify_attn_shared_quant_workspace_bytes(params: AttnQuantParams) -> int:
+    return int(_lib.war_verify_attn_shared_quant_workspace_bytes(C.byref(params)))
+
+
+def new_shared_workspace(params: AttnParams, device) -> torch.Tensor:
+    """A device buffer of the size war_verify_attn_shared asks for."""
+    n = war_verify_attn_shared_workspace_bytes(params)
+    if n == 0:
+        raise WarError("war_verify_attn_shared_workspace_bytes", 6)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def new_shared_quant_workspace(params: AttnQuantParams, device) -> torch.Tensor:
+    """A device buffer of the size war_verify_attn_shared_quant asks for."""
+    n = war_verify_attn_shared_quant_workspace_bytes(params)
+    if n == 0:
+        raise WarError("war_verify_attn_shared_quant_workspace_bytes", 6)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+@_by_layout
+def _attn_shared_call(q, table, prefix, nodes, parent, leader, shared, out, lse, k_pool, v_pool, k_scale, v_scale, scale, kernel) -> Tuple[bytes, int]:
+    """The parameter structure for these tensors, as bytes, and the workspace's size; checks that they belong together."""
+    kv, block = _pool_layout(k_pool, v_pool, k_scale, v_scale)
+    if len(q) != 4 or len(table) != 2:
+        raise ValueError("d_q must be [B, N, Hq, D], d_page_table [B, max_pages]")
+    B, N, Hq, D = q
+    num_pages, Hkv, pg, pool_D = k_pool[1]
+    for shape, want in ((table[:1], (B,)), (prefix, (B,)), (nodes, (B,)), (leader, (B,)), (shared, (B,)), (parent, (B, N)), (out, (B, N, Hq, D)),
+                        (lse, (B, N, Hq)), ((D,), (pool_D,))):
+        if shape is not None and tuple(shape) != want:
+            raise ValueError(f"expected shape {want}, got {tuple(shape)}")
+    p = AttnParams() if kv == 0 else AttnQuantParams()
+    a = p if kv == 0 else p.attn
+    a.B, a.N, a.Hq, a.Hkv, a.D, a.page_size, a.max_pages_per_req, a.kernel, a.num_pages, a.scale = B, N, Hq, Hkv, D, pg, table[1], kernel, num_pages, scale
+    a.k_strides[:], a.v_strides[:] = k_pool[2], v_pool[2]
+    if kv == 0:
+        return bytes(p), war_verify_attn_shared_workspace_bytes(p)
+    p.kv_type, p.scale_block = kv, block
+    return bytes(p), war_verify_attn_shared_quant_workspace_bytes(p)
+
+
+def _attn_shared(fn: str, tensors, pools, params, attn: AttnParams, d_workspace, d_out, d_lse) -> None:
+    d_q, table, prefix, nodes, parent, leader, shared = tensors
+    k_pool, v_pool, k_scale, v_scale = pools
+    i32 = torch.int32
+    described, workspace = _attn_shared_call(d_q.shape, table.shape, prefix.shape, nodes.shape, parent.shape, leader.shape, shared.shape, d_out.shape,
+                                             None if d_lse is None else d_lse.shape, _layout(k_pool), _layout(v_pool), _layout(k_scale),
+                                             _layout(v_scale), attn.scale, attn.kernel)
+    if described != bytes(params):
+        raise ValueError("params do not describe these tensors (see attn_params and attn_quant_params)")
+    if d_workspace.numel() * d_workspace.element_size() < workspace:
+        raise ValueError(f"workspace is smaller than {fn}_workspace_bytes")
+    scales = () if k_scale is None else (_ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32))
+    code = getattr(_lib, fn)(_ptr(d_q, torch.bfloat16), _address(k_pool), _address(v_pool), *scales, _ptr(table, i32), _ptr(prefix, i32),
+                             _ptr(nodes, i32), _ptr(parent, i32), _ptr(leader, i32), _ptr(shared, i32), C.byref(params), _ptr(d_workspace),
+                             _ptr(d_out, torch.bfloat16), _ptr(d_lse, torch.float32), _stream_of(*tensors, *pools, d_workspace, d_out, d_lse))
+    _check(fn, code)
+
+
+def war_verify_attn_shared(d_q: torch.Tensor, d_kpool: torch.Tensor, d_vpool: torch.Tensor, d_page_table: torch.Tensor,
+                           d_prefix_len: torch.Tensor, d_num_nodes: torch.Tensor, d_parent: torch.Tensor, d_leader: torch.Tensor,
+                           d_shared_len: torch.Tensor, params: AttnParams, d_workspace: torch.Tensor, d_out: torch.Tensor,
+                           d_lse: Optional[torch.Tensor]) -> None:
+    """war_verify_attn for groups of requests that share a prefix (d_leader, d_shared_len: see war_prefix_groups); params from
+    attn_params, workspace from new_shared_workspace."""
+    if d_kpool.dtype != torch.bfloat16:
+        raise ValueError("pools must be bf16; war_verify_attn_shared_quant reads an 8-bit cache")
+    _attn_shared("war_verify_attn_shared", (d_q, d_page_table, d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len),
+                 (d_kpool, d_vpool, None, None), params, params, d_workspace, d_out, d_lse)
+
+
+def war_verify_attn_shared_quant(d_q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                                 d_page_table: torch.Tensor, d_prefix_len: torch.Tensor, d_num_nodes: torch.Tensor, d_parent: torch.Tensor,
+                                 d_leader: torch.Tensor, d_shared_len: torch.Tensor, params: AttnQuantParams, d_workspace: torch.Tensor,
+                                 d_out: torch.Tensor, d_lse: Optional[torch.Tensor]) -> None:
+    """war_verify_attn_shared over a float8_e4m3fn / float8_e5m2 cache; params from attn_quant_params, workspace from
+    new_shared_quant_workspace."""
+    if k_scale is None or v_scale is None:
+        raise ValueError("an 8-bit cache has scales; war_verify_attn_shared reads a bf16 cache")
+    _attn_shared("war_verify_attn_shared_quant", (d_q, d_page_table, d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len),
+                 (k_pool, v_pool, k_scale, v_scale), params, params.attn, d_workspace, d_out, d_lse)

@@ -4,6 +4,7 @@
 #include "war_quant.cuh"
 #include "war_attn_quant.cuh"
 #include "war_attn_sm100_parts.cuh"
+#include "war_attn_shared.cuh"
 
 namespace {
 
@@ -25,6 +26,8 @@ struct QuantKernelArgs {
     const int32_t* parent;
     int B;
     unsigned long long call;
+    const SharedUnit* shared_units;       // shared-prefix variant
+    const int* slot_map;
 };
 
 // One (page, head) of a pool: tensor (d, token, head, page), 128 bytes x page_size.
@@ -182,6 +185,7 @@ inline bool quant_kernel_args(const void* q, const AttnQuantPools& pools, const 
     a->page_shift = log2_of(p->page_size); a->block_shift = log2_of(pools.block); a->bpp_shift = a->page_shift - a->block_shift;
     a->kv_e5m2 = pools.kv == kKvE5M2;
     a->num_nodes = num_nodes; a->parent = parent; a->B = p->B; a->call = fused ? war_attn_next_call() : 0;
+    a->shared_units = nullptr; a->slot_map = nullptr;
     return true;
 }
 

@@ -23,6 +23,7 @@ struct UnitView {
     int req, kvh, rb, tile_begin, tile_end, n_chunks, chunk, n_nodes;
     int slot;                            // index of this unit's partial in the workspace
     int slot_base, slot_stride, bump;    // fused-plan variant: partial of chunk c is slot_base + c * slot_stride (+ bump for c == 0)
+    int page0, n_keys, visible, rows, slot0, part0;      // shared-prefix variant: see SharedUnit
 };
 
 // Ancestor-or-self bit masks of one tree, by one warp: lane l holds slots l and l + 32.  After round r a slot's mask

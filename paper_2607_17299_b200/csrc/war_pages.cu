@@ -1,0 +1,760 @@
+// The books of a paged cache: which pages requests hold, who shares them, which are free; and the copies that follow from it.
+//
+// refs[page] counts the table entries that hold a page, bit page % 32 of free[page / 32] is set iff it is 0.  Whatever changes the
+// books gives the same result in any order of the atomics: counts are sums, bits follow from counts, and pages are given out by
+// number (the k-th page wanted is the k-th lowest free one), not by who comes first.
+//
+// All of this is a few kilobytes to a few megabytes of integers per call, so a call costs its launch and the chain of dependent reads.
+// One launch each, then.  Fork, compaction and groups need all blocks to have read before one writes; they run as one cluster of
+// eight blocks, whose hardware barrier takes the place of further launches (a barrier: about 0.5 us; a launch in a graph: 1.5 to 2).
+#include <cooperative_groups.h>
+#include <mutex>
+#include "war_common.cuh"
+#include "war_quant.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int kMaxB = 4096;
+constexpr int kThreads = 1024;
+constexpr int kCluster = 8;
+constexpr int kMaxTail = 32;
+constexpr int kRound = 4 * kThreads;      // words of the free map that a block looks at together
+
+// ------------------------------------------------------------------------------------------------
+// block-wide sums
+// ------------------------------------------------------------------------------------------------
+struct ScanScratch { int warp[33]; };
+
+// Exclusive scan of x over the block, and the sum.  Block barriers inside.
+__device__ __forceinline__ int block_scan(int x, ScanScratch& s, int* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += y; }
+    if (lane == 31) s.warp[warp] = incl;
+    __syncthreads();
+    if (warp == 0) {
+        const int y = s.warp[lane];
+        int yi = y;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const int z = __shfl_up_sync(0xffffffffu, yi, o); if (lane >= o) yi += z; }
+        s.warp[lane] = yi - y;
+        if (lane == 31) s.warp[32] = yi;
+    }
+    __syncthreads();
+    const int before = s.warp[warp];
+    *total = s.warp[32];
+    __syncthreads();
+    return before + incl - x;
+}
+
+// the position of the k-th (from 0) set bit of a word that has it
+__device__ __forceinline__ int nth_bit(uint32_t word, int k) {
+    int at = 0;
+#pragma unroll
+    for (int width = 16; width > 0; width >>= 1) {
+        const int low = __popc((word >> at) & ((1u << width) - 1u));
+        if (k >= low) { k -= low; at += width; }
+    }
+    return at;
+}
+
+// largest i in [0, n) with a[i] <= x (a ascending, a[0] <= x)
+__device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// A round of the free map in shared memory: words, and how many free pages lie before each.
+struct FreeRound { uint32_t word[kRound]; int before[kRound + 1]; };
+
+// Loads words [first, first + kRound) (those behind n_words as empty); `before` counts from `base` on.  Returns the free pages.
+__device__ __forceinline__ int load_round(FreeRound& r, const uint32_t* free_map, long long first, long long n_words, int base, ScanScratch& s) {
+    const int w0 = (int)threadIdx.x * 4;
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {                                // (coalesced, then turned: a thread's four words are neighbours)
+        const int at = (int)threadIdx.x + k * kThreads;
+        r.word[at] = first + at < n_words ? free_map[first + at] : 0u;
+    }
+    __syncthreads();
+    int count = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { w[k] = r.word[w0 + k]; count += __popc(w[k]); }
+    int total, run = base + block_scan(count, s, &total);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { r.before[w0 + k] = run; run += __popc(w[k]); }
+    if (threadIdx.x == kThreads - 1) r.before[kRound] = run;
+    __syncthreads();
+    return total;
+}
+// The k-th free page (counted over all rounds) of the round that holds it.
+__device__ __forceinline__ int nth_free(const FreeRound& r, long long first, int k) {
+    const int at = last_at_most(r.before, kRound, k);            // (the last of equals: a word that holds pages)
+    return (int)((first + at) * 32 + nth_bit(r.word[at], k - r.before[at]));
+}
+
+// ------------------------------------------------------------------------------------------------
+// free
+// ------------------------------------------------------------------------------------------------
+// A block per request.  Pages of a cancelled group come back with their last holder, whichever block that is.
+__global__ void __launch_bounds__(256)
+pages_free_kernel(war_pages_t p, const int32_t* __restrict__ done, int32_t* tail_len, int* status_word) {
+    const int b = blockIdx.x;
+    if (done[b] == 0) return;
+    const int held = p.d_held[b];
+    int32_t* row = p.d_page_table + (size_t)b * p.max_pages_per_req;
+    if (held < 0 || held > p.max_pages_per_req) {
+        if (threadIdx.x == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+        return;
+    }
+#pragma unroll 4
+    for (int j = threadIdx.x; j < held; j += 256) {
+        const int page = row[j];
+        row[j] = -1;
+        if (page < 0 || page >= p.num_pages) { war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
+        const int had = atomicSub(&p.d_refs[page], 1);
+        if (had == 1) atomicOr(&p.d_free[page >> 5], 1u << (page & 31));
+        if (had <= 0) { atomicAdd(&p.d_refs[page], 1); war_set_device_status(status_word, WAR_ERR_BAD_PAGE); }
+    }
+    __syncthreads();                                              // (every thread has read held)
+    if (threadIdx.x == 0) {
+        p.d_held[b] = 0;
+        if (tail_len) tail_len[b] = -1;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// grow
+// ------------------------------------------------------------------------------------------------
+struct GrowShared {
+    ScanScratch scan;
+    FreeRound round;
+    int upto[kMaxB + 1];                   // pages wanted by the requests before
+    int held[kMaxB];
+};
+
+__global__ void __launch_bounds__(kThreads)
+pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ tail_len, int32_t* granted,
+                  int* status_word) {
+    extern __shared__ __align__(16) uint8_t pages_smem[];
+    GrowShared& s = *reinterpret_cast<GrowShared*>(pages_smem);
+    const int tid = threadIdx.x, B = p.B;
+    const long long n_words = (p.num_pages + 31) / 32;
+    // ---- what every request wants ----
+    int wanted = 0;
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+        const int b = b0 + tid;
+        int need = 0, have = 0;
+        if (b < B) {
+            have = p.d_held[b];
+            const long long pl = prefix_len[b];
+            const bool runs = !tail_len || tail_len[b] >= 0;
+            const long long want = (pl + N + p.page_size - 1) / p.page_size;
+            bool ok = runs;
+            if (runs && (pl < 0 || have < 0 || have > p.max_pages_per_req || want > p.max_pages_per_req)) {
+                war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+                ok = false;
+            }
+            need = ok ? max(0, (int)want - have) : 0;
+            s.held[b] = ok ? have : -1;                           // (-1: not to be served)
+        }
+        int total;
+        const int before = wanted + block_scan(need, s.scan, &total);
+        if (b < B) s.upto[b] = before;
+        wanted += total;
+    }
+    if (tid == 0) s.upto[B] = wanted;
+    __syncthreads();
+    // ---- are there so many?  (rounds of the map until there are) ----
+    int found = 0, rounds = 0;
+    if (wanted > 0)
+        for (long long first = 0; first < n_words && found < wanted; first += kRound, ++rounds) found += load_round(s.round, p.d_free, first, n_words, found, s.scan);
+    // a request is served iff all pages wanted up to and with it are there
+    int served = wanted;
+    if (found < wanted) served = s.upto[last_at_most(s.upto, B + 1, found)];
+    // ---- the k-th of them goes to the request that wants it ----
+    int base = 0;
+    for (int r = 0; r < rounds && base < served; ++r) {
+        const long long first = (long long)r * kRound;
+        int here = s.round.before[kRound] - s.round.before[0];
+        if (rounds > 1) {
+            __syncthreads();
+            here = load_round(s.round, p.d_free, first, n_words, base, s.scan);
+        }
+        for (int k = base + tid; k < min(base + here, served); k += kThreads) {
+            const int page = nth_free(s.round, first, k);
+            const int b = last_at_most(s.upto, B, k);
+            p.d_page_table[(size_t)b * p.max_pages_per_req + s.held[b] + (k - s.upto[b])] = page;
+            p.d_refs[page] = 1;
+            atomicAnd(&p.d_free[page >> 5], ~(1u << (page & 31)));
+        }
+        base += here;
+    }
+    for (int b = tid; b < B; b += kThreads) {
+        const int need = s.upto[b + 1] - s.upto[b];
+        const bool ok = s.held[b] >= 0 && (need == 0 || s.upto[b + 1] <= served);
+        if (granted) granted[b] = ok;
+        if (ok && need > 0) p.d_held[b] = s.held[b] + need;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// fork
+// ------------------------------------------------------------------------------------------------
+// What changes is decided by every block for itself from the books as they are; after the cluster's barrier the blocks write, a tile of
+// columns each at a time: a table's column is changed by one block alone, which holds all of its old entries in shared memory, so
+// requests that swap places need no second table.
+constexpr int kForkTile = 16384;          // entries of a tile
+struct ForkShared {
+    ScanScratch scan;
+    FreeRound round;
+    int16_t src[kMaxB];                    // source, -1: the request stays as it is
+    int first[kMaxB];                      // lowest request that takes this one, kMaxB: none
+    int takers[kMaxB];
+    int full[kMaxB];                       // full pages of this request
+    int held[kMaxB];
+    int last[kMaxB];                       // a request that is replaced: its partly filled page; -1: none
+    int fresh[kMaxB];                      // pages wanted by the requests before
+    int entries[kForkTile];
+    int columns;
+};
+
+__global__ void __launch_bounds__(kThreads)
+pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32_t* prefix_len, int32_t* tail, int32_t* tail_len,
+                  int32_t* copies, int32_t* n_copies, int32_t* ok_word, int* status_word) {
+    extern __shared__ __align__(16) uint8_t pages_smem[];
+    ForkShared& s = *reinterpret_cast<ForkShared*>(pages_smem);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, B = p.B, rank = (int)cluster.block_rank(), width = p.max_pages_per_req, page_size = p.page_size;
+    const long long n_words = (p.num_pages + 31) / 32;
+    // ---- who becomes whom ----
+    for (int b = tid; b < B; b += kThreads) { s.first[b] = kMaxB; s.takers[b] = 0; }
+    if (tid == 0) s.columns = 0;
+    __syncthreads();
+    for (int b = tid; b < B; b += kThreads) {
+        int src = d_src[b];
+        const int held = p.d_held[b];
+        s.held[b] = held;
+        s.full[b] = prefix_len[b] / page_size;                    // (looked at for sources only, which are checked)
+        if (src == b || src < 0) src = -1;
+        else {
+            bool ok = src < B && held >= 0 && held <= width;
+            if (ok && tail_len[src] < 0) ok = false;
+            if (ok) {
+                const int pl = prefix_len[src], src_held = p.d_held[src];
+                ok = pl >= 0 && src_held >= 0 && src_held <= width && (pl + (long long)page_size - 1) / page_size <= src_held;
+            }
+            if (!ok) { if (rank == 0) war_set_device_status(status_word, WAR_ERR_INVALID_ARG); src = -1; }
+        }
+        s.src[b] = (int16_t)src;
+        if (src >= 0) { atomicMin(&s.first[src], b); atomicAdd(&s.takers[src], 1); }
+    }
+    __syncthreads();
+    // ---- partly filled pages: the first that takes a request which is itself replaced gets its page, the others a fresh one ----
+    int wanted = 0;
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+        const int b = b0 + tid;
+        int fresh = 0;
+        if (b < B) {
+            const int src = s.src[b];
+            int last = -1;
+            if (src >= 0 && prefix_len[src] % page_size != 0) {
+                last = p.d_page_table[(size_t)src * width + s.full[src]];
+                const bool bad = last < 0 || last >= p.num_pages;
+                if (bad) { if (rank == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); last = 0; }
+                fresh = bad || !(s.src[src] >= 0 && s.first[src] == b && p.d_refs[last] == 1);
+            }
+            s.last[b] = last;
+            if (src >= 0) atomicMax(&s.columns, max(s.held[b], s.full[src] + (last >= 0)));
+        }
+        int total;
+        const int before = wanted + block_scan(fresh, s.scan, &total);
+        if (b < B) s.fresh[b] = fresh ? before : -1;
+        wanted += total;
+    }
+    // ---- the fresh pages; all or nothing ----
+    int found = 0;
+    bool enough = true;
+    __syncthreads();
+    if (wanted > 0) {
+        // (fresh[b] holds the page's number in the order of the free ones until its round comes, then ~page)
+        for (long long first = 0; first < n_words && found < wanted; first += kRound) {
+            const int here = load_round(s.round, p.d_free, first, n_words, found, s.scan);
+            for (int b = tid; b < B; b += kThreads) {
+                const int k = s.fresh[b];
+                if (k >= found && k < found + here) s.fresh[b] = ~nth_free(s.round, first, k) - 1;           // (below -1)
+            }
+            found += here;
+            __syncthreads();
+        }
+        enough = found >= wanted;
+    }
+    const int columns = s.columns;
+    if (rank == 0 && tid == 0) { *ok_word = enough; *n_copies = enough ? wanted : 0; }
+    // ---- everything has been read but the rows themselves and the tails; every block takes its columns ----
+    const int tail_tile = 1;                                      // (one more tile: the tail windows)
+    const int tile_cols = max(1, min(64, kForkTile / max(1, B)));
+    const int tiles = (columns + tile_cols - 1) / tile_cols + tail_tile;
+    int pl_new[kMaxB / kThreads], tl_new[kMaxB / kThreads];
+#pragma unroll
+    for (int k = 0; k < kMaxB / kThreads; ++k) {
+        const int b = tid + k * kThreads;
+        pl_new[k] = tl_new[k] = 0;
+        if (b < B && s.src[b] >= 0) { pl_new[k] = prefix_len[s.src[b]]; tl_new[k] = tail_len[s.src[b]]; }
+    }
+    // ---- list of copies: fresh pages in the order of the requests ----
+    int listed = 0;
+    if (rank == 0 && enough) {
+        for (int b0 = 0; b0 < B; b0 += kThreads) {
+            const int b = b0 + tid;
+            const bool fresh = b < B && s.fresh[b] < -1;
+            int total;
+            const int at = listed + block_scan(fresh ? 1 : 0, s.scan, &total);
+            if (fresh) {
+                copies[3 * at] = s.last[b]; copies[3 * at + 1] = ~(s.fresh[b] + 1); copies[3 * at + 2] = prefix_len[s.src[b]] % page_size;
+            }
+            listed += total;
+        }
+    }
+    cluster.sync();
+    if (!enough) return;
+    if (rank == 0) {
+#pragma unroll
+        for (int k = 0; k < kMaxB / kThreads; ++k) {
+            const int b = tid + k * kThreads;
+            if (b >= B || s.src[b] < 0) continue;
+            prefix_len[b] = pl_new[k];
+            tail_len[b] = tl_new[k];
+            p.d_held[b] = s.full[s.src[b]] + (s.last[b] >= 0);
+            if (s.fresh[b] < -1) {
+                const int page = ~(s.fresh[b] + 1);
+                p.d_refs[page] = 1;
+                atomicAnd(&p.d_free[page >> 5], ~(1u << (page & 31)));
+            }
+        }
+    }
+    for (int t = rank; t < tiles; t += kCluster) {
+        const bool is_tail = t == tiles - 1;
+        const int c0 = is_tail ? 0 : t * tile_cols;
+        const int cols = is_tail ? P : min(tile_cols, columns - c0);
+        int32_t* const table = is_tail ? tail : p.d_page_table + c0;
+        const int stride = is_tail ? P : width;
+        const int batch = is_tail ? kForkTile / kMaxTail : B;     // (tails of many requests do not fit at once; see below)
+        if (is_tail && B > batch) {
+            // too many for one tile: column by column
+            for (int c = 0; c < P; ++c) {
+                __syncthreads();
+                for (int b = tid; b < B; b += kThreads) s.entries[b] = tail[(size_t)b * P + c];
+                __syncthreads();
+                for (int b = tid; b < B; b += kThreads) if (s.src[b] >= 0) tail[(size_t)b * P + c] = s.entries[s.src[b]];
+            }
+            continue;
+        }
+        __syncthreads();
+        for (int x = tid; x < B * cols; x += kThreads) {
+            const int b = x / cols, c = x - b * cols;
+            if (s.src[b] >= 0 || s.takers[b] > 0) s.entries[x] = table[(size_t)b * stride + c];
+        }
+        __syncthreads();
+        for (int x = tid; x < B * cols; x += kThreads) {
+            const int b = x / cols, c = x - b * cols, src = s.src[b];
+            if (is_tail) {
+                if (src >= 0) tail[(size_t)b * P + c] = s.entries[src * cols + c];
+                continue;
+            }
+            const int col = c0 + c;
+            // what this entry's page gains and loses: a holder for every request that takes it as a full page, this row if it is
+            // replaced, unless its partly filled page is handed on
+            int delta = (col < s.full[b] ? s.takers[b] : 0) - (src >= 0 && col < s.held[b] ? 1 : 0);
+            if (delta < 0 && col == s.full[b] && s.first[b] < kMaxB && s.last[s.first[b]] >= 0 && s.fresh[s.first[b]] == -1) delta = 0;
+            if (delta != 0) {
+                const int page = s.entries[x];
+                if (page < 0 || page >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+                else if (atomicAdd(&p.d_refs[page], delta) + delta == 0) atomicOr(&p.d_free[page >> 5], 1u << (page & 31));
+            }
+            if (src < 0) continue;
+            int now = -1;
+            if (col < s.full[src]) now = s.entries[src * cols + c];
+            else if (col == s.full[src] && s.last[b] >= 0) now = s.fresh[b] < -1 ? ~(s.fresh[b] + 1) : s.last[b];
+            else if (col >= s.held[b]) continue;                  // (nothing stood there)
+            p.d_page_table[(size_t)b * width + col] = now;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// compact
+// ------------------------------------------------------------------------------------------------
+// The i-th highest used page goes to the i-th lowest free page while it lies above it.  With U pages in use that moves exactly the
+// used pages at or above U, so the two lists are the free pages below U, upwards, and the used ones from U on, downwards.
+struct CompactShared {
+    ScanScratch scan;
+    int used;                              // of this block's words
+    int free_below, used_above;            // of this block's words, below / from U on
+};
+
+__global__ void __launch_bounds__(kThreads)
+pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies, int32_t* n_copies, int32_t* top, int* status_word) {
+    __shared__ CompactShared s;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, rank = (int)cluster.block_rank();
+    const int n_words = (int)((p.num_pages + 31) / 32);
+    int32_t* const place = ws;                                    // [num_pages] where a used page from U on goes
+    int32_t* const to = ws + p.num_pages;                         // free pages below U
+    int32_t* const from = to + p.num_pages;                       // used pages from U on
+    const int per = (n_words + kCluster - 1) / kCluster, w0 = min(n_words, rank * per), w1 = min(n_words, w0 + per);
+    auto valid = [&](int w) -> uint32_t {                         // pages of a word that exist
+        const long long left = p.num_pages - (long long)w * 32;
+        return left >= 32 ? 0xffffffffu : (1u << left) - 1u;
+    };
+    // ---- pages in use ----
+    int used = 0;
+    for (int w = w0 + tid; w < w1; w += kThreads) used += __popc(~p.d_free[w] & valid(w));
+    int total;
+    block_scan(used, s.scan, &total);
+    if (tid == 0) s.used = total;
+    cluster.sync();
+    int U = 0;
+    for (int r = 0; r < kCluster; ++r) U += *cluster.map_shared_rank(&s.used, r);
+    // ---- this block's part of both lists ----
+    auto below = [&](int w) -> uint32_t {                         // pages of a word below U
+        const int left = U - w * 32;
+        return left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+    };
+    int lo = 0, hi = 0;
+    for (int w = w0 + tid; w < w1; w += kThreads) {
+        const uint32_t f = p.d_free[w];
+        lo += __popc(f & below(w));
+        hi += __popc(~f & valid(w) & ~below(w));
+    }
+    int lo_all, hi_all;
+    block_scan(lo, s.scan, &lo_all);
+    block_scan(hi, s.scan, &hi_all);
+    if (tid == 0) { s.free_below = lo_all; s.used_above = hi_all; }
+    cluster.sync();
+    int lo_at = 0, hi_at = 0, moves = 0;                          // free ones before this block's, used ones behind it
+    for (int r = 0; r < kCluster; ++r) {
+        const int x = *cluster.map_shared_rank(&s.free_below, r), y = *cluster.map_shared_rank(&s.used_above, r);
+        if (r < rank) lo_at += x;
+        if (r > rank) hi_at += y;
+        moves += x;
+    }
+    hi_at += hi_all;
+    for (int first = w0; first < w1; first += kThreads) {         // words in order: free ones from the front, used ones from the back
+        const int w = first + tid;
+        const uint32_t f = w < w1 ? p.d_free[w] : 0u;
+        uint32_t a = w < w1 ? f & below(w) : 0u, c = w < w1 ? ~f & valid(w) & ~below(w) : 0u;
+        int a_all, c_all;
+        int at = lo_at + block_scan(__popc(a), s.scan, &a_all);
+        int back = hi_at - block_scan(__popc(c), s.scan, &c_all);
+        lo_at += a_all; hi_at -= c_all;
+        while (a) { to[at++] = w * 32 + __ffs(a) - 1; a &= a - 1; }
+        while (c) { from[--back] = w * 32 + __ffs(c) - 1; c &= c - 1; }
+    }
+    cluster.sync();
+    // ---- the moves ----
+    const int done = min(moves, max_copies);
+    for (int i = rank * kThreads + tid; i < moves; i += kCluster * kThreads) {
+        const int a = from[i], c = to[i];
+        place[a] = i < done ? c : a;
+        if (i >= done) continue;
+        p.d_refs[c] = p.d_refs[a];
+        p.d_refs[a] = 0;
+        atomicAnd(&p.d_free[c >> 5], ~(1u << (c & 31)));
+        atomicOr(&p.d_free[a >> 5], 1u << (a & 31));
+        copies[3 * i] = a; copies[3 * i + 1] = c; copies[3 * i + 2] = p.page_size;
+    }
+    if (rank == 0 && tid == 0) {
+        *n_copies = done;
+        *top = done < moves ? from[done] + 1 : U;
+    }
+    cluster.sync();
+    // ---- the tables follow ----
+    for (int b = rank; b < p.B; b += kCluster) {
+        const int held = p.d_held[b];
+        int32_t* row = p.d_page_table + (size_t)b * p.max_pages_per_req;
+        if (held < 0 || held > p.max_pages_per_req) { if (tid == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
+        for (int j = tid; j < held; j += kThreads) {
+            const int page = row[j];
+            if (page < 0 || page >= p.num_pages) { war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
+            if (page < U) continue;
+            const int now = place[page];
+            if (now < 0 || now >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);   // (a held page marked as free)
+            else row[j] = now;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// groups
+// ------------------------------------------------------------------------------------------------
+struct GroupShared { int key[kMaxB]; };
+
+__global__ void __launch_bounds__(kThreads)
+prefix_groups_kernel(const int32_t* __restrict__ table, const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ tail_len,
+                     int B, int page_size, int width, int column, int32_t* leader, int32_t* shared_len) {
+    __shared__ GroupShared s;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, rank = (int)cluster.block_rank();
+    constexpr int kNone = 0x7fffffff;
+    auto full_of = [&](int b) -> int { return min(max(prefix_len[b], 0) / page_size, width); };
+    for (int b = tid; b < B; b += kThreads) {
+        const bool runs = !tail_len || tail_len[b] >= 0;
+        s.key[b] = runs && column < full_of(b) ? table[(size_t)b * width + column] : -1;
+    }
+    __syncthreads();
+    // ---- the lowest request with the same page, a warp each; the smallest common length starts as "nobody else" ----
+    for (int b = (rank * kThreads + tid) >> 5; b < B; b += kCluster * (kThreads / 32)) {
+        const int key = s.key[b];
+        int l = b;
+        for (int q = 0; key >= 0 && q < b; q += 32) {
+            const uint32_t m = __ballot_sync(0xffffffffu, q + lane < b && s.key[q + lane] == key);
+            if (m) { l = q + __ffs(m) - 1; break; }
+        }
+        if (lane == 0) { leader[b] = l; shared_len[b] = kNone; }
+    }
+    cluster.sync();
+    // ---- common full pages of every member with its leader, a warp each, 128 columns at a time ----
+    for (int b = (rank * kThreads + tid) >> 5; b < B; b += kCluster * (kThreads / 32)) {
+        const int l = leader[b];
+        if (l == b) continue;
+        const int n = min(full_of(b), full_of(l));
+        const int32_t *x = table + (size_t)b * width, *y = table + (size_t)l * width;
+        int same = n;
+        for (int c = 0; c < n; c += 128) {
+            uint32_t differ[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int at = c + k * 32 + lane;
+                differ[k] = at < n ? (uint32_t)(x[at] != y[at]) : 0u;
+            }
+            bool stop = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t m = __ballot_sync(0xffffffffu, differ[k] != 0);
+                if (m && !stop) { same = c + k * 32 + __ffs(m) - 1; stop = true; }
+            }
+            if (stop) break;
+        }
+        if (lane == 0) atomicMin(&shared_len[l], same);
+    }
+    cluster.sync();
+    const int b = rank * kThreads + tid;                          // (one request a thread: B <= 8192)
+    int l = b, common = kNone;
+    if (b < B) { l = leader[b]; common = *(volatile int32_t*)&shared_len[l]; }
+    cluster.sync();
+    if (b < B) {
+        const bool group = common != kNone && common > column;
+        leader[b] = group ? l : b;
+        shared_len[b] = group ? common * page_size : 0;
+    }
+}
+static_assert(kMaxB <= kCluster * kThreads, "one request a thread");
+
+// ------------------------------------------------------------------------------------------------
+// copy
+// ------------------------------------------------------------------------------------------------
+struct CopyArgs {
+    uint8_t *k, *v;
+    float *kscale, *vscale;
+    long long ks[3], vs[3];                // strides (page, head, token) in bytes
+    const int32_t *copies, *n_copies;
+    long long num_pages;
+    int max_copies, Hkv, page_size, row_bytes, block;
+};
+
+// A warp per (copy, K or V, head): rows of 256 or 128 bytes, 512 bytes a warp's instruction, up to eight of them in flight.
+constexpr int kCopyWarps = 8;
+template <int kLanesPerRow>                // 16-byte pieces of a row: 16 (bf16) or 8
+__global__ void __launch_bounds__(kCopyWarps * 32)
+pages_copy_kernel(const CopyArgs a, int* status_word) {
+    constexpr int kRows = 32 / kLanesPerRow, kDeep = 8;
+    const int lane = threadIdx.x & 31, r0 = lane / kLanesPerRow, piece = lane % kLanesPerRow;
+    const int n = min(max(*a.n_copies, 0), a.max_copies);
+    const long long tasks = (long long)n * 2 * a.Hkv, step = (long long)gridDim.x * kCopyWarps;
+    for (long long t = (long long)blockIdx.x * kCopyWarps + (threadIdx.x >> 5); t < tasks; t += step) {
+        const int c = (int)(t / (2 * a.Hkv)), rest = (int)(t - (long long)c * 2 * a.Hkv), which = rest / a.Hkv, h = rest - which * a.Hkv;
+        const long long from = a.copies[3 * c], to = a.copies[3 * c + 1];
+        const int rows = min(max(a.copies[3 * c + 2], 0), a.page_size);
+        if (from < 0 || from >= a.num_pages || to < 0 || to >= a.num_pages) {
+            if (lane == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+            continue;
+        }
+        uint8_t* const pool = which ? a.v : a.k;
+        const long long s_page = which ? a.vs[0] : a.ks[0], s_head = which ? a.vs[1] : a.ks[1], s_row = which ? a.vs[2] : a.ks[2];
+        const uint8_t* src = pool + from * s_page + h * s_head + piece * 16;
+        uint8_t* dst = pool + to * s_page + h * s_head + piece * 16;
+        for (int r = r0; r < rows; r += kRows * kDeep) {
+            uint4 x[kDeep];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k)
+                if (r + k * kRows < rows) x[k] = __ldcs(reinterpret_cast<const uint4*>(src + (r + k * kRows) * s_row));
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k)
+                if (r + k * kRows < rows) *reinterpret_cast<uint4*>(dst + (r + k * kRows) * s_row) = x[k];
+        }
+        if (a.block > 0) {                                        // scales of the blocks that hold these rows
+            float* const sc = which ? a.vscale : a.kscale;
+            const int bpp = a.page_size / a.block;
+            if (lane < (rows + a.block - 1) / a.block) sc[(to * a.Hkv + h) * bpp + lane] = sc[(from * a.Hkv + h) * bpp + lane];
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+constexpr int kMaxDevices = 64;
+std::once_flag g_dev_once[kMaxDevices];
+int g_sm_count[kMaxDevices];
+war_status_t g_dev_status[kMaxDevices];
+
+war_status_t device_setup(int* sm_count) {
+    int dev = 0;
+    WAR_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices) return WAR_ERR_UNSUPPORTED;
+    std::call_once(g_dev_once[dev], [dev]() {
+        g_dev_status[dev] = WAR_ERR_CUDA;
+        if (cudaDeviceGetAttribute(&g_sm_count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return;
+        if (cudaFuncSetAttribute(pages_grow_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GrowShared)) != cudaSuccess) return;
+        if (cudaFuncSetAttribute(pages_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ForkShared)) != cudaSuccess) return;
+        g_dev_status[dev] = WAR_OK;
+    });
+    if (g_dev_status[dev] != WAR_OK) (void)cudaGetLastError();
+    *sm_count = g_sm_count[dev];
+    return g_dev_status[dev];
+}
+static_assert(sizeof(ForkShared) <= 232448 && sizeof(GrowShared) <= 232448, "shared memory");
+
+// One cluster of kCluster blocks.
+template <class... Params, class... Args>
+war_status_t launch_cluster(void (*kernel)(Params...), size_t smem, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kCluster); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kCluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    WAR_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...));
+    return WAR_OK;
+}
+
+war_status_t check_pages(const war_pages_t* p) {
+    if (!p || p->B < 0 || p->page_size < 1 || p->max_pages_per_req < 1 || p->num_pages < 1) return WAR_ERR_INVALID_ARG;
+    if (p->B > kMaxB || p->num_pages > (1ll << 30)) return WAR_ERR_UNSUPPORTED;
+    if (p->B > 0 && (!p->d_refs || !p->d_free || !p->d_page_table || !p->d_held)) return WAR_ERR_INVALID_ARG;
+    return WAR_OK;
+}
+
+}  // namespace
+
+extern "C" war_status_t war_pages_free(const war_pages_t* p, const int32_t* d_done, int32_t* d_tail_len, war_stream_t stream) {
+    const war_status_t st = check_pages(p);
+    if (st != WAR_OK) return st;
+    if (p->B == 0) return WAR_OK;
+    if (!d_done) return WAR_ERR_INVALID_ARG;
+    int* status_word = war_status_word();
+    if (!status_word) return WAR_ERR_CUDA;
+    pages_free_kernel<<<p->B, 256, 0, stream>>>(*p, d_done, d_tail_len, status_word);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
+}
+
+extern "C" war_status_t war_pages_grow(const war_pages_t* p, int32_t N, const int32_t* d_prefix_len, const int32_t* d_tail_len,
+                                       int32_t* d_granted, war_stream_t stream) {
+    war_status_t st = check_pages(p);
+    if (st != WAR_OK) return st;
+    if (N < 0 || (long long)N + p->page_size >= (1ll << 30)) return WAR_ERR_INVALID_ARG;
+    if (p->B == 0) return WAR_OK;
+    if (!d_prefix_len || !d_granted) return WAR_ERR_INVALID_ARG;
+    int* status_word = war_status_word();
+    if (!status_word) return WAR_ERR_CUDA;
+    int sms;
+    st = device_setup(&sms);
+    if (st != WAR_OK) return st;
+    pages_grow_kernel<<<1, kThreads, sizeof(GrowShared), stream>>>(*p, N, d_prefix_len, d_tail_len, d_granted, status_word);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
+}
+
+extern "C" war_status_t war_pages_fork(const war_pages_t* p, const int32_t* d_src, int32_t P, int32_t* d_prefix_len, int32_t* d_tail,
+                                       int32_t* d_tail_len, int32_t* d_copies, int32_t* d_n_copies, int32_t* d_ok, war_stream_t stream) {
+    war_status_t st = check_pages(p);
+    if (st != WAR_OK) return st;
+    if (P < 1 || P > kMaxTail) return WAR_ERR_INVALID_ARG;
+    if (p->B == 0) return WAR_OK;
+    if (!d_src || !d_prefix_len || !d_tail || !d_tail_len || !d_copies || !d_n_copies || !d_ok) return WAR_ERR_INVALID_ARG;
+    int* status_word = war_status_word();
+    if (!status_word) return WAR_ERR_CUDA;
+    int sms;
+    st = device_setup(&sms);
+    if (st != WAR_OK) return st;
+    return launch_cluster(pages_fork_kernel, sizeof(ForkShared), stream, *p, d_src, P, d_prefix_len, d_tail, d_tail_len, d_copies, d_n_copies,
+                          d_ok, status_word);
+}
+
+extern "C" size_t war_pages_compact_workspace_bytes(int64_t num_pages) {
+    return num_pages < 1 || num_pages > (1ll << 30) ? 0 : (size_t)num_pages * 3 * sizeof(int32_t);
+}
+
+extern "C" war_status_t war_pages_compact(const war_pages_t* p, void* d_workspace, int32_t max_copies, int32_t* d_copies,
+                                          int32_t* d_n_copies, int32_t* d_top, war_stream_t stream) {
+    war_status_t st = check_pages(p);
+    if (st != WAR_OK) return st;
+    if (max_copies < 0 || !p->d_refs || !p->d_free) return WAR_ERR_INVALID_ARG;
+    if (!d_workspace || ((uintptr_t)d_workspace & 3) || (!d_copies && max_copies > 0) || !d_n_copies || !d_top) return WAR_ERR_INVALID_ARG;
+    int* status_word = war_status_word();
+    if (!status_word) return WAR_ERR_CUDA;
+    int sms;
+    st = device_setup(&sms);
+    if (st != WAR_OK) return st;
+    return launch_cluster(pages_compact_kernel, 0, stream, *p, (int32_t*)d_workspace, max_copies, d_copies, d_n_copies, d_top, status_word);
+}
+
+extern "C" war_status_t war_prefix_groups(const int32_t* d_page_table, const int32_t* d_prefix_len, const int32_t* d_tail_len, int32_t B,
+                                          int32_t page_size, int32_t max_pages_per_req, int32_t min_shared, int32_t* d_leader,
+                                          int32_t* d_shared_len, war_stream_t stream) {
+    if (B < 0 || page_size < 1 || max_pages_per_req < 1 || min_shared < 1) return WAR_ERR_INVALID_ARG;
+    if (B > kMaxB) return WAR_ERR_UNSUPPORTED;
+    if (B == 0) return WAR_OK;
+    if (!d_page_table || !d_prefix_len || !d_leader || !d_shared_len) return WAR_ERR_INVALID_ARG;
+    const int column = (min_shared - 1) / page_size;
+    return launch_cluster(prefix_groups_kernel, 0, stream, d_page_table, d_prefix_len, d_tail_len, B, page_size, max_pages_per_req, column,
+                          d_leader, d_shared_len);
+}
+
+extern "C" war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d_n_copies, int32_t max_copies, void* d_kpool, void* d_vpool,
+                                       float* d_kscale, float* d_vscale, const war_pages_copy_params_t* q, war_stream_t stream) {
+    if (!q || max_copies < 0 || q->Hkv < 1 || q->Hkv > 65535 || q->page_size < 1 || q->num_pages < 1) return WAR_ERR_INVALID_ARG;
+    if (q->kv_type != kKvBf16 && q->kv_type != kKvE4M3 && q->kv_type != kKvE5M2) return WAR_ERR_INVALID_ARG;
+    if (q->D != 128 || q->num_pages > (1ll << 30)) return WAR_ERR_UNSUPPORTED;
+    const bool quant = q->kv_type != kKvBf16;
+    if (quant && !war_quant_block_ok(q->page_size, q->scale_block)) return WAR_ERR_UNSUPPORTED;
+    if (quant && q->page_size / q->scale_block > 32) return WAR_ERR_UNSUPPORTED;
+    const int size = quant ? 1 : 2;
+    if (!war_rows_aligned(q->kpool_strides, size) || !war_rows_aligned(q->vpool_strides, size)) return WAR_ERR_UNSUPPORTED;
+    if (max_copies == 0) return WAR_OK;
+    if (!d_copies || !d_n_copies || !d_kpool || !d_vpool || (quant && (!d_kscale || !d_vscale))) return WAR_ERR_INVALID_ARG;
+    if (((uintptr_t)d_kpool | (uintptr_t)d_vpool) & 15) return WAR_ERR_INVALID_ARG;
+    int* status_word = war_status_word();
+    if (!status_word) return WAR_ERR_CUDA;
+    int sms;
+    const war_status_t st = device_setup(&sms);
+    if (st != WAR_OK) return st;
+    CopyArgs a;
+    a.k = (uint8_t*)d_kpool; a.v = (uint8_t*)d_vpool; a.kscale = d_kscale; a.vscale = d_vscale;
+    for (int i = 0; i < 3; ++i) { a.ks[i] = q->kpool_strides[i] * size; a.vs[i] = q->vpool_strides[i] * size; }
+    a.copies = d_copies; a.n_copies = d_n_copies; a.num_pages = q->num_pages; a.max_copies = max_copies;
+    a.Hkv = q->Hkv; a.page_size = q->page_size; a.row_bytes = 128 * size; a.block = quant ? q->scale_block : 0;
+    const long long blocks = ((long long)max_copies * 2 * q->Hkv + kCopyWarps - 1) / kCopyWarps;
+    const int grid = (int)(blocks < sms * 8ll ? blocks : sms * 8ll);
+    if (quant) pages_copy_kernel<8><<<grid, kCopyWarps * 32, 0, stream>>>(a, status_word);
+    else pages_copy_kernel<16><<<grid, kCopyWarps * 32, 0, stream>>>(a, status_word);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
+}

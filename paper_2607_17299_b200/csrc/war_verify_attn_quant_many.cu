@@ -30,6 +30,7 @@
 #include <mutex>
 #include <type_traits>
 #include "war_attn_quant_sm100_parts.cuh"
+#include "war_attn_shared.cuh"
 
 namespace {
 
@@ -92,8 +93,8 @@ __device__ __forceinline__ void tmem_zero8(uint32_t taddr) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%1], {%0, %0, %0, %0, %0, %0, %0, %0};" ::"r"(0), "r"(taddr) : "memory");
 }
 
-// kFused: see attn_sm100_kernel.
-template <bool kFused>
+// kFused, kShared: see attn_sm100_kernel.
+template <bool kFused, bool kShared = false>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const QuantKernelArgs a) {
     extern __shared__ uint8_t smem_raw[];
@@ -111,7 +112,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     if (!kFused) {
         n_units = a.w.counters[1];
         // k-th unit of this CTA: its own contiguous list, or the snake deal of the longest-first list
-        contiguous = a.w.counters[3] != 0 && gridDim.x <= (unsigned)kMaxPlanCtas;
+        contiguous = !kShared && a.w.counters[3] != 0 && gridDim.x <= (unsigned)kMaxPlanCtas;
         list_first = contiguous ? a.w.cta_first[blockIdx.x] : 0; list_end = contiguous ? a.w.cta_first[blockIdx.x + 1] : 0;
     }
     auto unit_at = [&](int k) -> int {
@@ -131,6 +132,13 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         }
         const int u = unit_at(cur.k++);
         if (u >= n_units) return false;
+        if (kShared) {
+            const SharedUnit x = a.shared_units[u];
+            un.req = x.req; un.kvh = x.kvh; un.rb = x.rb; un.tile_begin = x.tile_begin; un.tile_end = x.tile_end;
+            un.n_chunks = x.whole ? 1 : 2; un.chunk = 0; un.n_nodes = 0;
+            un.page0 = x.page0; un.n_keys = x.n_keys; un.visible = x.visible; un.rows = x.rows; un.slot0 = x.slot0; un.part0 = x.part0;
+            return true;
+        }
         const AttnUnit x = a.w.units[u];
         un.req = x.req; un.kvh = x.kvh; un.rb = x.rb; un.tile_begin = x.tile_begin; un.tile_end = x.tile_end;
         un.n_chunks = x.n_chunks; un.chunk = x.chunk; un.n_nodes = a.w.req[x.req].n_nodes;
@@ -206,9 +214,9 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             UnitView un;
             if (!fetch(cur, un)) break;
             const int i = un.req;
-            const int L = a.prefix_len[i] + un.n_nodes;
+            const int L = kShared ? un.n_keys : a.prefix_len[i] + un.n_nodes;
             const int total_pages = (L + a.page_size - 1) / a.page_size;
-            const int32_t* pt = a.page_table + (size_t)i * a.max_pages;
+            const int32_t* pt = a.page_table + (size_t)i * a.max_pages + (kShared ? un.page0 : 0);
             const int T = un.tile_end - un.tile_begin;
             auto page_of = [&](int t) -> int {                   // this lane's page id in local tile t (-1: none)
                 if (t >= T || lane >= pages_per_tile) return -1;
@@ -367,16 +375,17 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             if (!fetch(cur, un)) break;
             const int i = un.req;
             const int n = un.n_nodes;
-            const int R = a.G * n;
-            const int pl = a.prefix_len[i];
-            const int L = pl + n;
+            const int R = kShared ? un.rows : a.G * n;
+            const int pl = kShared ? un.visible : a.prefix_len[i];
+            const int L = kShared ? un.n_keys : pl + n;
             const bool twice = R - un.rb * kRowBlock <= 64;
             const int copy = twice ? row >> 6 : 0;
             const int r_l = twice ? row & 63 : row;                      // row in the block
             const int gr = un.rb * kRowBlock + r_l;
             const bool in_tree = gr < R;
             const int j = in_tree ? gr / a.G : 0, g = in_tree ? gr % a.G : 0;
-            const size_t qrow = ((size_t)i * a.N + j) * a.Hq + un.kvh * a.G + g;
+            const size_t slot_row = kShared && un.slot0 >= 0 ? (size_t)a.slot_map[un.slot0 + j] : (size_t)i * a.N + j;
+            const size_t qrow = slot_row * a.Hq + un.kvh * a.G + g;
             const int T = un.tile_end - un.tile_begin;
             // fused-plan variant: the plan has looked at num_nodes and prefix_len only; the tree itself is checked
             // below, by every warp that is about to use it (all come to the same verdict).  Its parent row is
@@ -447,7 +456,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                 anc = tree_ok ? warp_ancestor_mask(q0, q1, n, j, lane) : 0ull;
                 if (!valid) anc = 0ull;
             } else {
-                anc = valid ? a.w.anc[(size_t)i * a.N + j] : 0ull;
+                anc = valid && !(kShared && un.slot0 >= 0) ? a.w.anc[slot_row] : 0ull;
             }
             float m_used = -CUDART_INF_F, l = 0.f;
             float v_ref = 1.f;                                             // power of two that V's scales are taken relative to
@@ -610,7 +619,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                     const float f1 = (m1 == -CUDART_INF_F ? 0.f : exp2f(m1 - M)) * st_w[128 + row] * norm;
                     const bool use1 = theirs > 0;                          // uniform: O of group 1 is stale when it had no tile
                     __nv_bfloat16* const out = a.out + qrow * 128;
-                    float* const part = split ? a.w.part_o + ((size_t)un.slot * a.w.rows + r_l) * 128 : nullptr;
+                    const size_t part_row = kShared ? (size_t)un.part0 + r_l : (size_t)un.slot * a.w.rows + r_l;
+                    float* const part = split ? a.w.part_o + part_row * 128 : nullptr;
                     auto store8 = [&](int col, const float* x) {           // eight columns of this row
                         if (split) {
                             float4* dst = reinterpret_cast<float4*>(part + col);
@@ -673,8 +683,8 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                         if (!split) {
                             if (a.lse) a.lse[qrow] = (M + log2f(lsum)) * kLn2;
                         } else {
-                            a.w.part_ml[((size_t)un.slot * a.w.rows + r_l) * 2] = M;
-                            a.w.part_ml[((size_t)un.slot * a.w.rows + r_l) * 2 + 1] = lsum;
+                            a.w.part_ml[part_row * 2] = M;
+                            a.w.part_ml[part_row * 2 + 1] = lsum;
                         }
                     }
                 }
@@ -771,7 +781,7 @@ war_status_t g_dev_status[kMaxDevices];
 war_status_t device_setup(int dev) {
     std::call_once(g_dev_once[dev], [dev]() {
         g_dev_status[dev] = WAR_ERR_CUDA;
-        for (const auto kernel : {attn_quant_many_kernel<false>, attn_quant_many_kernel<true>})
+        for (const auto kernel : {attn_quant_many_kernel<false>, attn_quant_many_kernel<true>, attn_quant_many_kernel<false, true>})
             if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) return;
         g_dev_status[dev] = WAR_OK;
     });
@@ -798,6 +808,28 @@ war_status_t war_attn_quant_launch_many(const void* q, const AttnQuantPools& poo
         return WAR_ERR_UNSUPPORTED;
     if (fused) attn_quant_many_kernel<true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
     else attn_quant_many_kernel<false><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
+}
+
+war_status_t war_attn_quant_launch_shared(const void* q, const AttnQuantPools& pools, const int32_t* page_table,
+                                          const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse,
+                                          int* status_word, cudaStream_t s) {
+    int dev = 0;
+    WAR_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices) return WAR_ERR_UNSUPPORTED;
+    const war_status_t st = device_setup(dev);
+    if (st != WAR_OK) return st;
+    const int grid = war_attn_sm_count();
+    if (grid <= 0) return WAR_ERR_CUDA;
+    AttnWorkspace parts{};
+    parts.counters = w.counters; parts.anc = w.anc; parts.part_ml = w.part_ml; parts.part_o = w.part_o;
+    CUtensorMap k_map, v_map;
+    QuantKernelArgs a;
+    if (!quant_kernel_args(q, pools, page_table, nullptr, nullptr, nullptr, p, parts, false, out, lse, status_word, &a, &k_map, &v_map))
+        return WAR_ERR_UNSUPPORTED;
+    a.shared_units = w.units; a.slot_map = w.slot_map;
+    attn_quant_many_kernel<false, true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
     WAR_LAUNCH_CHECK();
     return WAR_OK;
 }
