@@ -26,7 +26,8 @@ struct QuantKernelArgs {
     const int32_t* parent;
     int B;
     unsigned long long call;
-    const SharedUnit* shared_units;       // shared-prefix variant
+    const uint2* shared_units;            // shared-prefix variant
+    const SharedPart* shared_parts;
     const int* slot_map;
 };
 
@@ -60,47 +61,6 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// The bounded wait of war_sm100_prims.cuh in a dozen instructions (the main loops stand in the instruction cache, and a
-// tile has eight waits): gives up after kWaitBudgetNs or when another waiter of the CTA has.
-__device__ __forceinline__ uint32_t timer_lo() {
-    uint32_t t;
-    asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
-    return t;
-}
-// mbarrier.try_wait with a time hint: the warp is suspended until the phase completes or about that time has passed.
-__device__ __forceinline__ bool mbar_try_wait_long(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(1000000u) : "memory");
-    return ok != 0;
-}
-template <class BarsT>
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, BarsT* bars, int* status_word) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const uint32_t t0 = timer_lo();
-    while (!mbar_try_wait_long(bar, parity)) {
-        if (*(volatile int*)&bars->abort_flag) return false;
-        if (timer_lo() - t0 > (uint32_t)kWaitBudgetNs) {
-            war_set_device_status(status_word, WAR_ERR_TIMEOUT);
-            *(volatile int*)&bars->abort_flag = 1;
-            return false;
-        }
-    }
-    return true;
-}
-
-// One arrival for a whole warp: 32 lanes arriving on one barrier queue up behind each other.
-__device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar);
-}
-
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
-                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
-}
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
@@ -111,9 +71,6 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
 }
 __device__ __forceinline__ void st_shared8(uint32_t at, uint32_t x, uint32_t y) {
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
-}
-__device__ __forceinline__ void st_shared16(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
 // the larger magnitude of two packed bf16, as bits
@@ -185,7 +142,7 @@ inline bool quant_kernel_args(const void* q, const AttnQuantPools& pools, const 
     a->page_shift = log2_of(p->page_size); a->block_shift = log2_of(pools.block); a->bpp_shift = a->page_shift - a->block_shift;
     a->kv_e5m2 = pools.kv == kKvE5M2;
     a->num_nodes = num_nodes; a->parent = parent; a->B = p->B; a->call = fused ? war_attn_next_call() : 0;
-    a->shared_units = nullptr; a->slot_map = nullptr;
+    a->shared_units = nullptr; a->shared_parts = nullptr; a->slot_map = nullptr;
     return true;
 }
 

@@ -1,5 +1,5 @@
 // Parts of the tensor-core verify attention that do not depend on the cache's type: ancestor masks, the counting of split
-// units' partial results and their merge, the tensor-map encoder (library-internal, device code).
+// units' partial results and their merge, tensor maps (library-internal, device code).
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -18,12 +18,58 @@ using namespace sm100;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// The bounded wait of war_sm100_prims.cuh in a dozen instructions (the main loops stand in the instruction cache, and a
+// tile has eight waits): gives up after kWaitBudgetNs or when another waiter of the CTA has.
+__device__ __forceinline__ uint32_t timer_lo() {
+    uint32_t t;
+    asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
+    return t;
+}
+// mbarrier.try_wait with a time hint: the warp is suspended until the phase completes or about that time has passed.
+__device__ __forceinline__ bool mbar_try_wait_long(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(1000000u) : "memory");
+    return ok != 0;
+}
+template <class BarsT>
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, BarsT* bars, int* status_word) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint32_t t0 = timer_lo();
+    while (!mbar_try_wait_long(bar, parity)) {
+        if (*(volatile int*)&bars->abort_flag) return false;
+        if (timer_lo() - t0 > (uint32_t)kWaitBudgetNs) {
+            war_set_device_status(status_word, WAR_ERR_TIMEOUT);
+            *(volatile int*)&bars->abort_flag = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+// One arrival for a whole warp: 32 lanes arriving on one barrier queue up behind each other.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+}
+
+__device__ __forceinline__ void st_shared16(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+
 // What the three roles need to know about a unit, wherever the plan lives.
 struct UnitView {
     int req, kvh, rb, tile_begin, tile_end, n_chunks, chunk, n_nodes;
     int slot;                            // index of this unit's partial in the workspace
     int slot_base, slot_stride, bump;    // fused-plan variant: partial of chunk c is slot_base + c * slot_stride (+ bump for c == 0)
-    int page0, n_keys, visible, rows, slot0, part0;      // shared-prefix variant: see SharedUnit
+    int page0, n_keys, visible, rows, slot0, part0, part_rows;      // shared-prefix variant: see SharedUnit (rows: end of the unit's rows)
 };
 
 // Ancestor-or-self bit masks of one tree, by one warp: lane l holds slots l and l + 32.  After round r a slot's mask
@@ -251,6 +297,28 @@ EncodeTiledFn encode_tiled_fn() {
         fn = (EncodeTiledFn)p;
     }
     return fn;
+}
+
+// A head-major pool [num_pages, Hkv, page_size, 128] bf16 seen as blocks of (page, head): [blocks][token/8][d/64][token%8][d%64].
+// A token-major pool (page, token, head, d) seen as (d, token, head, page) with a box of 64 dims x all tokens of one head.
+bool make_pool_map(CUtensorMap* map, const void* pool, long long num_pages, int Hkv, int page_size, int token_major) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    if (token_major) {
+        const cuuint64_t dims[4] = {128, (cuuint64_t)page_size, (cuuint64_t)Hkv, (cuuint64_t)num_pages};
+        const cuuint64_t strides[3] = {(cuuint64_t)Hkv * 256, 256, (cuuint64_t)page_size * Hkv * 256};
+        const cuuint32_t box[4] = {64, (cuuint32_t)page_size, 1, 1};
+        return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
+    const cuuint64_t dims[5] = {64, 8, 2, (cuuint64_t)(page_size / 8), (cuuint64_t)(num_pages * Hkv)};
+    const cuuint64_t strides[4] = {256, 128, 2048, (cuuint64_t)page_size * 256};
+    const cuuint32_t box[5] = {64, 8, 2, (cuuint32_t)(page_size / 8), 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(pool), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace

@@ -133,10 +133,11 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         const int u = unit_at(cur.k++);
         if (u >= n_units) return false;
         if (kShared) {
-            const SharedUnit x = a.shared_units[u];
-            un.req = x.req; un.kvh = x.kvh; un.rb = x.rb; un.tile_begin = x.tile_begin; un.tile_end = x.tile_end;
-            un.n_chunks = x.whole ? 1 : 2; un.chunk = 0; un.n_nodes = 0;
-            un.page0 = x.page0; un.n_keys = x.n_keys; un.visible = x.visible; un.rows = x.rows; un.slot0 = x.slot0; un.part0 = x.part0;
+            const SharedUnit x = shared_unit(a.shared_units, a.shared_parts, u, a.Hkv, kRowBlock);
+            un.req = x.part.req; un.kvh = x.kvh; un.rb = x.row0 / kRowBlock; un.tile_begin = x.tile_begin; un.tile_end = x.tile_end;
+            un.n_chunks = x.part.whole ? 1 : 2; un.chunk = 0; un.n_nodes = x.part.n_keys - x.part.visible;
+            un.page0 = x.part.page0; un.n_keys = x.part.n_keys; un.visible = x.part.visible; un.rows = x.row0 + x.rows;
+            un.slot0 = x.part.slot0; un.part0 = x.part0; un.part_rows = x.part.rows;
             return true;
         }
         const AttnUnit x = a.w.units[u];
@@ -391,7 +392,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             // below, by every warp that is about to use it (all come to the same verdict).  Its parent row is
             // requested here, ahead of the Q rows, and looked at after them.
             int q0 = 0, q1 = 0;
-            if (kFused) {
+            if (kFused || (kShared && un.slot0 < 0)) {
                 const int32_t* prow = a.parent + (size_t)i * a.N;
                 q0 = lane < a.N ? prow[lane] : 0; q1 = lane + 32 < a.N ? prow[lane + 32] : 0;
             }
@@ -455,8 +456,11 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
             if (kFused) {
                 anc = tree_ok ? warp_ancestor_mask(q0, q1, n, j, lane) : 0ull;
                 if (!valid) anc = 0ull;
+            } else if (kShared) {
+                anc = un.slot0 < 0 ? warp_ancestor_mask(q0, q1, n, j, lane) : 0ull;      // (the plan has looked at the tree)
+                if (!valid) anc = 0ull;
             } else {
-                anc = valid && !(kShared && un.slot0 >= 0) ? a.w.anc[slot_row] : 0ull;
+                anc = valid ? a.w.anc[(size_t)i * a.N + j] : 0ull;
             }
             float m_used = -CUDART_INF_F, l = 0.f;
             float v_ref = 1.f;                                             // power of two that V's scales are taken relative to
@@ -619,13 +623,14 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
                     const float f1 = (m1 == -CUDART_INF_F ? 0.f : exp2f(m1 - M)) * st_w[128 + row] * norm;
                     const bool use1 = theirs > 0;                          // uniform: O of group 1 is stale when it had no tile
                     __nv_bfloat16* const out = a.out + qrow * 128;
-                    const size_t part_row = kShared ? (size_t)un.part0 + r_l : (size_t)un.slot * a.w.rows + r_l;
-                    float* const part = split ? a.w.part_o + part_row * 128 : nullptr;
+                    const size_t part_row = kShared ? (size_t)un.part0 + gr : (size_t)un.slot * a.w.rows + r_l;
+                    // (shared-prefix variant: pieces of four columns, see SharedUnit)
+                    float* const part = !split ? nullptr : kShared ? a.w.part_o + ((size_t)un.part0 * 32 + gr) * 4 : a.w.part_o + part_row * 128;
                     auto store8 = [&](int col, const float* x) {           // eight columns of this row
                         if (split) {
-                            float4* dst = reinterpret_cast<float4*>(part + col);
+                            float4* dst = reinterpret_cast<float4*>(kShared ? part + (size_t)col * un.part_rows : part + col);
                             dst[0] = make_float4(x[0], x[1], x[2], x[3]);
-                            dst[1] = make_float4(x[4], x[5], x[6], x[7]);
+                            dst[kShared ? un.part_rows : 1] = make_float4(x[4], x[5], x[6], x[7]);
                         } else {
                             uint32_t w4[4];
 #pragma unroll
@@ -812,7 +817,7 @@ war_status_t war_attn_quant_launch_many(const void* q, const AttnQuantPools& poo
     return WAR_OK;
 }
 
-war_status_t war_attn_quant_launch_shared(const void* q, const AttnQuantPools& pools, const int32_t* page_table,
+war_status_t war_attn_quant_launch_shared(const void* q, const AttnQuantPools& pools, const int32_t* page_table, const int32_t* parent,
                                           const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse,
                                           int* status_word, cudaStream_t s) {
     int dev = 0;
@@ -823,12 +828,12 @@ war_status_t war_attn_quant_launch_shared(const void* q, const AttnQuantPools& p
     const int grid = war_attn_sm_count();
     if (grid <= 0) return WAR_ERR_CUDA;
     AttnWorkspace parts{};
-    parts.counters = w.counters; parts.anc = w.anc; parts.part_ml = w.part_ml; parts.part_o = w.part_o;
+    parts.counters = w.counters; parts.part_ml = w.part_ml; parts.part_o = w.part_o;
     CUtensorMap k_map, v_map;
     QuantKernelArgs a;
-    if (!quant_kernel_args(q, pools, page_table, nullptr, nullptr, nullptr, p, parts, false, out, lse, status_word, &a, &k_map, &v_map))
+    if (!quant_kernel_args(q, pools, page_table, nullptr, nullptr, parent, p, parts, false, out, lse, status_word, &a, &k_map, &v_map))
         return WAR_ERR_UNSUPPORTED;
-    a.shared_units = w.units; a.slot_map = w.slot_map;
+    a.shared_units = w.units; a.shared_parts = w.parts; a.slot_map = w.slot_map;
     attn_quant_many_kernel<false, true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
     WAR_LAUNCH_CHECK();
     return WAR_OK;

@@ -9,7 +9,6 @@
 #include <mutex>
 #include "war_common.cuh"
 #include "war_attn_shared.cuh"
-#include "war_attn_fused_plan.cuh"
 #include "war_attn_quant.cuh"
 #include "war_quant.cuh"
 
@@ -17,16 +16,9 @@ namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPlanThreads = 1024;
-constexpr int kSearchMaxB = 64;           // up to this many requests the chunk length is searched
-
-__device__ __forceinline__ uint64_t shfl64(uint64_t v, int src) {
-    const uint32_t lo = __shfl_sync(0xffffffffu, (uint32_t)v, src);
-    const uint32_t hi = __shfl_sync(0xffffffffu, (uint32_t)(v >> 32), src);
-    return ((uint64_t)hi << 32) | lo;
-}
 
 // Exclusive scan of x over the block, and the sum.  Contains block barriers.
-__device__ __forceinline__ int block_scan(int x, int* warp_sums, int* total) {
+__device__ __forceinline__ int block_scan(int x, int* warp_sums, int n_warps, int* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int incl = x;
 #pragma unroll
@@ -34,7 +26,7 @@ __device__ __forceinline__ int block_scan(int x, int* warp_sums, int* total) {
     if (lane == 31) warp_sums[warp] = incl;
     __syncthreads();
     if (warp == 0) {
-        const int y = warp_sums[lane];
+        const int y = lane < n_warps ? warp_sums[lane] : 0;
         int yi = y;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const int z = __shfl_up_sync(0xffffffffu, yi, o); if (lane >= o) yi += z; }
@@ -48,23 +40,13 @@ __device__ __forceinline__ int block_scan(int x, int* warp_sums, int* total) {
     return before + incl - x;
 }
 
-// Exclusive scan of n numbers in shared memory, in place; returns the sum.
-__device__ __forceinline__ int scan_array(int* a, int n, int* warp_sums) {
-    const int per = (n + kPlanThreads - 1) / kPlanThreads, b0 = min(n, (int)threadIdx.x * per), b1 = min(n, b0 + per);
-    int sum = 0, total;
-    for (int q = b0; q < b1; ++q) sum += a[q];
-    int run = block_scan(sum, warp_sums, &total);
-    for (int q = b0; q < b1; ++q) { const int x = a[q]; a[q] = run; run += x; }
-    __syncthreads();
-    return total;
-}
-
 struct PlanArrays {                       // dynamic shared memory of the planning kernel, E = B + B / 2 parts
-    int *tiles, *rows, *units, *part;     // [E]; units and part by position, then their exclusive scans
+    int *tiles, *rows, *units;            // [E]; units: cost of a part's longest unit
     int *members, *group_rows, *first;    // [B] by leader: running members, their rows, the lowest of them
+    int *first_unit;                      // [E] units before each position; where members and group_rows were
     int *slots;                           // [B] by leader: first entry in slot_map
-    int *shared;                          // [B] by request: keys that it shares with its group (0: none)
-    uint16_t *order;                      // [E] part at each position
+    int *prefix, *shared;                 // [B] prefix_len, shared_len
+    uint16_t *order, *nc;                 // [E] part at each position; chunks of a part
     uint16_t *leader, *group;             // [B]; number of the group by leader
     uint16_t *lead;                       // [B / 2] leader by number of the group
     uint8_t *n;                           // [B] validated slot count
@@ -73,78 +55,79 @@ __host__ __device__ inline size_t plan_arrays(PlanArrays* a, uint8_t* base, int 
     const int E = B + B / 2 + 4;
     size_t at = 0;
     auto take = [&](size_t bytes) { uint8_t* p = base + at; at += (bytes + 15) & ~(size_t)15; return p; };
-    a->tiles = (int*)take(4 * E); a->rows = (int*)take(4 * E); a->units = (int*)take(4 * E); a->part = (int*)take(4 * E);
-    a->members = (int*)take(4 * B); a->group_rows = (int*)take(4 * B); a->first = (int*)take(4 * B); a->slots = (int*)take(4 * B);
-    a->shared = (int*)take(4 * B);
-    a->order = (uint16_t*)take(2 * E); a->leader = (uint16_t*)take(2 * B); a->group = (uint16_t*)take(2 * B);
+    a->tiles = (int*)take(4 * E); a->rows = (int*)take(4 * E); a->units = (int*)take(4 * E);
+    a->members = a->first_unit = (int*)take(4 * (2 * B > E ? 2 * B : E)); a->group_rows = a->members + B;
+    a->first = (int*)take(4 * B); a->slots = (int*)take(4 * B);
+    a->prefix = (int*)take(4 * B); a->shared = (int*)take(4 * B);
+    a->order = (uint16_t*)take(2 * E); a->nc = (uint16_t*)take(2 * E); a->leader = (uint16_t*)take(2 * B); a->group = (uint16_t*)take(2 * B);
     a->lead = (uint16_t*)take(2 * (B / 2 + 1)); a->n = (uint8_t*)take(B);
     return at;
 }
 
-__device__ __forceinline__ int row_blocks_of(int rows) { return (rows + kRowBlock - 1) / kRowBlock; }
+constexpr int kNobody = 0xffff;
+constexpr int kMaxChunks = 0x7fff;
+constexpr int kMinChunkCost = 4;          // tiles of one row block
 
-// One block.  Trees and groups are checked, parts are laid out, cut into chunks and dealt as in attn_plan_kernel (longest part
-// first; up to 64 requests the chunk length is searched).
-__global__ void __launch_bounds__(kPlanThreads)
+// One block.  Trees and groups are checked, parts are laid out and cut into chunks.  The time of a part's tile counts 1, or 2 where two
+// row blocks of 128 rows work on it together.  A chunk costs C = max(4, sqrt(6 * all / CTAs), all / kTargetUnits): smaller ones pay for
+// more units (about four tiles each), larger ones for a longer tail.  The units are sorted, the longest first.
+__global__ void __launch_bounds__(kPlanThreads)                    // (a quarter of the threads for small batches: barriers are cheaper)
 attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ num_nodes, const int32_t* __restrict__ parent,
                         const int32_t* __restrict__ leader, const int32_t* __restrict__ shared_len, int B, int N, int Hkv, int G,
-                        int page_size, int max_pages, int n_ctas, SharedWorkspace w, int* status_word) {
+                        int page_size, int max_pages, int n_ctas, int block, SharedWorkspace w, int* status_word) {
     extern __shared__ __align__(16) uint8_t plan_smem[];
-    __shared__ int s_warp[33], s_keys[64], s_tmax;
+    __shared__ int s_warp[33];
     __shared__ long long s_sum[32];
     PlanArrays a;
     plan_arrays(&a, plan_smem, B);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) s_tmax = 0;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_threads = blockDim.x, n_warps = n_threads >> 5;
+    auto row_blocks_of = [block](int rows) -> int { return (rows + block - 1) / block; };
+    auto tile_cost = [](int rows) -> int { return rows > kRowBlock ? 2 : 1; };
 
-    // ---- per request, one warp: the tree (lane l holds slots l and l + 32; pointer jumping: after round r a slot's mask covers its
-    // 2^r nearest ancestors-or-self) ----
-    for (int i = warp; i < B; i += 32) {
-        const int j0 = lane, j1 = lane + 32;
-        const int32_t* prow = parent + (size_t)i * N;
-        int p0 = j0 < N ? prow[j0] : 0, p1 = j1 < N ? prow[j1] : 0, n = num_nodes[i];
-        const int pl = prefix_len[i];
-        const bool bad_l = (j0 > 0 && j0 < n && (p0 < 0 || p0 >= j0)) || (j1 < n && (p1 < 0 || p1 >= j1));
-        bool bad = n < 0 || n > N || pl < 0;
-        bad = bad || __any_sync(0xffffffffu, bad_l);
-        if (bad) { if (lane == 0) war_set_device_status(status_word, WAR_ERR_BAD_TREE); n = 0; }
-        if (n > 0 && (long long)pl + n > (long long)max_pages * page_size) {
-            if (lane == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
-            n = 0;
-        }
-        if (n > 0) {
-            if (j0 == 0 || j0 >= n) p0 = 0;
-            if (j1 >= n) p1 = 0;
-            uint64_t a0 = 1ull << j0, a1 = 1ull << j1;
-#pragma unroll 1
-            for (int r = 1; r < n; r <<= 1) {
-                const uint64_t b00 = shfl64(a0, p0 & 31), b01 = shfl64(a1, p0 & 31), b10 = shfl64(a0, p1 & 31), b11 = shfl64(a1, p1 & 31);
-                const int q00 = __shfl_sync(0xffffffffu, p0, p0 & 31), q01 = __shfl_sync(0xffffffffu, p1, p0 & 31);
-                const int q10 = __shfl_sync(0xffffffffu, p0, p1 & 31), q11 = __shfl_sync(0xffffffffu, p1, p1 & 31);
-                a0 |= p0 >= 32 ? b01 : b00;
-                a1 |= p1 >= 32 ? b11 : b10;
-                p0 = p0 >= 32 ? q01 : q00;
-                p1 = p1 >= 32 ? q11 : q10;
-            }
-            if (j0 < n) w.anc[(size_t)i * N + j0] = a0;
-            if (j1 < n) w.anc[(size_t)i * N + j1] = a1;
-        }
-        if (lane == 0) a.n[i] = (uint8_t)n;
+    for (int i = tid; i < B; i += n_threads) {
+        const int l = leader[i];
+        a.leader[i] = l >= 0 && l < B ? (uint16_t)l : (uint16_t)kNobody;
+        a.shared[i] = shared_len[i];
+        a.members[i] = 0; a.group_rows[i] = 0; a.first[i] = B;
     }
-    for (int i = tid; i < B; i += kPlanThreads) { a.members[i] = 0; a.group_rows[i] = 0; a.first[i] = B; }
+    // ---- per request, one warp: is the tree one?  (lane l holds slots l and l + 32).  Four requests are asked for at a time: a warp
+    // waits once for memory, not four times.  What a slot sees is worked out by the warps that use it (200 trees' ancestors take
+    // one SM 16 thousand cycles). ----
+    const int j0 = lane, j1 = lane + 32;
+    for (int i0 = warp; i0 < B; i0 += 4 * n_warps) {
+        int q0[4], q1[4], nn[4], pf[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + n_warps * k;
+            const int32_t* prow = parent + (size_t)i * N;
+            q0[k] = i < B && j0 < N ? prow[j0] : 0; q1[k] = i < B && j1 < N ? prow[j1] : 0;
+            nn[k] = i < B ? num_nodes[i] : 0; pf[k] = i < B ? prefix_len[i] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + n_warps * k;
+            int n = nn[k];
+            const bool bad_l = (j0 > 0 && j0 < n && (q0[k] < 0 || q0[k] >= j0)) || (j1 < n && (q1[k] < 0 || q1[k] >= j1));
+            const bool bad = __any_sync(0xffffffffu, bad_l) || n < 0 || n > N || pf[k] < 0;
+            if (lane == 0 && i < B) {
+                if (bad) { war_set_device_status(status_word, WAR_ERR_BAD_TREE); n = 0; }
+                if (n > 0 && (long long)pf[k] + n > (long long)max_pages * page_size) { war_set_device_status(status_word, WAR_ERR_BAD_PAGE); n = 0; }
+                a.n[i] = (uint8_t)n; a.prefix[i] = pf[k];
+            }
+        }
+    }
     __syncthreads();
 
     // ---- groups: members behind their leader, then the leader itself (its shared_len does not count when it is alone) ----
-    auto shares = [&](int l) -> int { return shared_len[l] / page_size * page_size; };
+    auto shares = [&](int l) -> int { return a.shared[l] / page_size * page_size; };
     for (int pass = 0; pass < 2; ++pass) {
-        for (int i = tid; i < B; i += kPlanThreads) {
+        for (int i = tid; i < B; i += n_threads) {
             if (a.n[i] == 0) continue;
-            const int l = leader[i];
+            const int l = a.leader[i];
             if ((l == i) != (pass == 1)) continue;
-            bool ok = l >= 0 && l < B && leader[l] == l;
-            if (ok && (pass == 0 || a.members[i] > 0)) ok = shared_len[l] >= 0 && shares(l) <= prefix_len[i];
+            bool ok = l != kNobody && a.leader[l] == l;
+            if (ok && (pass == 0 || a.members[i] > 0)) ok = a.shared[l] >= 0 && shares(l) <= a.prefix[i];
             if (!ok) { war_set_device_status(status_word, WAR_ERR_INVALID_ARG); a.n[i] = 0; continue; }
-            a.leader[i] = (uint16_t)l;
             atomicAdd(&a.members[l], 1);
             atomicAdd(&a.group_rows[l], G * a.n[i]);
             atomicMin(&a.first[l], i);
@@ -153,158 +136,173 @@ attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* _
     }
     // ---- number of every group that shares something, its place in slot_map, its part ----
     int groups = 0, slots = 0;
-    for (int i0 = 0; i0 < B; i0 += kPlanThreads) {
+    for (int i0 = 0; i0 < B; i0 += n_threads) {
         const int i = i0 + tid;
         const bool active = i < B && a.members[i] >= 2 && shares(i) > 0;
-        int more, more_slots;
-        const int g = groups + block_scan(active ? 1 : 0, s_warp, &more);
-        const int at = slots + block_scan(active ? a.group_rows[i] / G : 0, s_warp, &more_slots);
-        if (i < B) a.group[i] = active ? (uint16_t)g : (uint16_t)0xffff;
+        int both;                                                            // groups << 20 | slots (at most 2^18 in all)
+        const int before = block_scan(active ? (1 << 20) + a.group_rows[i] / G : 0, s_warp, n_warps, &both);
+        const int g = groups + (before >> 20);
+        if (i < B) a.group[i] = active ? (uint16_t)g : (uint16_t)kNobody;
         if (active) {
-            a.slots[i] = at;
+            a.slots[i] = slots + (before & 0xfffff);
             a.tiles[B + g] = (shares(i) + kTileKeys - 1) / kTileKeys;
             a.rows[B + g] = a.group_rows[i];
             a.lead[g] = (uint16_t)i;
         }
-        groups += more; slots += more_slots;
+        groups += both >> 20; slots += both & 0xfffff;
     }
     __syncthreads();
     const int E = B + groups;
-    for (int i = tid; i < B; i += kPlanThreads) {
+    for (int i = tid; i < B; i += n_threads) {
         const int n = a.n[i];
+        int sh = 0;
         SharedReq rq;
         rq.n = n; rq.group = -1; rq.row0 = 0; rq.pad = 0;
-        int sh = 0;
-        if (n > 0 && a.group[a.leader[i]] != 0xffff) {
+        if (n > 0 && a.group[a.leader[i]] != kNobody) {
             const int l = a.leader[i];
             sh = shares(l);
             int before = 0;                                                  // slots of the members before this one
-            for (int q = a.first[l]; q < i; ++q) if (a.n[q] > 0 && a.leader[q] == l) before += a.n[q];
+#pragma unroll 4
+            for (int q = a.first[l]; q < i; ++q) before += a.leader[q] == l ? (int)a.n[q] : 0;
             rq.group = a.group[l]; rq.row0 = before * G;
             for (int j = 0; j < n; ++j) w.slot_map[a.slots[l] + before + j] = i * N + j;
         }
         w.reqs[i] = rq;
-        a.shared[i] = sh;
-        a.tiles[i] = n > 0 ? (prefix_len[i] - sh + n + kTileKeys - 1) / kTileKeys : 0;
+        a.tiles[i] = n > 0 ? (a.prefix[i] - sh + n + kTileKeys - 1) / kTileKeys : 0;
         a.rows[i] = G * n;
     }
     __syncthreads();
 
-    // ---- chunk length ----
+    // ---- cost of a chunk ----
     long long mine = 0;
-    int t_mine = 0;
-    for (int e = tid; e < E; e += kPlanThreads) { mine += (long long)a.tiles[e] * row_blocks_of(a.rows[e]); t_mine = max(t_mine, a.tiles[e]); }
+    for (int e = tid; e < E; e += n_threads) mine += (long long)a.tiles[e] * row_blocks_of(a.rows[e]) * tile_cost(min(a.rows[e], block));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    t_mine = __reduce_max_sync(0xffffffffu, t_mine);
-    if (lane == 0) { s_sum[warp] = mine; atomicMax(&s_tmax, t_mine); }
+    if (lane == 0) s_sum[warp] = mine;
     __syncthreads();
-    long long tot = 0;
-    for (int k = 0; k < kPlanThreads / 32; ++k) tot += s_sum[k];
-    tot *= Hkv;
-    int chunk = (int)max((long long)kMinChunkTiles, (tot + kTargetUnits - 1) / kTargetUnits);
-    const int t_max = s_tmax;
-    if (B <= kSearchMaxB) {
-        int* const weight = a.units;                                         // (idle until the order is known)
-        for (int e = tid; e < E + 4; e += kPlanThreads) {
-            weight[e] = e < E && a.tiles[e] > 0 ? Hkv * row_blocks_of(a.rows[e]) : 0;
-            if (e >= E) a.tiles[e] = 0;
-        }
-        __syncthreads();
-        chunk = fused_plan::chunk_search<kFusedThreads>(a.tiles, weight, E, max(fused_plan::chunk_floor(t_max), chunk), t_max, n_ctas, s_keys);
-        __syncthreads();
+    long long all = lane < n_warps ? s_sum[lane] : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    all *= Hkv;
+    const long long least = (all + kTargetUnits - 1) / kTargetUnits;
+    const int chunk = (int)max(max((long long)kMinChunkCost, least), (long long)sqrtf(6.f * (float)all / (float)n_ctas));
+    // chunks of a part and the cost of the longest of them, for the order
+    for (int e = tid; e < E; e += n_threads) {
+        const int t = a.tiles[e], cost = tile_cost(min(a.rows[e], block)), nc = min((t * cost + chunk - 1) / chunk, min(t, kMaxChunks));
+        a.nc[e] = (uint16_t)nc;
+        a.units[e] = nc > 0 ? (t + nc - 1) / nc * cost : 0;
     }
-    auto chunks_of = [&](int t) -> int { return (t + chunk - 1) / chunk; };
+    __syncthreads();
 
-    // ---- longest first; units and rows of partial results by position ----
-    for (int e = tid; e < E; e += kPlanThreads) {
-        const int t = a.tiles[e];
-        int pos = 0;
-        for (int q = 0; q < E; ++q) pos += (a.tiles[q] > t) || (a.tiles[q] == t && q < e);
-        const int nc = chunks_of(t);
-        a.order[pos] = (uint16_t)e;
-        a.units[pos] = nc * Hkv * row_blocks_of(a.rows[e]);
-        a.part[pos] = nc * Hkv * a.rows[e];
+    // ---- longest first: a part's place is the number of parts in front of it, a warp each ----
+    for (int e = warp; e < E; e += n_warps) {
+        const int c = a.units[e];
+        int before = 0;
+        for (int q = lane; q < E; q += 32) before += a.units[q] > c || (a.units[q] == c && q < e);
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) a.order[before] = (uint16_t)e;
     }
     __syncthreads();
-    const int total = scan_array(a.units, E, s_warp);
-    scan_array(a.part, E, s_warp);
-    if (tid == 0) { w.counters[1] = total; w.counters[3] = 0; }
-    for (int pos = tid; pos < E; pos += kPlanThreads) {
-        const int e = a.order[pos];
+    // ---- units and rows of partial results before every part; the parts ----
+    int units = 0, rows_before = 0;
+    for (int p0 = 0; p0 < E; p0 += n_threads) {
+        const int pos = p0 + tid;
+        int u = 0, r = 0, e = 0;
+        if (pos < E) { e = a.order[pos]; u = a.nc[e] * Hkv * row_blocks_of(a.rows[e]); r = a.nc[e] * Hkv * a.rows[e]; }
+        int u_all, r_all;
+        const int u0 = units + block_scan(u, s_warp, n_warps, &u_all), r0 = rows_before + block_scan(r, s_warp, n_warps, &r_all);
+        units += u_all; rows_before += r_all;
+        if (pos >= E) continue;
+        a.first_unit[pos] = u0;
+        const int t = a.tiles[e], nc = a.nc[e];
         SharedPart x;
-        x.part0 = a.part[pos]; x.n_chunks = chunks_of(a.tiles[e]); x.rows = a.rows[e]; x.n_tiles = a.tiles[e];
-        w.parts[e] = x;
-    }
-    // ---- unit table, one thread per unit: (chunk, kv head, row block) ----
-    for (int u = tid; u < total; u += kPlanThreads) {
-        int lo = 0, hi = E - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.units[mid] <= u) lo = mid; else hi = mid - 1;
-        }
-        const int e = a.order[lo], t = a.tiles[e], rows = a.rows[e], nc = chunks_of(t), rbs = row_blocks_of(rows);
-        const int local = u - a.units[lo], c = local / (Hkv * rbs), rem = local % (Hkv * rbs);
-        SharedUnit x;
-        x.kvh = rem / rbs; x.rb = rem % rbs;
-        x.tile_begin = (int)((long long)t * c / nc); x.tile_end = (int)((long long)t * (c + 1) / nc);
-        x.rows = rows;
-        x.part0 = a.part[lo] + (c * Hkv + x.kvh) * rows + x.rb * kRowBlock;
+        x.part0 = r0; x.n_chunks = nc; x.rows = a.rows[e];
+        x.each = nc > 0 ? t / nc : 0; x.more = t - x.each * nc;
         if (e < B) {
-            x.req = e; x.page0 = a.shared[e] / page_size;
-            x.visible = prefix_len[e] - a.shared[e]; x.n_keys = x.visible + a.n[e];
-            x.slot0 = -1; x.whole = nc == 1 && a.shared[e] == 0;
+            const int l = a.leader[e], sh = a.n[e] > 0 && a.group[l] != kNobody ? shares(l) : 0;
+            x.req = e; x.page0 = sh / page_size;
+            x.visible = a.prefix[e] - sh; x.n_keys = x.visible + a.n[e];
+            x.slot0 = -1; x.whole = nc == 1 && sh == 0;
         } else {
             const int l = a.lead[e - B];
             x.req = a.first[l]; x.page0 = 0;
             x.visible = x.n_keys = shares(l);
             x.slot0 = a.slots[l]; x.whole = 0;
         }
-        w.units[u] = x;
+        x.pad = 0;
+        w.parts[e] = x;
+    }
+    if (tid == 0) { w.counters[0] = 0; w.counters[1] = units; w.counters[3] = 0; }
+    __syncthreads();
+    // ---- unit table: (chunk, kv head, row block), a thread each ----
+    for (int u = tid; u < units; u += n_threads) {
+        int lo = 0, hi = E - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (a.first_unit[mid] <= u) lo = mid; else hi = mid - 1;
+        }
+        const unsigned e = a.order[lo], rbs = (unsigned)row_blocks_of(a.rows[e]), local = (unsigned)(u - a.first_unit[lo]);
+        const unsigned c = local / (Hkv * rbs), rem = local - c * (Hkv * rbs), h = rem / rbs;
+        w.units[u] = make_uint2(e | (c << 16), h | ((rem - h * rbs) << 16));
     }
 }
 
-// One warp per output row: the chunks of the group's part, then those of the request's own, in this order (results do not depend
-// on timing).  Lanes first reduce the chunks' maxima, then stream their rows, float4 a lane.
-constexpr int kMergeWarps = 4;
+// A warp merges eight rows of one (request, kv head), half of the columns, four lanes a row: the chunks of the group's part, then those of
+// the request's own, in this order (results do not depend on timing), each folded in as it comes.  The lanes of a row take every fourth
+// piece of four columns.
+constexpr int kMergeWarps = 8;
 __global__ void __launch_bounds__(kMergeWarps * 32)
 attn_shared_merge_kernel(SharedWorkspace w, int B, int N, int Hq, int Hkv, int G, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
-    const int i = blockIdx.x / Hkv, kvh = blockIdx.x % Hkv;
+    const int i = blockIdx.x / Hkv, kvh = blockIdx.x - i * Hkv;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r = (blockIdx.y * (kMergeWarps / 2) + (warp >> 1)) * 8 + (lane & 7), c0 = (warp & 1) * 16 + (lane >> 3);
     const SharedReq rq = w.reqs[i];
     const SharedPart own = w.parts[i];
-    const int lane = threadIdx.x & 31, r = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
-    if (r >= G * rq.n || (rq.group < 0 && own.n_chunks <= 1)) return;
-    SharedPart grp{0, 0, 0, 0};
-    if (rq.group >= 0) grp = w.parts[B + rq.group];
-    const int n_chunks = grp.n_chunks + own.n_chunks;
-    auto at = [&](int c) -> size_t {
-        if (c < grp.n_chunks) return (size_t)grp.part0 + (size_t)(c * Hkv + kvh) * grp.rows + rq.row0 + r;
-        return (size_t)own.part0 + (size_t)((c - grp.n_chunks) * Hkv + kvh) * own.rows + r;
-    };
-    float M = -CUDART_INF_F;
-    for (int c = lane; c < n_chunks; c += 32) M = fmaxf(M, w.part_ml[at(c) * 2]);
+    if (r - (lane & 7) >= G * rq.n || (rq.group < 0 && own.n_chunks <= 1)) return;
+    const bool live = r < G * rq.n;
+    int g_chunks = 0, g_part0 = 0, g_rows = 0;
+    if (rq.group >= 0) { const SharedPart& g = w.parts[B + rq.group]; g_chunks = g.n_chunks; g_part0 = g.part0; g_rows = g.rows; }
+    const int rr = live ? r : 0;
+    float M = -CUDART_INF_F, l = 0.f;
+    float4 acc[4];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto fold = [&](int n, int part0, int rows, int row) {
+        const float2* ml = reinterpret_cast<const float2*>(w.part_ml) + part0 + (size_t)kvh * rows + row;
+        const float4* o = reinterpret_cast<const float4*>(w.part_o) + ((size_t)part0 + (size_t)kvh * rows) * 32 + (size_t)c0 * rows + row;
+        const size_t step = (size_t)Hkv * rows;
 #pragma unroll 4
-    for (int c = 0; c < n_chunks; ++c) {
-        const size_t base = at(c);
-        const float2 ml = *reinterpret_cast<const float2*>(w.part_ml + base * 2);
-        const float4 o = *reinterpret_cast<const float4*>(w.part_o + base * 128 + lane * 4);
-        const float sc = ml.x == -CUDART_INF_F ? 0.f : exp2f(ml.x - M);
-        l = fmaf(ml.y, sc, l);
-        acc.x = fmaf(o.x, sc, acc.x); acc.y = fmaf(o.y, sc, acc.y); acc.z = fmaf(o.z, sc, acc.z); acc.w = fmaf(o.w, sc, acc.w);
-    }
+        for (int c = 0; c < n; ++c, ml += step, o += step * 32) {
+            const float2 y = __ldcs(ml);
+            float4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = __ldcs(o + (size_t)(4 * k) * rows);
+            const float top = fmaxf(M, y.x);
+            const float keep = M == -CUDART_INF_F ? 0.f : exp2f(M - top), sc = y.x == -CUDART_INF_F ? 0.f : exp2f(y.x - top);
+            M = top;
+            l = fmaf(l, keep, y.y * sc);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                acc[k].x = fmaf(acc[k].x, keep, x[k].x * sc); acc[k].y = fmaf(acc[k].y, keep, x[k].y * sc);
+                acc[k].z = fmaf(acc[k].z, keep, x[k].z * sc); acc[k].w = fmaf(acc[k].w, keep, x[k].w * sc);
+            }
+        }
+    };
+    fold(g_chunks, g_part0, g_rows, rq.row0 + rr);
+    fold(own.n_chunks, own.part0, own.rows, rr);
+    if (!live) return;
     const float inv = 1.f / l;
-    const int j = r / G, g = r % G;
-    const size_t row = ((size_t)i * N + j) * Hq + kvh * G + g;
-    const __nv_bfloat162 h0 = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), h1 = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-    uint2 packed;
-    packed.x = *reinterpret_cast<const uint32_t*>(&h0);
-    packed.y = *reinterpret_cast<const uint32_t*>(&h1);
-    *reinterpret_cast<uint2*>(out + row * 128 + lane * 4) = packed;
-    if (lse && lane == 0) lse[row] = (M + log2f(l)) * kLn2;
+    const int j = r / G, g = r - j * G;
+    const size_t at = ((size_t)i * N + j) * Hq + kvh * G + g;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __nv_bfloat162 h0 = __floats2bfloat162_rn(acc[k].x * inv, acc[k].y * inv), h1 = __floats2bfloat162_rn(acc[k].z * inv, acc[k].w * inv);
+        uint2 packed;
+        packed.x = *reinterpret_cast<const uint32_t*>(&h0);
+        packed.y = *reinterpret_cast<const uint32_t*>(&h1);
+        *reinterpret_cast<uint2*>(out + at * 128 + (c0 + 4 * k) * 4) = packed;
+    }
+    if (lse && c0 == 0) lse[at] = (M + log2f(l)) * kLn2;
 }
 
 constexpr int kMaxDevices = 64;
@@ -351,7 +349,7 @@ war_status_t check_quant(const war_attn_quant_params_t* q) {
 }
 
 war_status_t launch_plan(const int32_t* prefix_len, const int32_t* num_nodes, const int32_t* parent, const int32_t* leader,
-                         const int32_t* shared_len, const war_attn_params_t* p, const SharedWorkspace& w, int* status_word, cudaStream_t s) {
+                         const int32_t* shared_len, const war_attn_params_t* p, int block, const SharedWorkspace& w, int* status_word, cudaStream_t s) {
     int dev = 0;
     WAR_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= kMaxDevices) return WAR_ERR_UNSUPPORTED;
@@ -360,15 +358,15 @@ war_status_t launch_plan(const int32_t* prefix_len, const int32_t* num_nodes, co
     const int n_sm = war_attn_sm_count();
     if (n_sm <= 0) return WAR_ERR_CUDA;
     PlanArrays a;
-    attn_shared_plan_kernel<<<1, kPlanThreads, plan_arrays(&a, nullptr, p->B), s>>>(prefix_len, num_nodes, parent, leader, shared_len, p->B, p->N,
+    attn_shared_plan_kernel<<<1, p->B <= 128 ? kPlanThreads / 4 : kPlanThreads, plan_arrays(&a, nullptr, p->B), s>>>(prefix_len, num_nodes, parent, leader, shared_len, p->B, p->N,
                                                                               p->Hkv, p->Hq / p->Hkv, p->page_size, p->max_pages_per_req,
-                                                                              n_sm, w, status_word);
+                                                                              n_sm, block, w, status_word);
     WAR_LAUNCH_CHECK();
     return WAR_OK;
 }
 war_status_t launch_merge(const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse, cudaStream_t s) {
     const int G = p->Hq / p->Hkv;
-    attn_shared_merge_kernel<<<dim3(p->B * p->Hkv, (G * p->N + kMergeWarps - 1) / kMergeWarps), kMergeWarps * 32, 0, s>>>(
+    attn_shared_merge_kernel<<<dim3(p->B * p->Hkv, (G * p->N + kMergeWarps * 4 - 1) / (kMergeWarps * 4)), kMergeWarps * 32, 0, s>>>(
         w, p->B, p->N, p->Hq, p->Hkv, G, (__nv_bfloat16*)out, lse);
     WAR_LAUNCH_CHECK();
     return WAR_OK;
@@ -395,9 +393,9 @@ extern "C" war_status_t war_verify_attn_shared(const void* d_q, const void* d_kp
     int* status_word = war_status_word();
     if (!status_word) return WAR_ERR_CUDA;
     const SharedWorkspace w = war_attn_shared_layout(p, d_workspace);
-    st = launch_plan(d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len, p, w, status_word, stream);
+    st = launch_plan(d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len, p, kSharedBlock, w, status_word, stream);
     if (st != WAR_OK) return st;
-    st = war_attn_launch_sm100_shared(d_q, d_kpool, d_vpool, d_page_table, p, w, d_out, d_lse, status_word, stream);
+    st = war_attn_shared_launch(d_q, d_kpool, d_vpool, d_page_table, d_parent, p, w, d_out, d_lse, status_word, stream);
     return st == WAR_OK ? launch_merge(p, w, d_out, d_lse, stream) : st;
 }
 
@@ -426,8 +424,8 @@ extern "C" war_status_t war_verify_attn_shared_quant(const void* d_q, const void
     for (int i = 0; i < 3; ++i) { pools.ks[i] = p->k_strides[i]; pools.vs[i] = p->v_strides[i]; }
     pools.kv = qp->kv_type; pools.block = qp->scale_block;
     const SharedWorkspace w = war_attn_shared_layout(p, d_workspace);
-    st = launch_plan(d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len, p, w, status_word, stream);
+    st = launch_plan(d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len, p, kSharedQuantBlock, w, status_word, stream);
     if (st != WAR_OK) return st;
-    st = war_attn_quant_launch_shared(d_q, pools, d_page_table, p, w, d_out, d_lse, status_word, stream);
+    st = war_attn_quant_launch_shared(d_q, pools, d_page_table, d_parent, p, w, d_out, d_lse, status_word, stream);
     return st == WAR_OK ? launch_merge(p, w, d_out, d_lse, stream) : st;
 }

@@ -33,7 +33,6 @@
 #include "war_attn_plan.cuh"
 #include "war_attn_fused_plan.cuh"
 #include "war_attn_sm100_parts.cuh"
-#include "war_attn_shared.cuh"
 
 namespace {
 using namespace sm100;
@@ -91,9 +90,6 @@ struct KernelArgs {
     const int32_t* parent;
     int B;
     unsigned long long call;             // number of this launch (48 bits, never 0)
-    // shared-prefix variant
-    const SharedUnit* shared_units;
-    const int* slot_map;
 };
 
 // kTokenMajor: pool layout, false = (page, head, token, d), true = (page, token, head, d).
@@ -101,9 +97,7 @@ struct KernelArgs {
 // units afterwards; true = every CTA works its own units out (war_attn_fused_plan.cuh), a spare warp counts the split
 // units whose partials are out, and once a CTA is through its units its softmax warps merge the split triples that
 // fall to it (waiting, with a bound, for their last chunk), so the call is one launch.
-// kShared (with kFused false): the plan is that of war_attn_shared.cuh; a unit's keys begin at a page of their own, and its rows may be
-// those of several requests.
-template <bool kTokenMajor, bool kFused, bool kShared = false>
+template <bool kTokenMajor, bool kFused>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const KernelArgs a) {
     extern __shared__ uint8_t smem_raw[];
@@ -118,7 +112,7 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     if (!kFused) {
         n_units = a.w.counters[1];
         // k-th unit of this CTA: its own contiguous list, or the snake deal of the longest-first list
-        contiguous = !kShared && a.w.counters[3] != 0 && gridDim.x <= (unsigned)kMaxPlanCtas;
+        contiguous = a.w.counters[3] != 0 && gridDim.x <= (unsigned)kMaxPlanCtas;
         list_first = contiguous ? a.w.cta_first[blockIdx.x] : 0; list_end = contiguous ? a.w.cta_first[blockIdx.x + 1] : 0;
     }
     auto unit_at = [&](int k) -> int {
@@ -138,13 +132,6 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         }
         const int u = unit_at(cur.k++);
         if (u >= n_units) return false;
-        if (kShared) {
-            const SharedUnit x = a.shared_units[u];
-            un.req = x.req; un.kvh = x.kvh; un.rb = x.rb; un.tile_begin = x.tile_begin; un.tile_end = x.tile_end;
-            un.n_chunks = x.whole ? 1 : 2; un.chunk = 0; un.n_nodes = 0;
-            un.page0 = x.page0; un.n_keys = x.n_keys; un.visible = x.visible; un.rows = x.rows; un.slot0 = x.slot0; un.part0 = x.part0;
-            return true;
-        }
         const AttnUnit x = a.w.units[u];
         un.req = x.req; un.kvh = x.kvh; un.rb = x.rb; un.tile_begin = x.tile_begin; un.tile_end = x.tile_end;
         un.n_chunks = x.n_chunks; un.chunk = x.chunk; un.n_nodes = a.w.req[x.req].n_nodes;
@@ -203,9 +190,9 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             UnitView un;
             if (!fetch(cur, un)) break;
             const int i = un.req;
-            const int L = kShared ? un.n_keys : a.prefix_len[i] + un.n_nodes;
+            const int L = a.prefix_len[i] + un.n_nodes;
             const int total_pages = (L + a.page_size - 1) / a.page_size;
-            const int32_t* pt = a.page_table + (size_t)i * a.max_pages + (kShared ? un.page0 : 0);
+            const int32_t* pt = a.page_table + (size_t)i * a.max_pages;
             const int T = un.tile_end - un.tile_begin;
             auto page_of = [&](int t) -> int {                   // this lane's page id in local tile t (-1: none)
                 if (t >= T || lane >= pages_per_tile) return -1;
@@ -371,14 +358,13 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const int u = un.slot;
             const int i = un.req;
             const int n = un.n_nodes;
-            const int R = kShared ? un.rows : a.G * n;
-            const int pl = kShared ? un.visible : a.prefix_len[i];
-            const int L = kShared ? un.n_keys : pl + n;
+            const int R = a.G * n;
+            const int pl = a.prefix_len[i];
+            const int L = pl + n;
             const int gr = un.rb * kRowBlock + row;
             const bool in_tree = gr < R;
             const int j = in_tree ? gr / a.G : 0, g = in_tree ? gr % a.G : 0;
-            const size_t slot_row = kShared && un.slot0 >= 0 ? (size_t)a.slot_map[un.slot0 + j] : (size_t)i * a.N + j;
-            const size_t qrow = slot_row * a.Hq + un.kvh * a.G + g;
+            const size_t qrow = ((size_t)i * a.N + j) * a.Hq + un.kvh * a.G + g;
             const int T = un.tile_end - un.tile_begin;
             // fused-plan variant: the plan has looked at num_nodes and prefix_len only; the tree itself is checked
             // below, by every warp that is about to use it (all come to the same verdict).  Its parent row is
@@ -417,7 +403,7 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                 anc = tree_ok ? warp_ancestor_mask(q0, q1, n, j, lane) : 0ull;
                 if (!valid) anc = 0ull;
             } else {
-                anc = valid && !(kShared && un.slot0 >= 0) ? a.w.anc[slot_row] : 0ull;
+                anc = valid ? a.w.anc[(size_t)i * a.N + j] : 0ull;
             }
             float m_used = -CUDART_INF_F, l = 0.f;
             for (int t = grp; t < T && ok; t += 2, ++cgm) {
@@ -546,7 +532,6 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                     const float w1 = m1 == -CUDART_INF_F ? 0.f : exp2f(m1 - M);
                     const float lsum = l * w0 + l1 * w1;
                     const bool split = un.n_chunks != 1;
-                    const size_t part_row = kShared ? (size_t)un.part0 + row : (size_t)u * a.w.rows + row;
                     const float f0 = split ? w0 : (lsum > 0.f ? w0 / lsum : 0.f), f1 = split ? w1 : (lsum > 0.f ? w1 / lsum : 0.f);
                     const bool use1 = theirs > 0;                  // uniform: O of group 1 is stale when it had no tile
 #pragma unroll 1                                                    // (once per unit: kept small, see the mask path above)
@@ -575,7 +560,7 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                                     dst[v] = make_uint4(w4[0], w4[1], w4[2], w4[3]);
                                 }
                             } else {
-                                float4* dst = reinterpret_cast<float4*>(a.w.part_o + part_row * 128 + c * 16);
+                                float4* dst = reinterpret_cast<float4*>(a.w.part_o + ((size_t)u * a.w.rows + row) * 128 + c * 16);
 #pragma unroll
                                 for (int v = 0; v < 4; ++v) dst[v] = make_float4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]);
                             }
@@ -585,8 +570,8 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                         if (!split) {
                             if (a.lse) a.lse[qrow] = (M + log2f(lsum)) * kLn2;
                         } else {
-                            a.w.part_ml[part_row * 2] = M;
-                            a.w.part_ml[part_row * 2 + 1] = lsum;
+                            a.w.part_ml[((size_t)u * a.w.rows + row) * 2] = M;
+                            a.w.part_ml[((size_t)u * a.w.rows + row) * 2 + 1] = lsum;
                         }
                     }
                 }
@@ -674,28 +659,6 @@ attn_sm100_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     }
 }
 
-// A head-major pool [num_pages, Hkv, page_size, 128] bf16 seen as blocks of (page, head): [blocks][token/8][d/64][token%8][d%64].
-// A token-major pool (page, token, head, d) seen as (d, token, head, page) with a box of 64 dims x all tokens of one head.
-bool make_pool_map(CUtensorMap* map, const void* pool, long long num_pages, int Hkv, int page_size, int token_major) {
-    EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
-    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-    if (token_major) {
-        const cuuint64_t dims[4] = {128, (cuuint64_t)page_size, (cuuint64_t)Hkv, (cuuint64_t)num_pages};
-        const cuuint64_t strides[3] = {(cuuint64_t)Hkv * 256, 256, (cuuint64_t)page_size * Hkv * 256};
-        const cuuint32_t box[4] = {64, (cuuint32_t)page_size, 1, 1};
-        return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-    }
-    const cuuint64_t dims[5] = {64, 8, 2, (cuuint64_t)(page_size / 8), (cuuint64_t)(num_pages * Hkv)};
-    const cuuint64_t strides[4] = {256, 128, 2048, (cuuint64_t)page_size * 256};
-    const cuuint32_t box[5] = {64, 8, 2, (cuuint32_t)(page_size / 8), 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(pool), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // The two tensor maps of a call depend only on the pools (address, pages, heads, page size, layout), which an engine
 // keeps for its whole life, so they are encoded once and looked up afterwards: a handful of entries, most recent first.
 struct PoolMapKey {
@@ -732,7 +695,7 @@ bool pool_maps(const PoolMapKey& key, CUtensorMap* k_map, CUtensorMap* v_map) {
     return true;
 }
 
-// Per-device set-up (SM count, shared-memory opt-in of the kernel variants), once per device.
+// Per-device set-up (SM count, shared-memory opt-in of the four kernel variants), once per device.
 constexpr int kMaxDevices = 64;
 std::once_flag g_dev_once[kMaxDevices];
 int g_sm_count[kMaxDevices];
@@ -746,8 +709,6 @@ war_status_t device_setup(int dev) {
         if (cudaFuncSetAttribute(attn_sm100_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) return;
         if (cudaFuncSetAttribute(attn_sm100_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesFused) != cudaSuccess) return;
         if (cudaFuncSetAttribute(attn_sm100_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesFused) != cudaSuccess) return;
-        if (cudaFuncSetAttribute(attn_sm100_kernel<false, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) return;
-        if (cudaFuncSetAttribute(attn_sm100_kernel<true, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) return;
         g_dev_status[dev] = WAR_OK;
     });
     if (g_dev_status[dev] != WAR_OK) (void)cudaGetLastError();
@@ -825,7 +786,6 @@ war_status_t war_attn_launch_sm100(const void* q, const void* k, const void* v, 
     a.num_pages = p->num_pages; a.scale_log2 = p->scale * kLog2e;
     a.N = p->N; a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.page_size = p->page_size; a.max_pages = p->max_pages_per_req;
     a.num_nodes = num_nodes; a.parent = parent; a.B = p->B; a.call = 0;
-    a.shared_units = nullptr; a.slot_map = nullptr;
     const int grid = g_sm_count[dev];
     if (fused) {
         a.call = war_attn_next_call();
@@ -835,32 +795,6 @@ war_status_t war_attn_launch_sm100(const void* q, const void* k, const void* v, 
         if (token_major) attn_sm100_kernel<true, false><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
         else attn_sm100_kernel<false, false><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
     }
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
-}
-
-war_status_t war_attn_launch_sm100_shared(const void* q, const void* k, const void* v, const int32_t* page_table,
-                                          const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse,
-                                          int* status_word, cudaStream_t s) {
-    int dev = 0;
-    WAR_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= kMaxDevices) return WAR_ERR_UNSUPPORTED;
-    const war_status_t st = device_setup(dev);
-    if (st != WAR_OK) return st;
-    const int token_major = war_attn_pool_layout(p->k_strides, p) == 1;
-    CUtensorMap k_map, v_map;
-    if (!make_pool_map(&k_map, k, p->num_pages, p->Hkv, p->page_size, token_major) ||
-        !make_pool_map(&v_map, v, p->num_pages, p->Hkv, p->page_size, token_major))
-        return WAR_ERR_CUDA;
-    KernelArgs a{};
-    a.q = (const __nv_bfloat16*)q; a.page_table = page_table; a.out = (__nv_bfloat16*)out; a.lse = lse; a.status_word = status_word;
-    a.w.counters = w.counters; a.w.anc = w.anc; a.w.part_ml = w.part_ml; a.w.part_o = w.part_o;
-    a.num_pages = p->num_pages; a.scale_log2 = p->scale * kLog2e;
-    a.N = p->N; a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.page_size = p->page_size; a.max_pages = p->max_pages_per_req;
-    a.B = p->B; a.shared_units = w.units; a.slot_map = w.slot_map;
-    const int grid = g_sm_count[dev];
-    if (token_major) attn_sm100_kernel<true, false, true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
-    else attn_sm100_kernel<false, false, true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
     WAR_LAUNCH_CHECK();
     return WAR_OK;
 }
