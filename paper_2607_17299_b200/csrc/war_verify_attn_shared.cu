@@ -69,8 +69,10 @@ constexpr int kMaxChunks = 0x7fff;
 constexpr int kMinChunkCost = 4;          // tiles of one row block
 
 // One block.  Trees and groups are checked, parts are laid out and cut into chunks.  The time of a part's tile counts 1, or 2 where two
-// row blocks of 128 rows work on it together.  A chunk costs C = max(4, sqrt(6 * all / CTAs), all / kTargetUnits): smaller ones pay for
-// more units (about four tiles each), larger ones for a longer tail.  The units are sorted, the longest first.
+// row blocks of 128 rows work on it together.  A chunk costs C = max(4, sqrt(36 * all / CTAs), all / kTargetUnits): smaller ones pay for
+// more units (queries, first S, partial results written and merged: 12 to 18 such tiles each), larger ones for a longer tail.  (Nine shapes:
+// 6 in place of 36 is 2 to 25 % slower, 100 from 3 % faster to 29 % slower; a search over 32 chunk costs by an estimate of the time was no
+// better.)  Units are sorted, the longest first; the CTAs draw them one by one.
 __global__ void __launch_bounds__(kPlanThreads)                    // (a quarter of the threads for small batches: barriers are cheaper)
 attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ num_nodes, const int32_t* __restrict__ parent,
                         const int32_t* __restrict__ leader, const int32_t* __restrict__ shared_len, int B, int N, int Hkv, int G,
@@ -185,7 +187,7 @@ attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* _
     for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
     all *= Hkv;
     const long long least = (all + kTargetUnits - 1) / kTargetUnits;
-    const int chunk = (int)max(max((long long)kMinChunkCost, least), (long long)sqrtf(6.f * (float)all / (float)n_ctas));
+    const int chunk = (int)max(max((long long)kMinChunkCost, least), (long long)sqrtf(36.f * (float)all / (float)n_ctas));
     // chunks of a part and the cost of the longest of them, for the order
     for (int e = tid; e < E; e += n_threads) {
         const int t = a.tiles[e], cost = tile_cost(min(a.rows[e], block)), nc = min((t * cost + chunk - 1) / chunk, min(t, kMaxChunks));
