@@ -5,7 +5,7 @@
 // number (the k-th page wanted is the k-th lowest free one), not by who comes first.
 //
 // All of this is a few kilobytes to a few megabytes of integers per call, so a call costs its launch and the chain of dependent reads.
-// One launch each, then.  Fork, compaction and groups need all blocks to have read before one writes; they run as one cluster of
+// One launch each, then.  Fork and compaction need all blocks to have read before one writes; they run as one cluster of
 // eight blocks, whose hardware barrier takes the place of further launches (a barrier: about 0.5 us; a launch in a graph: 1.5 to 2).
 #include <cooperative_groups.h>
 #include <mutex>
@@ -48,6 +48,30 @@ __device__ __forceinline__ int block_scan(int x, ScanScratch& s, int* total) {
     *total = s.warp[32];
     __syncthreads();
     return before + incl - x;
+}
+
+// The same for two numbers at once.
+__device__ __forceinline__ int2 block_scan2(int2 x, int2* s_warp, int2* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int2 incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl.x, o), z = __shfl_up_sync(0xffffffffu, incl.y, o);
+        if (lane >= o) { incl.x += y; incl.y += z; }
+    }
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    const int2 w = s_warp[lane];                                  // every warp adds the warps' sums up for itself: one barrier less
+    int2 wi = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, wi.x, o), z = __shfl_up_sync(0xffffffffu, wi.y, o);
+        if (lane >= o) { wi.x += y; wi.y += z; }
+    }
+    const int2 before = make_int2(__shfl_sync(0xffffffffu, wi.x - w.x, warp), __shfl_sync(0xffffffffu, wi.y - w.y, warp));
+    *total = make_int2(__shfl_sync(0xffffffffu, wi.x, 31), __shfl_sync(0xffffffffu, wi.y, 31));
+    __syncthreads();
+    return make_int2(before.x + incl.x - x.x, before.y + incl.y - x.y);
 }
 
 // the position of the k-th (from 0) set bit of a word that has it
@@ -103,8 +127,10 @@ __device__ __forceinline__ int nth_free(const FreeRound& r, long long first, int
 // ------------------------------------------------------------------------------------------------
 // free
 // ------------------------------------------------------------------------------------------------
-// A block per request.  Pages of a cancelled group come back with their last holder, whichever block that is.
-__global__ void __launch_bounds__(256)
+// A block per request.  Pages of a group come back with their last holder, whichever block that is.  A thread asks for four entries at
+// once and then for the four counts (one after the other they cost two trips to L2 each).
+constexpr int kFreeThreads = 256, kFreeDeep = 4;
+__global__ void __launch_bounds__(kFreeThreads)
 pages_free_kernel(war_pages_t p, const int32_t* __restrict__ done, int32_t* tail_len, int* status_word) {
     const int b = blockIdx.x;
     if (done[b] == 0) return;
@@ -114,14 +140,20 @@ pages_free_kernel(war_pages_t p, const int32_t* __restrict__ done, int32_t* tail
         if (threadIdx.x == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
         return;
     }
-#pragma unroll 4
-    for (int j = threadIdx.x; j < held; j += 256) {
-        const int page = row[j];
-        row[j] = -1;
-        if (page < 0 || page >= p.num_pages) { war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
-        const int had = atomicSub(&p.d_refs[page], 1);
-        if (had == 1) atomicOr(&p.d_free[page >> 5], 1u << (page & 31));
-        if (had <= 0) { atomicAdd(&p.d_refs[page], 1); war_set_device_status(status_word, WAR_ERR_BAD_PAGE); }
+    for (int j0 = threadIdx.x; j0 < held; j0 += kFreeThreads * kFreeDeep) {
+        int page[kFreeDeep], had[kFreeDeep];
+#pragma unroll
+        for (int k = 0; k < kFreeDeep; ++k) page[k] = j0 + k * kFreeThreads < held ? row[j0 + k * kFreeThreads] : -2;
+#pragma unroll
+        for (int k = 0; k < kFreeDeep; ++k) had[k] = page[k] >= 0 && page[k] < p.num_pages ? atomicSub(&p.d_refs[page[k]], 1) : 2;
+#pragma unroll
+        for (int k = 0; k < kFreeDeep; ++k) {
+            if (page[k] == -2 && j0 + k * kFreeThreads >= held) continue;
+            row[j0 + k * kFreeThreads] = -1;
+            if (page[k] < 0 || page[k] >= p.num_pages) { war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
+            if (had[k] == 1) atomicOr(&p.d_free[page[k] >> 5], 1u << (page[k] & 31));
+            if (had[k] <= 0) { atomicAdd(&p.d_refs[page[k]], 1); war_set_device_status(status_word, WAR_ERR_BAD_PAGE); }
+        }
     }
     __syncthreads();                                              // (every thread has read held)
     if (threadIdx.x == 0) {
@@ -140,7 +172,7 @@ struct GrowShared {
     int held[kMaxB];
 };
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 1)
 pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ tail_len, int32_t* granted,
                   int* status_word) {
     extern __shared__ __align__(16) uint8_t pages_smem[];
@@ -211,6 +243,7 @@ pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, 
 // What changes is decided by every block for itself from the books as they are; after the cluster's barrier the blocks write, a tile of
 // columns each at a time: a table's column is changed by one block alone, which holds all of its old entries in shared memory, so
 // requests that swap places need no second table.
+constexpr int kDeep = 4, kForkDeep = 8;   // entries that a thread asks for at once
 constexpr int kForkTile = 16384;          // entries of a tile
 struct ForkShared {
     ScanScratch scan;
@@ -226,7 +259,7 @@ struct ForkShared {
     int columns;
 };
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 1)
 pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32_t* prefix_len, int32_t* tail, int32_t* tail_len,
                   int32_t* copies, int32_t* n_copies, int32_t* ok_word, int* status_word) {
     extern __shared__ __align__(16) uint8_t pages_smem[];
@@ -299,9 +332,14 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
     const int columns = s.columns;
     if (rank == 0 && tid == 0) { *ok_word = enough; *n_copies = enough ? wanted : 0; }
     // ---- everything has been read but the rows themselves and the tails; every block takes its columns ----
-    const int tail_tile = 1;                                      // (one more tile: the tail windows)
-    const int tile_cols = max(1, min(64, kForkTile / max(1, B)));
-    const int tiles = (columns + tile_cols - 1) / tile_cols + tail_tile;
+    // Tiles of 2^lg columns (and one more, the tail windows): the width that leaves the least to the busiest block, a tile's barriers and
+    // trips to memory counted as 16 columns.
+    int lg = 0, least = 0x7fffffff;
+    for (int w = 0; w <= 6 && ((long long)B << w) <= kForkTile; ++w) {
+        const int busiest = ((((columns + (1 << w) - 1) >> w) + kCluster - 1) / kCluster) * ((1 << w) + 16);
+        if (busiest <= least) { least = busiest; lg = w; }
+    }
+    const int tile_cols = 1 << lg, tiles = ((columns + tile_cols - 1) >> lg) + 1;
     int pl_new[kMaxB / kThreads], tl_new[kMaxB / kThreads];
 #pragma unroll
     for (int k = 0; k < kMaxB / kThreads; ++k) {
@@ -358,33 +396,52 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
             continue;
         }
         __syncthreads();
-        for (int x = tid; x < B * cols; x += kThreads) {
-            const int b = x / cols, c = x - b * cols;
-            if (s.src[b] >= 0 || s.takers[b] > 0) s.entries[x] = table[(size_t)b * stride + c];
+        const int wide = is_tail ? 5 : lg, entries = B << wide;   // (a tail window has at most 32 tokens)
+        for (int x0 = tid; x0 < entries; x0 += kThreads * kForkDeep) {
+            int v[kForkDeep];
+#pragma unroll
+            for (int k = 0; k < kForkDeep; ++k) {
+                const int x = x0 + k * kThreads, b = x >> wide, c = x & ((1 << wide) - 1);
+                v[k] = x < entries && c < cols && (s.src[b] >= 0 || s.takers[b] > 0) ? table[(size_t)b * stride + c] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < kForkDeep; ++k) if (x0 + k * kThreads < entries) s.entries[x0 + k * kThreads] = v[k];
         }
         __syncthreads();
-        for (int x = tid; x < B * cols; x += kThreads) {
-            const int b = x / cols, c = x - b * cols, src = s.src[b];
-            if (is_tail) {
-                if (src >= 0) tail[(size_t)b * P + c] = s.entries[src * cols + c];
-                continue;
+        for (int x0 = tid; x0 < entries; x0 += kThreads * kForkDeep) {
+            int left[kForkDeep], page[kForkDeep];
+#pragma unroll
+            for (int k = 0; k < kForkDeep; ++k) {
+                const int x = x0 + k * kThreads;
+                left[k] = 1;
+                page[k] = 0;
+                const int b = x >> wide, c = x & ((1 << wide) - 1);
+                if (x >= entries || c >= cols) continue;
+                const int src = s.src[b];
+                if (is_tail) {
+                    if (src >= 0) tail[(size_t)b * P + c] = s.entries[(src << wide) + c];
+                    continue;
+                }
+                const int col = c0 + c;
+                // what this entry's page gains and loses: a holder for every request that takes it as a full page, this row if it is
+                // replaced, unless its partly filled page is handed on
+                int delta = (col < s.full[b] ? s.takers[b] : 0) - (src >= 0 && col < s.held[b] ? 1 : 0);
+                if (delta < 0 && col == s.full[b] && s.first[b] < kMaxB && s.last[s.first[b]] >= 0 && s.fresh[s.first[b]] == -1) delta = 0;
+                if (delta != 0) {
+                    page[k] = s.entries[x];
+                    if (page[k] < 0 || page[k] >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+                    else if (delta > 0) atomicAdd(&p.d_refs[page[k]], delta);
+                    else left[k] = atomicAdd(&p.d_refs[page[k]], delta) + delta;
+                }
+                if (src < 0) continue;
+                int now = -1;
+                if (col < s.full[src]) now = s.entries[(src << wide) + c];
+                else if (col == s.full[src] && s.last[b] >= 0) now = s.fresh[b] < -1 ? ~(s.fresh[b] + 1) : s.last[b];
+                else if (col >= s.held[b]) continue;              // (nothing stood there)
+                p.d_page_table[(size_t)b * width + col] = now;
             }
-            const int col = c0 + c;
-            // what this entry's page gains and loses: a holder for every request that takes it as a full page, this row if it is
-            // replaced, unless its partly filled page is handed on
-            int delta = (col < s.full[b] ? s.takers[b] : 0) - (src >= 0 && col < s.held[b] ? 1 : 0);
-            if (delta < 0 && col == s.full[b] && s.first[b] < kMaxB && s.last[s.first[b]] >= 0 && s.fresh[s.first[b]] == -1) delta = 0;
-            if (delta != 0) {
-                const int page = s.entries[x];
-                if (page < 0 || page >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
-                else if (atomicAdd(&p.d_refs[page], delta) + delta == 0) atomicOr(&p.d_free[page >> 5], 1u << (page & 31));
-            }
-            if (src < 0) continue;
-            int now = -1;
-            if (col < s.full[src]) now = s.entries[src * cols + c];
-            else if (col == s.full[src] && s.last[b] >= 0) now = s.fresh[b] < -1 ? ~(s.fresh[b] + 1) : s.last[b];
-            else if (col >= s.held[b]) continue;                  // (nothing stood there)
-            p.d_page_table[(size_t)b * width + col] = now;
+#pragma unroll
+            for (int k = 0; k < kForkDeep; ++k) if (left[k] == 0) atomicOr(&p.d_free[page[k] >> 5], 1u << (page[k] & 31));
         }
     }
 }
@@ -395,12 +452,12 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
 // The i-th highest used page goes to the i-th lowest free page while it lies above it.  With U pages in use that moves exactly the
 // used pages at or above U, so the two lists are the free pages below U, upwards, and the used ones from U on, downwards.
 struct CompactShared {
-    ScanScratch scan;
+    int2 warp[32];
     int used;                              // of this block's words
     int free_below, used_above;            // of this block's words, below / from U on
 };
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 1)
 pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies, int32_t* n_copies, int32_t* top, int* status_word) {
     __shared__ CompactShared s;
     cg::cluster_group cluster = cg::this_cluster();
@@ -415,11 +472,13 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
         return left >= 32 ? 0xffffffffu : (1u << left) - 1u;
     };
     // ---- pages in use ----
-    int used = 0;
-    for (int w = w0 + tid; w < w1; w += kThreads) used += __popc(~p.d_free[w] & valid(w));
-    int total;
-    block_scan(used, s.scan, &total);
-    if (tid == 0) s.used = total;
+    const bool once = w1 - w0 <= kThreads;                        // a word a thread: it is read and summed up once
+    const uint32_t mine = w0 + tid < w1 ? p.d_free[w0 + tid] : 0u;
+    int used = w0 + tid < w1 ? __popc(~mine & valid(w0 + tid)) : 0;
+    for (int w = w0 + tid + kThreads; w < w1; w += kThreads) used += __popc(~p.d_free[w] & valid(w));
+    int2 total;
+    block_scan2(make_int2(used, 0), s.warp, &total);
+    if (tid == 0) s.used = total.x;
     cluster.sync();
     int U = 0;
     for (int r = 0; r < kCluster; ++r) U += *cluster.map_shared_rank(&s.used, r);
@@ -428,66 +487,82 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
         const int left = U - w * 32;
         return left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
     };
-    int lo = 0, hi = 0;
-    for (int w = w0 + tid; w < w1; w += kThreads) {
-        const uint32_t f = p.d_free[w];
-        lo += __popc(f & below(w));
-        hi += __popc(~f & valid(w) & ~below(w));
-    }
-    int lo_all, hi_all;
-    block_scan(lo, s.scan, &lo_all);
-    block_scan(hi, s.scan, &hi_all);
-    if (tid == 0) { s.free_below = lo_all; s.used_above = hi_all; }
+    auto free_of = [&](int w, uint32_t f) -> uint32_t { return w < w1 ? f & below(w) : 0u; };
+    auto used_of = [&](int w, uint32_t f) -> uint32_t { return w < w1 ? ~f & valid(w) & ~below(w) : 0u; };
+    int2 own = make_int2(__popc(free_of(w0 + tid, mine)), __popc(used_of(w0 + tid, mine)));
+    for (int w = w0 + tid + kThreads; w < w1; w += kThreads) { const uint32_t f = p.d_free[w]; own.x += __popc(free_of(w, f)); own.y += __popc(used_of(w, f)); }
+    const int2 before = block_scan2(own, s.warp, &total);
+    if (tid == 0) { s.free_below = total.x; s.used_above = total.y; }
     cluster.sync();
-    int lo_at = 0, hi_at = 0, moves = 0;                          // free ones before this block's, used ones behind it
+    int lo_at = 0, hi_at = total.y, moves = 0;                    // free ones before this block's, used ones from its own on
     for (int r = 0; r < kCluster; ++r) {
         const int x = *cluster.map_shared_rank(&s.free_below, r), y = *cluster.map_shared_rank(&s.used_above, r);
         if (r < rank) lo_at += x;
         if (r > rank) hi_at += y;
         moves += x;
     }
-    hi_at += hi_all;
     for (int first = w0; first < w1; first += kThreads) {         // words in order: free ones from the front, used ones from the back
         const int w = first + tid;
-        const uint32_t f = w < w1 ? p.d_free[w] : 0u;
-        uint32_t a = w < w1 ? f & below(w) : 0u, c = w < w1 ? ~f & valid(w) & ~below(w) : 0u;
-        int a_all, c_all;
-        int at = lo_at + block_scan(__popc(a), s.scan, &a_all);
-        int back = hi_at - block_scan(__popc(c), s.scan, &c_all);
-        lo_at += a_all; hi_at -= c_all;
+        const uint32_t f = first == w0 ? mine : w < w1 ? p.d_free[w] : 0u;
+        uint32_t a = free_of(w, f), c = used_of(w, f);
+        int2 round, at2 = before;
+        if (!once) at2 = block_scan2(make_int2(__popc(a), __popc(c)), s.warp, &round);
+        int at = lo_at + at2.x, back = hi_at - at2.y;
+        if (!once) { lo_at += round.x; hi_at -= round.y; }
         while (a) { to[at++] = w * 32 + __ffs(a) - 1; a &= a - 1; }
         while (c) { from[--back] = w * 32 + __ffs(c) - 1; c &= c - 1; }
     }
     cluster.sync();
     // ---- the moves ----
     const int done = min(moves, max_copies);
-    for (int i = rank * kThreads + tid; i < moves; i += kCluster * kThreads) {
-        const int a = from[i], c = to[i];
-        place[a] = i < done ? c : a;
-        if (i >= done) continue;
-        p.d_refs[c] = p.d_refs[a];
-        p.d_refs[a] = 0;
-        atomicAnd(&p.d_free[c >> 5], ~(1u << (c & 31)));
-        atomicOr(&p.d_free[a >> 5], 1u << (a & 31));
-        copies[3 * i] = a; copies[3 * i + 1] = c; copies[3 * i + 2] = p.page_size;
+    for (int i0 = rank * kThreads + tid; i0 < moves; i0 += kCluster * kThreads * kDeep) {
+        int a[kDeep], c[kDeep], refs[kDeep];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const int i = i0 + k * kCluster * kThreads;
+            a[k] = i < moves ? from[i] : 0; c[k] = i < done ? to[i] : a[k];
+        }
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) refs[k] = i0 + k * kCluster * kThreads < done ? p.d_refs[a[k]] : 0;
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const int i = i0 + k * kCluster * kThreads;
+            if (i >= moves) break;
+            place[a[k]] = c[k];
+            if (i >= done) continue;
+            p.d_refs[c[k]] = refs[k];
+            p.d_refs[a[k]] = 0;
+            atomicAnd(&p.d_free[c[k] >> 5], ~(1u << (c[k] & 31)));
+            atomicOr(&p.d_free[a[k] >> 5], 1u << (a[k] & 31));
+            copies[3 * i] = a[k]; copies[3 * i + 1] = c[k]; copies[3 * i + 2] = p.page_size;
+        }
     }
     if (rank == 0 && tid == 0) {
         *n_copies = done;
         *top = done < moves ? from[done] + 1 : U;
     }
     cluster.sync();
-    // ---- the tables follow ----
-    for (int b = rank; b < p.B; b += kCluster) {
-        const int held = p.d_held[b];
+    // ---- the tables follow, a warp a row ----
+    for (int b = (rank * kThreads + tid) >> 5; b < p.B; b += kCluster * kThreads / 32) {
+        const int held = p.d_held[b], lane = tid & 31;
         int32_t* row = p.d_page_table + (size_t)b * p.max_pages_per_req;
-        if (held < 0 || held > p.max_pages_per_req) { if (tid == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
-        for (int j = tid; j < held; j += kThreads) {
-            const int page = row[j];
-            if (page < 0 || page >= p.num_pages) { war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
-            if (page < U) continue;
-            const int now = place[page];
-            if (now < 0 || now >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);   // (a held page marked as free)
-            else row[j] = now;
+        if (held < 0 || held > p.max_pages_per_req) { if (lane == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
+        for (int j0 = lane; j0 < held; j0 += 32 * 2 * kDeep) {
+            int page[2 * kDeep], now[2 * kDeep];
+#pragma unroll
+            for (int k = 0; k < 2 * kDeep; ++k) page[k] = j0 + k * 32 < held ? row[j0 + k * 32] : 0;
+#pragma unroll
+            for (int k = 0; k < 2 * kDeep; ++k) {
+                const bool bad = page[k] < 0 || page[k] >= p.num_pages;
+                if (bad) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+                now[k] = !bad && page[k] >= U && j0 + k * 32 < held ? place[page[k]] : -1;
+            }
+#pragma unroll
+            for (int k = 0; k < 2 * kDeep; ++k) {
+                if (j0 + k * 32 >= held || page[k] < U || page[k] >= p.num_pages) continue;
+                if (now[k] < 0 || now[k] >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);   // (a held page marked as free)
+                else row[j0 + k * 32] = now[k];
+            }
         }
     }
 }
@@ -495,68 +570,82 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
 // ------------------------------------------------------------------------------------------------
 // groups
 // ------------------------------------------------------------------------------------------------
-struct GroupShared { int key[kMaxB]; };
-
-__global__ void __launch_bounds__(kThreads)
+// A block per request: it leaves if a lower request has the same page in that column, else it is the leader and compares its row with
+// all of its members', a column a thread, until the columns in which all agree end.  Blocks have nothing to tell each other.
+constexpr int kGroupThreads = 512, kGroupDeep = 2, kGroupRows = 4;
+__global__ void __launch_bounds__(kGroupThreads)
 prefix_groups_kernel(const int32_t* __restrict__ table, const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ tail_len,
                      int B, int page_size, int width, int column, int32_t* leader, int32_t* shared_len) {
-    __shared__ GroupShared s;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int tid = threadIdx.x, lane = tid & 31, rank = (int)cluster.block_rank();
-    constexpr int kNone = 0x7fffffff;
-    auto full_of = [&](int b) -> int { return min(max(prefix_len[b], 0) / page_size, width); };
-    for (int b = tid; b < B; b += kThreads) {
-        const bool runs = !tail_len || tail_len[b] >= 0;
-        s.key[b] = runs && column < full_of(b) ? table[(size_t)b * width + column] : -1;
-    }
+    __shared__ uint16_t s_member[kMaxB];
+    __shared__ int s_members, s_full, s_same;
+    const int tid = threadIdx.x, me = blockIdx.x;
+    auto full_of = [&](int b) -> int {                            // full pages of a running request's prefix
+        const int pl = prefix_len[b], run = tail_len ? tail_len[b] : 0;
+        return run >= 0 && pl > 0 ? min(pl / page_size, width) : 0;
+    };
+    const int my_full = full_of(me), my_key = table[(size_t)me * width + min(column, width - 1)];
+    if (tid == 0) { s_members = 0; s_full = my_full; }
+    bool lower = false;
     __syncthreads();
-    // ---- the lowest request with the same page, a warp each; the smallest common length starts as "nobody else" ----
-    for (int b = (rank * kThreads + tid) >> 5; b < B; b += kCluster * (kThreads / 32)) {
-        const int key = s.key[b];
-        int l = b;
-        for (int q = 0; key >= 0 && q < b; q += 32) {
-            const uint32_t m = __ballot_sync(0xffffffffu, q + lane < b && s.key[q + lane] == key);
-            if (m) { l = q + __ffs(m) - 1; break; }
-        }
-        if (lane == 0) { leader[b] = l; shared_len[b] = kNone; }
-    }
-    cluster.sync();
-    // ---- common full pages of every member with its leader, a warp each, 128 columns at a time ----
-    for (int b = (rank * kThreads + tid) >> 5; b < B; b += kCluster * (kThreads / 32)) {
-        const int l = leader[b];
-        if (l == b) continue;
-        const int n = min(full_of(b), full_of(l));
-        const int32_t *x = table + (size_t)b * width, *y = table + (size_t)l * width;
-        int same = n;
-        for (int c = 0; c < n; c += 128) {
-            uint32_t differ[4];
+    if (my_full > column && my_key >= 0) {                        // (uniform: all threads have read the same)
+        for (int q0 = 0; q0 < B; q0 += kGroupThreads * kGroupDeep) {
+            int key[kGroupDeep], full[kGroupDeep];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int at = c + k * 32 + lane;
-                differ[k] = at < n ? (uint32_t)(x[at] != y[at]) : 0u;
+            for (int k = 0; k < kGroupDeep; ++k) {
+                const int q = q0 + k * kGroupThreads + tid;
+                full[k] = q < B ? full_of(q) : 0;
+                key[k] = q < B ? table[(size_t)q * width + column] : -1;
             }
-            bool stop = false;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t m = __ballot_sync(0xffffffffu, differ[k] != 0);
-                if (m && !stop) { same = c + k * 32 + __ffs(m) - 1; stop = true; }
+            for (int k = 0; k < kGroupDeep; ++k) {
+                const int q = q0 + k * kGroupThreads + tid;
+                if (full[k] <= column || key[k] != my_key || q == me) continue;
+                if (q < me) lower = true;
+                else { s_member[atomicAdd(&s_members, 1)] = (uint16_t)q; atomicMin(&s_full, full[k]); }
             }
-            if (stop) break;
+            if (__syncthreads_or(lower)) return;                  // (the leader's block answers for this request)
         }
-        if (lane == 0) atomicMin(&shared_len[l], same);
     }
-    cluster.sync();
-    const int b = rank * kThreads + tid;                          // (one request a thread: B <= 8192)
-    int l = b, common = kNone;
-    if (b < B) { l = leader[b]; common = *(volatile int32_t*)&shared_len[l]; }
-    cluster.sync();
-    if (b < B) {
-        const bool group = common != kNone && common > column;
-        leader[b] = group ? l : b;
-        shared_len[b] = group ? common * page_size : 0;
+    const int members = s_members, n = s_full;
+    const int32_t* mine = table + (size_t)me * width;
+    int same = 0;
+    if (members > 0) {
+        for (same = 0; same < n;) {
+            if (tid == 0) s_same = n;
+            __syncthreads();
+            int first = n;
+            int x[kGroupDeep];
+#pragma unroll
+            for (int k = 0; k < kGroupDeep; ++k) { const int c = same + k * kGroupThreads + tid; x[k] = c < n ? mine[c] : 0; }
+            for (int m = 0; m < members; m += kGroupRows) {       // (the rows of a few members at once)
+                int y[kGroupRows][kGroupDeep];
+#pragma unroll
+                for (int r = 0; r < kGroupRows; ++r) {
+                    const int32_t* row = table + (size_t)s_member[min(m + r, members - 1)] * width;
+#pragma unroll
+                    for (int k = 0; k < kGroupDeep; ++k) { const int c = same + k * kGroupThreads + tid; y[r][k] = c < n ? row[c] : x[k]; }
+                }
+#pragma unroll
+                for (int r = 0; r < kGroupRows; ++r)
+#pragma unroll
+                    for (int k = kGroupDeep - 1; k >= 0; --k) if (y[r][k] != x[k]) first = min(first, same + k * kGroupThreads + tid);
+            }
+            if (first < n) atomicMin(&s_same, first);
+            __syncthreads();
+            const int end = s_same, next = min(n, same + kGroupThreads * kGroupDeep);
+            __syncthreads();
+            same = min(end, next);
+            if (end < next) break;
+        }
+    }
+    const bool group = members > 0 && same > column;
+    if (tid == 0) { leader[me] = me; shared_len[me] = group ? same * page_size : 0; }
+    for (int m = tid; m < members; m += kGroupThreads) {
+        const int q = s_member[m];
+        leader[q] = group ? me : q;
+        shared_len[q] = group ? same * page_size : 0;
     }
 }
-static_assert(kMaxB <= kCluster * kThreads, "one request a thread");
 
 // ------------------------------------------------------------------------------------------------
 // copy
@@ -660,7 +749,7 @@ extern "C" war_status_t war_pages_free(const war_pages_t* p, const int32_t* d_do
     if (!d_done) return WAR_ERR_INVALID_ARG;
     int* status_word = war_status_word();
     if (!status_word) return WAR_ERR_CUDA;
-    pages_free_kernel<<<p->B, 256, 0, stream>>>(*p, d_done, d_tail_len, status_word);
+    pages_free_kernel<<<p->B, kFreeThreads, 0, stream>>>(*p, d_done, d_tail_len, status_word);
     WAR_LAUNCH_CHECK();
     return WAR_OK;
 }
@@ -724,8 +813,10 @@ extern "C" war_status_t war_prefix_groups(const int32_t* d_page_table, const int
     if (B == 0) return WAR_OK;
     if (!d_page_table || !d_prefix_len || !d_leader || !d_shared_len) return WAR_ERR_INVALID_ARG;
     const int column = (min_shared - 1) / page_size;
-    return launch_cluster(prefix_groups_kernel, 0, stream, d_page_table, d_prefix_len, d_tail_len, B, page_size, max_pages_per_req, column,
-                          d_leader, d_shared_len);
+    prefix_groups_kernel<<<B, kGroupThreads, 0, stream>>>(d_page_table, d_prefix_len, d_tail_len, B, page_size, max_pages_per_req, column,
+                                                         d_leader, d_shared_len);
+    WAR_LAUNCH_CHECK();
+    return WAR_OK;
 }
 
 extern "C" war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d_n_copies, int32_t max_copies, void* d_kpool, void* d_vpool,
