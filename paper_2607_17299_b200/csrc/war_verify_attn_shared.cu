@@ -72,7 +72,7 @@ constexpr int kMinChunkCost = 4;          // tiles of one row block
 // row blocks of 128 rows work on it together.  A chunk costs C = max(4, sqrt(36 * all / CTAs), all / kTargetUnits): smaller ones pay for
 // more units (queries, first S, partial results written and merged: 12 to 18 such tiles each), larger ones for a longer tail.  (Nine shapes:
 // 6 in place of 36 is 2 to 25 % slower, 100 from 3 % faster to 29 % slower; a search over 32 chunk costs by an estimate of the time was no
-// better.)  Units are sorted, the longest first; the CTAs draw them one by one.
+// better.)  With little work C is what makes a unit for every CTA, if that is less.  Units are sorted, the longest first; the CTAs draw them one by one.
 __global__ void __launch_bounds__(kPlanThreads)                    // (a quarter of the threads for small batches: barriers are cheaper)
 attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ num_nodes, const int32_t* __restrict__ parent,
                         const int32_t* __restrict__ leader, const int32_t* __restrict__ shared_len, int B, int N, int Hkv, int G,
@@ -177,17 +177,26 @@ attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* _
 
     // ---- cost of a chunk ----
     long long mine = 0;
-    for (int e = tid; e < E; e += n_threads) mine += (long long)a.tiles[e] * row_blocks_of(a.rows[e]) * tile_cost(min(a.rows[e], block));
+    int blocks = 0;
+    for (int e = tid; e < E; e += n_threads) {
+        const int rbs = row_blocks_of(a.rows[e]);
+        mine += (long long)a.tiles[e] * rbs * tile_cost(min(a.rows[e], block));
+        blocks += a.tiles[e] > 0 ? rbs : 0;
+    }
+    blocks = __reduce_add_sync(0xffffffffu, blocks);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    if (lane == 0) s_sum[warp] = mine;
+    if (lane == 0) { s_sum[warp] = mine; s_warp[warp] = blocks; }
     __syncthreads();
     long long all = lane < n_warps ? s_sum[lane] : 0;
+    blocks = __reduce_add_sync(0xffffffffu, lane < n_warps ? s_warp[lane] : 0) * Hkv;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
     all *= Hkv;
     const long long least = (all + kTargetUnits - 1) / kTargetUnits;
-    const int chunk = (int)max(max((long long)kMinChunkCost, least), (long long)sqrtf(36.f * (float)all / (float)n_ctas));
+    long long want = (long long)sqrtf(36.f * (float)all / (float)n_ctas);
+    if (blocks < n_ctas) want = min(want, (all + n_ctas - blocks - 1) / (n_ctas - blocks));
+    const int chunk = (int)max(max((long long)kMinChunkCost, least), want);
     // chunks of a part and the cost of the longest of them, for the order
     for (int e = tid; e < E; e += n_threads) {
         const int t = a.tiles[e], cost = tile_cost(min(a.rows[e], block)), nc = min((t * cost + chunk - 1) / chunk, min(t, kMaxChunks));
