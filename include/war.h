@@ -581,8 +581,9 @@ war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d_n_copies, 
  * shared_len[leader] says how many leading tokens its members share (rounded down to whole pages; at most any member's prefix_len): their K and
  * V are read once, through the table of the group's lowest request with num_nodes > 0, and multiplied with the queries of all members.
  * Requests with num_nodes = 0 do not count as members, and a group with one member is a request for itself, whatever its shared_len.
- * A member whose leader or shared_len breaks these rules records WAR_ERR_INVALID_ARG and its rows are left as they are.
- * kernel must be 0; B * N * Hq < 2^29.  Three launches.  Pages of the shared prefix are taken from one table: tables that differ there
+ * A member whose leader or shared_len breaks these rules records WAR_ERR_INVALID_ARG, its rows are left as they are and it does not
+ * count; members that are no leaders are looked at first, so a leader that they leave alone is a request for itself.
+ * kernel must be 0; Hkv <= 65535, B * N * Hq < 2^29.  Three launches.  Pages of the shared prefix are taken from one table: tables that differ there
  * give the results of that one.
  * ------------------------------------------------------------------------------------------------ */
 war_status_t war_prefix_groups(const int32_t* d_page_table, const int32_t* d_prefix_len, const int32_t* d_tail_len, int32_t B,

@@ -337,7 +337,8 @@ war_status_t check_shape(const war_attn_params_t* p) {
         return WAR_ERR_INVALID_ARG;
     if (p->D != 128 || (p->page_size != 8 && p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128))
         return WAR_ERR_UNSUPPORTED;
-    if ((p->Hq / p->Hkv) * p->N > 512 || p->B > kMaxPlanB || (long long)p->B * p->N * p->Hq >= (1ll << 29)) return WAR_ERR_UNSUPPORTED;
+    // (a unit's record has 16 bits for the kv head; rows of partial results are counted in 32)
+    if ((p->Hq / p->Hkv) * p->N > 512 || p->B > kMaxPlanB || p->Hkv > 65535 || (long long)p->B * p->N * p->Hq >= (1ll << 29)) return WAR_ERR_UNSUPPORTED;
     if ((long long)p->max_pages_per_req * p->page_size >= (1ll << 30)) return WAR_ERR_UNSUPPORTED;    // contexts below 2^30 tokens
     return WAR_OK;
 }
