@@ -522,7 +522,7 @@ war_status_t war_commit_quant(const int32_t* d_ids, const int32_t* d_accept_len,
  *   d_page_table [B, max_pages_per_req], d_held [B]   the first held[b] entries of row b are in use
  * A new pool has refs and held 0 and all bits of its pages set.  The pages of all layers go by one table: a list of copies
  * int32 [n, 3] = (from, to, rows) is given to war_pages_copy once per layer.  Results do not depend on timing: pages are given
- * out from the lowest free one up, to the requests in order.  B <= 4096, num_pages <= 2^30.  One launch each; nothing is allocated.
+ * out from the lowest free one up, to the requests in order.  B <= 4096, num_pages <= 2^30, B * max_pages_per_req < 2^31.  One launch each; nothing is allocated.
  * Books that contradict themselves (a page outside the pool, more entries than refs counts, held outside [0, max_pages_per_req]) record
  * WAR_ERR_BAD_PAGE; such entries are left out.
  *

@@ -98,14 +98,15 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
 // A round of the free map in shared memory: words, and how many free pages lie before each.
 struct FreeRound { uint32_t word[kRound]; int before[kRound + 1]; };
 
-// Loads words [first, first + kRound) (those behind n_words as empty); `before` counts from `base` on.  Returns the free pages.
-__device__ __forceinline__ int load_round(FreeRound& r, const uint32_t* free_map, long long first, long long n_words, int base, ScanScratch& s) {
+// Loads words [first, first + kRound) (pages behind the pool's last one as taken); `before` counts from `base` on.  Returns the free pages.
+__device__ __forceinline__ int load_round(FreeRound& r, const uint32_t* free_map, long long first, long long num_pages, int base, ScanScratch& s) {
     const int w0 = (int)threadIdx.x * 4;
     uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {                                // (coalesced, then turned: a thread's four words are neighbours)
         const int at = (int)threadIdx.x + k * kThreads;
-        r.word[at] = first + at < n_words ? free_map[first + at] : 0u;
+        const long long left = num_pages - (first + at) * 32;
+        r.word[at] = left <= 0 ? 0u : free_map[first + at] & (left >= 32 ? 0xffffffffu : (1u << left) - 1u);
     }
     __syncthreads();
     int count = 0;
@@ -207,7 +208,7 @@ pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, 
     // ---- are there so many?  (rounds of the map until there are) ----
     int found = 0, rounds = 0;
     if (wanted > 0)
-        for (long long first = 0; first < n_words && found < wanted; first += kRound, ++rounds) found += load_round(s.round, p.d_free, first, n_words, found, s.scan);
+        for (long long first = 0; first < n_words && found < wanted; first += kRound, ++rounds) found += load_round(s.round, p.d_free, first, p.num_pages, found, s.scan);
     // a request is served iff all pages wanted up to and with it are there
     int served = wanted;
     if (found < wanted) served = s.upto[last_at_most(s.upto, B + 1, found)];
@@ -218,7 +219,7 @@ pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, 
         int here = s.round.before[kRound] - s.round.before[0];
         if (rounds > 1) {
             __syncthreads();
-            here = load_round(s.round, p.d_free, first, n_words, base, s.scan);
+            here = load_round(s.round, p.d_free, first, p.num_pages, base, s.scan);
         }
         for (int k = base + tid; k < min(base + here, served); k += kThreads) {
             const int page = nth_free(s.round, first, k);
@@ -319,7 +320,7 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
     if (wanted > 0) {
         // (fresh[b] holds the page's number in the order of the free ones until its round comes, then ~page)
         for (long long first = 0; first < n_words && found < wanted; first += kRound) {
-            const int here = load_round(s.round, p.d_free, first, n_words, found, s.scan);
+            const int here = load_round(s.round, p.d_free, first, p.num_pages, found, s.scan);
             for (int b = tid; b < B; b += kThreads) {
                 const int k = s.fresh[b];
                 if (k >= found && k < found + here) s.fresh[b] = ~nth_free(s.round, first, k) - 1;           // (below -1)
@@ -441,7 +442,10 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
                 p.d_page_table[(size_t)b * width + col] = now;
             }
 #pragma unroll
-            for (int k = 0; k < kForkDeep; ++k) if (left[k] == 0) atomicOr(&p.d_free[page[k] >> 5], 1u << (page[k] & 31));
+            for (int k = 0; k < kForkDeep; ++k) {
+                if (left[k] == 0) atomicOr(&p.d_free[page[k] >> 5], 1u << (page[k] & 31));
+                if (left[k] < 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);          // more entries than refs counts
+            }
         }
     }
 }
@@ -670,8 +674,9 @@ pages_copy_kernel(const CopyArgs a, int* status_word) {
     const long long tasks = (long long)n * 2 * a.Hkv, step = (long long)gridDim.x * kCopyWarps;
     for (long long t = (long long)blockIdx.x * kCopyWarps + (threadIdx.x >> 5); t < tasks; t += step) {
         const int c = (int)(t / (2 * a.Hkv)), rest = (int)(t - (long long)c * 2 * a.Hkv), which = rest / a.Hkv, h = rest - which * a.Hkv;
-        const long long from = a.copies[3 * c], to = a.copies[3 * c + 1];
-        const int rows = min(max(a.copies[3 * c + 2], 0), a.page_size);
+        const int32_t* const line = a.copies + 3 * (long long)c;
+        const long long from = line[0], to = line[1];
+        const int rows = min(max(line[2], 0), a.page_size);
         if (from < 0 || from >= a.num_pages || to < 0 || to >= a.num_pages) {
             if (lane == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
             continue;
@@ -735,7 +740,7 @@ war_status_t launch_cluster(void (*kernel)(Params...), size_t smem, cudaStream_t
 
 war_status_t check_pages(const war_pages_t* p) {
     if (!p || p->B < 0 || p->page_size < 1 || p->max_pages_per_req < 1 || p->num_pages < 1) return WAR_ERR_INVALID_ARG;
-    if (p->B > kMaxB || p->num_pages > (1ll << 30)) return WAR_ERR_UNSUPPORTED;
+    if (p->B > kMaxB || p->num_pages > (1ll << 30) || (long long)p->B * p->max_pages_per_req >= (1ll << 31)) return WAR_ERR_UNSUPPORTED;   // (entries are counted in 32 bits)
     if (p->B > 0 && (!p->d_refs || !p->d_free || !p->d_page_table || !p->d_held)) return WAR_ERR_INVALID_ARG;
     return WAR_OK;
 }

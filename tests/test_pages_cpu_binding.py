@@ -205,7 +205,7 @@ PAGES = {"war_pages_grow": lambda p: (p, 8, SOME, SOME, SOME, None), "war_pages_
 
 @pytest.mark.parametrize("name", list(PAGES))
 @pytest.mark.parametrize("over,status", [(dict(B=-1), INVALID), (dict(page_size=0), INVALID), (dict(max_pages_per_req=0), INVALID), (dict(num_pages=0), INVALID),
-                                         (dict(B=4097), UNSUPPORTED), (dict(num_pages=(1 << 30) + 1), UNSUPPORTED), (dict(d_refs=None), INVALID),
+                                         (dict(B=4097), UNSUPPORTED), (dict(num_pages=(1 << 30) + 1), UNSUPPORTED), (dict(max_pages_per_req=1 << 29), UNSUPPORTED), (dict(d_refs=None), INVALID),
                                          (dict(d_free=None), INVALID), (dict(d_page_table=None), INVALID), (dict(d_held=None), INVALID)])
 def test_books_limits(war, name, over, status):
     assert getattr(war._lib, name)(*PAGES[name](C.byref(books(war, **over)))) == status
