@@ -68,6 +68,8 @@ static_assert(sizeof(FusedPlanScratch) <= kSlots * kSlotBytes, "the plan scratch
 static_assert(kThreads == kFusedThreads, "fused_plan::make is written for the attention kernel's block size");
 static_assert(kThreads * 168 >= 256 * kRegsSoftmax + 128 * kRegsOther, "the hand-over draws on the registers of the launch");
 
+constexpr int kAhead = 2;                                // units whose numbers a CTA holds
+
 struct Bars {
     uint64_t full[kSlots], empty[kSlots];
     uint64_t s_ready[2][2], p_ready[2][2], pv_done[2][2];     // [group][half of a tile]
@@ -75,6 +77,8 @@ struct Bars {
     uint64_t exch;                       // the epilogue's exchange buffer has been written / read
     uint64_t q_ready, stats_ready, epi_done;
     uint64_t part_out, merge_full, merge_free;
+    uint64_t next_full[kAhead], next_free[kAhead];       // shared-prefix variant: numbers of the CTA's units, in the order they are run
+    int next[kAhead];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -115,7 +119,27 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         contiguous = !kShared && a.w.counters[3] != 0 && gridDim.x <= (unsigned)kMaxPlanCtas;
         list_first = contiguous ? a.w.cta_first[blockIdx.x] : 0; list_end = contiguous ? a.w.cta_first[blockIdx.x + 1] : 0;
     }
+    int drawn = blockIdx.x;                          // (shared-prefix variant, lane 0 of the K producer) the number of the next unit
     auto unit_at = [&](int k) -> int {
+        if (kShared) {                               // units are drawn one by one, as in war_verify_attn_shared_sm100.cu
+            const int at = k % kAhead;
+            const uint32_t phase = (uint32_t)(k / kAhead) & 1u;
+            if (warp != kWarpLoadK) {
+                if (!__all_sync(0xffffffffu, wait_for(&bars->next_full[at], phase, bars, a.status_word))) return n_units;
+                const int u = *(volatile int*)&bars->next[at];
+                warp_arrive(&bars->next_free[at], lane);
+                return u;
+            }
+            if (!__all_sync(0xffffffffu, wait_for(&bars->next_free[at], phase ^ 1u, bars, a.status_word))) return n_units;
+            const int u = __shfl_sync(0xffffffffu, min(drawn, n_units), 0);
+            if (lane == 0) {
+                *(volatile int*)&bars->next[at] = u;
+                mbar_arrive(&bars->next_full[at]);
+                if (u < n_units) drawn = (int)gridDim.x + atomicAdd(a.w.counters, 1);
+            }
+            __syncwarp();
+            return u;
+        }
         if (contiguous) return list_first + k < list_end ? list_first + k : n_units;
         return snake_unit(k, blockIdx.x, gridDim.x);
     };
@@ -170,6 +194,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
         mbar_init(&bars->part_out, 4);
         mbar_init(&bars->merge_full, 1);
         mbar_init(&bars->merge_free, 8);
+        for (int i = 0; i < kAhead; ++i) { mbar_init(&bars->next_full[i], 1); mbar_init(&bars->next_free[i], 11); }
         bars->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
