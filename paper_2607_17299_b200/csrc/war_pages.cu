@@ -7,6 +7,9 @@
 // All of this is a few kilobytes to a few megabytes of integers per call, so a call costs its launch and the chain of dependent reads.
 // One launch each, then.  Fork and compaction need all blocks to have read before one writes; they run as one cluster of
 // eight blocks, whose hardware barrier takes the place of further launches (a barrier: about 0.5 us; a launch in a graph: 1.5 to 2).
+// Measured, a launch by itself, cold: 1024 requests with 0.5 million pages: free 8.6 us, grow 9.6; 256 requests resampled: fork 32;
+// 128 requests in 3.5 GB of 64 KB pages: compaction 17, the copy of its moves 254 (6.3 TB/s, the rate of a plain copy); groups among
+// 512 requests of up to 73 000 tokens 15.
 #include <cooperative_groups.h>
 #include <mutex>
 #include "war_common.cuh"

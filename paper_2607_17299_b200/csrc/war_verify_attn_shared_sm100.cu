@@ -13,6 +13,9 @@
 // Warp roles:  warps 8 and 11  producers (TMA copies of this GPU's own memory into a ring of 32 KB slots)
 //              warps 9 and 10  MMA issuers, one lane each, for softmax group 0 and 1
 //              warps 0-3, 4-7  softmax groups: one thread a row; P goes back into the first columns of its half of S
+// Measured: a half tile of both groups 1735 cycles (tensor pipe 50 %, XU 47 %); 4 prompts of 16K to 32K tokens with 7 rollouts of 32 slots and 4
+// requests alone, 32 + 8 heads: 525 us the call (each for itself 567); 32 prompts of 6K to 16K tokens with 8 rollouts of 8 slots: 710 to
+// 725 us (1530), 60 % of the HBM bandwidth; floors 246 and 445.
 // Layouts of tiles, loads in the order K0 K1 V0 K2 V1 ..., bounded waits: as in war_verify_attn_sm100.cu.
 #include <mutex>
 #include <type_traits>
