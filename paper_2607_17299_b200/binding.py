@@ -781,18 +781,33 @@ def new_pages(num_pages: int, B: int, max_pages: int, device) -> Pages:
     return Pages(zeros(num_pages), words.to(device), torch.full((B, max_pages), -1, dtype=torch.int32, device=device), zeros(B))
 
 
-@_by_layout
-def _pages_shapes(refs, free, table, held) -> Tuple[int, int, int]:
-    if len(refs) != 1 or len(table) != 2 or tuple(held) != (table[0],) or tuple(free) != (-(-refs[0] // 32),):
-        raise ValueError("pages must be refs [num_pages], free [ceil(num_pages / 32)], page_table [B, max_pages], held [B]")
-    return table[0], table[1], refs[0]
+def _addresses(dtype, first: torch.Tensor, *others: Optional[torch.Tensor]) -> Tuple[list, int]:
+    """Addresses of contiguous tensors of one type (None stays None), all on the current device, and its current stream: what _ptr and
+    _stream_of look at, in one pass (a call of a few microseconds is bound by this)."""
+    device, at = first.get_device(), []
+    for t in (first, *others):
+        if t is None:
+            at.append(None)
+        elif t.get_device() == device >= 0 and t.dtype is dtype and t.is_contiguous():
+            at.append(t.data_ptr())
+        else:
+            _ptr(t, dtype)
+            break
+    else:
+        current = torch.cuda.current_device()
+        if device == current and _raw_stream is not None:
+            return at, _raw_stream(current)
+    return at, _stream_of(first, *others)
 
 
-def _books(pages: Pages, page_size: int) -> PagesBooks:
+def _books(pages: Pages, page_size: int, *tensors: Optional[torch.Tensor]) -> Tuple[PagesBooks, list, int]:
+    """The structure, the addresses of the call's other tensors, and the stream."""
     refs, free, table, held = pages
-    B, width, num_pages = _pages_shapes(refs.shape, free.shape, table.shape, held.shape)
-    i32 = torch.int32
-    return PagesBooks(_ptr(refs, i32), _ptr(free, i32), _ptr(table, i32), _ptr(held, i32), B, page_size, width, 0, num_pages)
+    n, width = refs.shape, table.shape
+    if len(n) != 1 or len(width) != 2 or held.shape != width[:1] or free.shape != (-(-n[0] // 32),):
+        raise ValueError("pages must be refs [num_pages], free [ceil(num_pages / 32)], page_table [B, max_pages], held [B]")
+    at, stream = _addresses(torch.int32, refs, free, table, held, *tensors)
+    return PagesBooks(at[0], at[1], at[2], at[3], width[0], page_size, width[1], 0, n[0]), at[4:], stream
 
 
 def _same_shape(want, *tensors) -> None:
@@ -802,45 +817,38 @@ def _same_shape(want, *tensors) -> None:
 
 
 def _copy_list(d_copies: torch.Tensor, least: int) -> int:
-    if d_copies.dim() != 2 or d_copies.shape[1] != 3 or d_copies.shape[0] < least:
+    shape = d_copies.shape
+    if len(shape) != 2 or shape[1] != 3 or shape[0] < least:
         raise ValueError(f"d_copies must be int32 [n, 3] with n >= {least}")
-    return d_copies.shape[0]
+    return shape[0]
 
 
 def war_pages_grow(pages: Pages, N: int, page_size: int, d_prefix_len: torch.Tensor, d_tail_len: Optional[torch.Tensor],
                    d_granted: torch.Tensor) -> None:
     """Pages for positions below prefix_len + N of every running request; d_granted [B]: 1 where a request has its room."""
-    i32 = torch.int32
-    books = _books(pages, page_size)
     _same_shape(pages.held.shape, d_prefix_len, d_tail_len, d_granted)
-    code = _lib.war_pages_grow(C.byref(books), N, _ptr(d_prefix_len, i32), _ptr(d_tail_len, i32), _ptr(d_granted, i32),
-                               _stream_of(*pages, d_prefix_len, d_tail_len, d_granted))
-    _check("war_pages_grow", code)
+    books, at, stream = _books(pages, page_size, d_prefix_len, d_tail_len, d_granted)
+    _check("war_pages_grow", _lib.war_pages_grow(C.byref(books), N, *at, stream))
 
 
 def war_pages_fork(pages: Pages, d_src: torch.Tensor, page_size: int, d_prefix_len: torch.Tensor, d_tail: torch.Tensor,
                    d_tail_len: torch.Tensor, d_copies: torch.Tensor, d_n_copies: torch.Tensor, d_ok: torch.Tensor) -> None:
     """Request b becomes a copy of request d_src[b] (-1 or b: stays); d_copies int32 [>= B, 3] and d_n_copies [1] for
     war_pages_copy, once per layer; d_ok [1]: 0 where the pool had too few pages and nothing was changed."""
-    i32 = torch.int32
-    books = _books(pages, page_size)
-    _same_shape(pages.held.shape, d_src, d_prefix_len, d_tail_len)
-    if d_tail.dim() != 2 or d_tail.shape[0] != pages.held.shape[0] or d_n_copies.numel() != 1 or d_ok.numel() != 1:
+    requests, tail = pages.held.shape, d_tail.shape
+    _same_shape(requests, d_src, d_prefix_len, d_tail_len)
+    if len(tail) != 2 or tail[:1] != requests or d_n_copies.numel() != 1 or d_ok.numel() != 1:
         raise ValueError("d_tail must be [B, P], d_n_copies and d_ok one number each")
-    _copy_list(d_copies, pages.held.shape[0])
-    code = _lib.war_pages_fork(C.byref(books), _ptr(d_src, i32), d_tail.shape[1], _ptr(d_prefix_len, i32), _ptr(d_tail, i32),
-                               _ptr(d_tail_len, i32), _ptr(d_copies, i32), _ptr(d_n_copies, i32), _ptr(d_ok, i32),
-                               _stream_of(*pages, d_src, d_prefix_len, d_tail, d_tail_len, d_copies, d_n_copies, d_ok))
-    _check("war_pages_fork", code)
+    _copy_list(d_copies, tail[0])
+    books, at, stream = _books(pages, page_size, d_src, d_prefix_len, d_tail, d_tail_len, d_copies, d_n_copies, d_ok)
+    _check("war_pages_fork", _lib.war_pages_fork(C.byref(books), at[0], tail[1], *at[1:], stream))
 
 
 def war_pages_free(pages: Pages, d_done: torch.Tensor, d_tail_len: Optional[torch.Tensor] = None) -> None:
     """Requests with d_done[b] != 0 give their pages back and, where d_tail_len is given, stop running (tail_len = -1)."""
-    i32 = torch.int32
-    books = _books(pages, 1)
     _same_shape(pages.held.shape, d_done, d_tail_len)
-    _check("war_pages_free", _lib.war_pages_free(C.byref(books), _ptr(d_done, i32), _ptr(d_tail_len, i32),
-                                                 _stream_of(*pages, d_done, d_tail_len)))
+    books, at, stream = _books(pages, 1, d_done, d_tail_len)
+    _check("war_pages_free", _lib.war_pages_free(C.byref(books), at[0], at[1], stream))
 
 
 def new_compact_workspace(pages: Pages) -> torch.Tensor:
@@ -854,15 +862,14 @@ def war_pages_compact(pages: Pages, page_size: int, d_workspace: torch.Tensor, d
                       d_top: torch.Tensor) -> None:
     """Moves used pages to the front of the pool, as many as d_copies int32 [n, 3] has lines for; d_n_copies [1], and d_top [1]: no
     page at or above it is in use.  Workspace from new_compact_workspace."""
-    i32 = torch.int32
-    books = _books(pages, page_size)
     if d_workspace.numel() * d_workspace.element_size() < _lib.war_pages_compact_workspace_bytes(pages.refs.numel()):
         raise ValueError("workspace is smaller than war_pages_compact_workspace_bytes")
     if d_n_copies.numel() != 1 or d_top.numel() != 1:
         raise ValueError("d_n_copies and d_top are one number each")
-    code = _lib.war_pages_compact(C.byref(books), _ptr(d_workspace), _copy_list(d_copies, 0), _ptr(d_copies, i32), _ptr(d_n_copies, i32),
-                                  _ptr(d_top, i32), _stream_of(*pages, d_workspace, d_copies, d_n_copies, d_top))
-    _check("war_pages_compact", code)
+    lines = _copy_list(d_copies, 0)
+    books, at, stream = _books(pages, page_size, d_copies, d_n_copies, d_top)
+    workspace, _ = _addresses(d_workspace.dtype, d_workspace)
+    _check("war_pages_compact", _lib.war_pages_compact(C.byref(books), workspace[0], lines, *at, stream))
 
 
 @_by_layout
@@ -878,23 +885,22 @@ def war_pages_copy(d_copies: torch.Tensor, d_n_copies: torch.Tensor, k_pool: tor
                    k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None) -> None:
     """Applies a list of copies (war_pages_fork, war_pages_compact) to one layer's cache: bf16, or 8-bit with its scales."""
     q = _copy_params(_layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
-    code = _lib.war_pages_copy(_ptr(d_copies, torch.int32), _ptr(d_n_copies, torch.int32), _copy_list(d_copies, 0), _address(k_pool),
-                               _address(v_pool), _address(k_scale), _address(v_scale), C.byref(q),
-                               _stream_of(d_copies, d_n_copies, k_pool, v_pool, k_scale, v_scale))
+    lines = _copy_list(d_copies, 0)
+    at, _ = _addresses(torch.int32, d_copies, d_n_copies)
+    code = _lib.war_pages_copy(at[0], at[1], lines, _address(k_pool), _address(v_pool), _address(k_scale), _address(v_scale), C.byref(q),
+                               _stream_of(k_pool, v_pool, k_scale, v_scale))
     _check("war_pages_copy", code)
 
 
 def war_prefix_groups(d_page_table: torch.Tensor, d_prefix_len: torch.Tensor, d_tail_len: Optional[torch.Tensor], page_size: int,
                       min_shared: int, d_leader: torch.Tensor, d_shared_len: torch.Tensor) -> None:
     """Groups of running requests that share at least min_shared tokens of their prefix: d_leader [B], d_shared_len [B]."""
-    i32 = torch.int32
-    if d_page_table.dim() != 2:
+    shape = d_page_table.shape
+    if len(shape) != 2:
         raise ValueError("d_page_table must be [B, max_pages]")
-    _same_shape(d_page_table.shape[:1], d_prefix_len, d_tail_len, d_leader, d_shared_len)
-    code = _lib.war_prefix_groups(_ptr(d_page_table, i32), _ptr(d_prefix_len, i32), _ptr(d_tail_len, i32), d_page_table.shape[0], page_size,
-                                  d_page_table.shape[1], min_shared, _ptr(d_leader, i32), _ptr(d_shared_len, i32),
-                                  _stream_of(d_page_table, d_prefix_len, d_tail_len, d_leader, d_shared_len))
-    _check("war_prefix_groups", code)
+    _same_shape(shape[:1], d_prefix_len, d_tail_len, d_leader, d_shared_len)
+    at, stream = _addresses(torch.int32, d_page_table, d_prefix_len, d_tail_len, d_leader, d_shared_len)
+    _check("war_prefix_groups", _lib.war_prefix_groups(at[0], at[1], at[2], shape[0], page_size, shape[1], min_shared, at[3], at[4], stream))
 
 
 def war_verify_attn_shared_workspace_bytes(params: AttnParams) -> int:
