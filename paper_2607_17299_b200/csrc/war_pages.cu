@@ -136,6 +136,7 @@ __device__ __forceinline__ int nth_free(const FreeRound& r, long long first, int
 constexpr int kFreeThreads = 256, kFreeDeep = 4;
 __global__ void __launch_bounds__(kFreeThreads)
 pages_free_kernel(war_pages_t p, const int32_t* __restrict__ done, int32_t* tail_len, int* status_word) {
+    war_wait_before();
     const int b = blockIdx.x;
     if (done[b] == 0) return;
     const int held = p.d_held[b];
@@ -180,6 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ tail_len, int32_t* granted,
                   int* status_word) {
     extern __shared__ __align__(16) uint8_t pages_smem[];
+    war_wait_before();
     GrowShared& s = *reinterpret_cast<GrowShared*>(pages_smem);
     const int tid = threadIdx.x, B = p.B;
     const long long n_words = (p.num_pages + 31) / 32;
@@ -267,6 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32_t* prefix_len, int32_t* tail, int32_t* tail_len,
                   int32_t* copies, int32_t* n_copies, int32_t* ok_word, int* status_word) {
     extern __shared__ __align__(16) uint8_t pages_smem[];
+    war_wait_before();
     ForkShared& s = *reinterpret_cast<ForkShared*>(pages_smem);
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, B = p.B, rank = (int)cluster.block_rank(), width = p.max_pages_per_req, page_size = p.page_size;
@@ -467,6 +470,7 @@ struct CompactShared {
 __global__ void __launch_bounds__(kThreads, 1)
 pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies, int32_t* n_copies, int32_t* top, int* status_word) {
     __shared__ CompactShared s;
+    war_wait_before();
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, rank = (int)cluster.block_rank();
     const int n_words = (int)((p.num_pages + 31) / 32);
@@ -585,6 +589,7 @@ prefix_groups_kernel(const int32_t* __restrict__ table, const int32_t* __restric
                      int B, int page_size, int width, int column, int32_t* leader, int32_t* shared_len) {
     __shared__ uint16_t s_member[kMaxB];
     __shared__ int s_members, s_full, s_same;
+    war_wait_before();
     const int tid = threadIdx.x, me = blockIdx.x;
     auto full_of = [&](int b) -> int {                            // full pages of a running request's prefix
         const int pl = prefix_len[b], run = tail_len ? tail_len[b] : 0;
@@ -672,6 +677,7 @@ template <int kLanesPerRow>                // 16-byte pieces of a row: 16 (bf16)
 __global__ void __launch_bounds__(kCopyWarps * 32)
 pages_copy_kernel(const CopyArgs a, int* status_word) {
     constexpr int kRows = 32 / kLanesPerRow, kDeep = 8;
+    war_wait_before();
     const int lane = threadIdx.x & 31, r0 = lane / kLanesPerRow, piece = lane % kLanesPerRow;
     const int n = min(max(*a.n_copies, 0), a.max_copies);
     const long long tasks = (long long)n * 2 * a.Hkv, step = (long long)gridDim.x * kCopyWarps;
@@ -728,19 +734,6 @@ war_status_t device_setup(int* sm_count) {
 }
 static_assert(sizeof(ForkShared) <= 232448 && sizeof(GrowShared) <= 232448, "shared memory");
 
-// One cluster of kCluster blocks.
-template <class... Params, class... Args>
-war_status_t launch_cluster(void (*kernel)(Params...), size_t smem, cudaStream_t stream, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kCluster); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kCluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    WAR_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...));
-    return WAR_OK;
-}
-
 war_status_t check_pages(const war_pages_t* p) {
     if (!p || p->B < 0 || p->page_size < 1 || p->max_pages_per_req < 1 || p->num_pages < 1) return WAR_ERR_INVALID_ARG;
     if (p->B > kMaxB || p->num_pages > (1ll << 30) || (long long)p->B * p->max_pages_per_req >= (1ll << 31)) return WAR_ERR_UNSUPPORTED;   // (entries are counted in 32 bits)
@@ -757,9 +750,7 @@ extern "C" war_status_t war_pages_free(const war_pages_t* p, const int32_t* d_do
     if (!d_done) return WAR_ERR_INVALID_ARG;
     int* status_word = war_status_word();
     if (!status_word) return WAR_ERR_CUDA;
-    pages_free_kernel<<<p->B, kFreeThreads, 0, stream>>>(*p, d_done, d_tail_len, status_word);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(pages_free_kernel, p->B, kFreeThreads, 0, 1, stream, *p, d_done, d_tail_len, status_word);
 }
 
 extern "C" war_status_t war_pages_grow(const war_pages_t* p, int32_t N, const int32_t* d_prefix_len, const int32_t* d_tail_len,
@@ -774,9 +765,7 @@ extern "C" war_status_t war_pages_grow(const war_pages_t* p, int32_t N, const in
     int sms;
     st = device_setup(&sms);
     if (st != WAR_OK) return st;
-    pages_grow_kernel<<<1, kThreads, sizeof(GrowShared), stream>>>(*p, N, d_prefix_len, d_tail_len, d_granted, status_word);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(pages_grow_kernel, 1, kThreads, sizeof(GrowShared), 1, stream, *p, N, d_prefix_len, d_tail_len, d_granted, status_word);
 }
 
 extern "C" war_status_t war_pages_fork(const war_pages_t* p, const int32_t* d_src, int32_t P, int32_t* d_prefix_len, int32_t* d_tail,
@@ -791,7 +780,7 @@ extern "C" war_status_t war_pages_fork(const war_pages_t* p, const int32_t* d_sr
     int sms;
     st = device_setup(&sms);
     if (st != WAR_OK) return st;
-    return launch_cluster(pages_fork_kernel, sizeof(ForkShared), stream, *p, d_src, P, d_prefix_len, d_tail, d_tail_len, d_copies, d_n_copies,
+    return war_launch_behind(pages_fork_kernel, kCluster, kThreads, sizeof(ForkShared), kCluster, stream, *p, d_src, P, d_prefix_len, d_tail, d_tail_len, d_copies, d_n_copies,
                           d_ok, status_word);
 }
 
@@ -810,7 +799,7 @@ extern "C" war_status_t war_pages_compact(const war_pages_t* p, void* d_workspac
     int sms;
     st = device_setup(&sms);
     if (st != WAR_OK) return st;
-    return launch_cluster(pages_compact_kernel, 0, stream, *p, (int32_t*)d_workspace, max_copies, d_copies, d_n_copies, d_top, status_word);
+    return war_launch_behind(pages_compact_kernel, kCluster, kThreads, 0, kCluster, stream, *p, (int32_t*)d_workspace, max_copies, d_copies, d_n_copies, d_top, status_word);
 }
 
 extern "C" war_status_t war_prefix_groups(const int32_t* d_page_table, const int32_t* d_prefix_len, const int32_t* d_tail_len, int32_t B,
@@ -821,10 +810,8 @@ extern "C" war_status_t war_prefix_groups(const int32_t* d_page_table, const int
     if (B == 0) return WAR_OK;
     if (!d_page_table || !d_prefix_len || !d_leader || !d_shared_len) return WAR_ERR_INVALID_ARG;
     const int column = (min_shared - 1) / page_size;
-    prefix_groups_kernel<<<B, kGroupThreads, 0, stream>>>(d_page_table, d_prefix_len, d_tail_len, B, page_size, max_pages_per_req, column,
-                                                         d_leader, d_shared_len);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(prefix_groups_kernel, B, kGroupThreads, 0, 1, stream, d_page_table, d_prefix_len, d_tail_len, B, page_size,
+                             max_pages_per_req, column, d_leader, d_shared_len);
 }
 
 extern "C" war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d_n_copies, int32_t max_copies, void* d_kpool, void* d_vpool,
@@ -852,8 +839,5 @@ extern "C" war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d
     a.Hkv = q->Hkv; a.page_size = q->page_size; a.row_bytes = 128 * size; a.block = quant ? q->scale_block : 0;
     const long long blocks = ((long long)max_copies * 2 * q->Hkv + kCopyWarps - 1) / kCopyWarps;
     const int grid = (int)(blocks < sms * 8ll ? blocks : sms * 8ll);
-    if (quant) pages_copy_kernel<8><<<grid, kCopyWarps * 32, 0, stream>>>(a, status_word);
-    else pages_copy_kernel<16><<<grid, kCopyWarps * 32, 0, stream>>>(a, status_word);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(quant ? pages_copy_kernel<8> : pages_copy_kernel<16>, grid, kCopyWarps * 32, 0, 1, stream, a, status_word);
 }

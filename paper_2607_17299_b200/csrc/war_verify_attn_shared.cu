@@ -79,6 +79,7 @@ attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* _
                         const int32_t* __restrict__ leader, const int32_t* __restrict__ shared_len, int B, int N, int Hkv, int G,
                         int page_size, int max_pages, int n_ctas, int block, SharedWorkspace w, int* status_word) {
     extern __shared__ __align__(16) uint8_t plan_smem[];
+    war_wait_before();
     __shared__ int s_warp[33];
     __shared__ long long s_sum[32];
     PlanArrays a;
@@ -265,6 +266,7 @@ attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* _
 constexpr int kMergeWarps = 8;
 __global__ void __launch_bounds__(kMergeWarps * 32)
 attn_shared_merge_kernel(SharedWorkspace w, int B, int N, int Hq, int Hkv, int G, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
+    war_wait_before();
     const int i = blockIdx.x / Hkv, kvh = blockIdx.x - i * Hkv;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int r = (blockIdx.y * (kMergeWarps / 2) + (warp >> 1)) * 8 + (lane & 7), c0 = (warp & 1) * 16 + (lane >> 3);
@@ -371,18 +373,14 @@ war_status_t launch_plan(const int32_t* prefix_len, const int32_t* num_nodes, co
     const int n_sm = war_attn_sm_count();
     if (n_sm <= 0) return WAR_ERR_CUDA;
     PlanArrays a;
-    attn_shared_plan_kernel<<<1, p->B <= 128 ? kPlanThreads / 4 : kPlanThreads, plan_arrays(&a, nullptr, p->B), s>>>(prefix_len, num_nodes, parent, leader, shared_len, p->B, p->N,
-                                                                              p->Hkv, p->Hq / p->Hkv, p->page_size, p->max_pages_per_req,
-                                                                              n_sm, block, w, status_word);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(attn_shared_plan_kernel, 1, p->B <= 128 ? kPlanThreads / 4 : kPlanThreads, plan_arrays(&a, nullptr, p->B), 1, s, prefix_len,
+                             num_nodes, parent, leader, shared_len, p->B, p->N, p->Hkv, p->Hq / p->Hkv, p->page_size, p->max_pages_per_req, n_sm,
+                             block, w, status_word);
 }
 war_status_t launch_merge(const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse, cudaStream_t s) {
     const int G = p->Hq / p->Hkv;
-    attn_shared_merge_kernel<<<dim3(p->B * p->Hkv, (G * p->N + kMergeWarps * 4 - 1) / (kMergeWarps * 4)), kMergeWarps * 32, 0, s>>>(
-        w, p->B, p->N, p->Hq, p->Hkv, G, (__nv_bfloat16*)out, lse);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(attn_shared_merge_kernel, dim3(p->B * p->Hkv, (G * p->N + kMergeWarps * 4 - 1) / (kMergeWarps * 4)), kMergeWarps * 32, 0, 1,
+                             s, w, p->B, p->N, p->Hq, p->Hkv, G, (__nv_bfloat16*)out, lse);
 }
 
 }  // namespace
