@@ -114,6 +114,7 @@ attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_c
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int n_units = 0, list_first = 0, list_end = 0;
     bool contiguous = false;
+    if (kShared) war_wait_before();                  // (launched behind the plan)
     if (!kFused) {
         n_units = a.w.counters[1];
         // k-th unit of this CTA: its own contiguous list, or the snake deal of the longest-first list
@@ -860,7 +861,5 @@ war_status_t war_attn_quant_launch_shared(const void* q, const AttnQuantPools& p
     if (!quant_kernel_args(q, pools, page_table, nullptr, nullptr, parent, p, parts, false, out, lse, status_word, &a, &k_map, &v_map))
         return WAR_ERR_UNSUPPORTED;
     a.shared_units = w.units; a.shared_parts = w.parts; a.slot_map = w.slot_map;
-    attn_quant_many_kernel<false, true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(attn_quant_many_kernel<false, true>, grid, kThreads, kSmemBytes, 1, s, k_map, v_map, a);
 }

@@ -158,6 +158,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
+    war_wait_before();                                              // the plan
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, bars->tmem_base, 0);
@@ -602,8 +603,5 @@ war_status_t war_attn_shared_launch(const void* q, const void* k, const void* v,
     a.part_ml = w.part_ml; a.part_o = w.part_o; a.out = (__nv_bfloat16*)out; a.lse = lse; a.status_word = status_word;
     a.num_pages = p->num_pages; a.scale_log2 = p->scale * kLog2e;
     a.N = p->N; a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.page_size = p->page_size; a.max_pages = p->max_pages_per_req;
-    if (token_major) attn_shared_kernel<true><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
-    else attn_shared_kernel<false><<<grid, kThreads, kSmemBytes, s>>>(k_map, v_map, a);
-    WAR_LAUNCH_CHECK();
-    return WAR_OK;
+    return war_launch_behind(token_major ? attn_shared_kernel<true> : attn_shared_kernel<false>, grid, kThreads, kSmemBytes, 1, s, k_map, v_map, a);
 }
