@@ -1,4 +1,4 @@
-"""Books of a pool for the tests: the checker's lists and the library's arrays of the same state."""
+"""Books of a pool for the tests: the oracle's lists and the library's arrays of the same state."""
 import copy
 
 import numpy as np

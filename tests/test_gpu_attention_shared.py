@@ -1,4 +1,4 @@
-"""GPU parity: attention over shared prefixes against the fp64 checker, which looks at every request by itself.
+"""GPU parity: attention over shared prefixes against the fp64 oracle, which looks at every request by itself.
 
 Tolerances.  bf16 cache: the weights are rounded to bf16 once (2^-8 of themselves), their sum is not, and the output once more, so
 per element  |error| <= 2^-8 |out| + 1.05 * 2^-8 * sum w |v|  (w: the exact weights; 5 % for 32-bit sums, the fast exp2 and products of roundings); the log-sum-exp sees 32-bit
@@ -144,7 +144,7 @@ CASES = [
 
 
 @pytest.mark.parametrize("case", CASES, ids=[str(c[0]) for c in CASES])
-def test_matches_checker(war, case):
+def test_matches_oracle(war, case):
     c = Case(*case)
     c.check(*c.run(war))
     assert war.war_device_status() == 0

@@ -1,4 +1,4 @@
-"""GPU parity: the calls that keep a pool's books against the checker's lists, exactly; and the copies that follow from them."""
+"""GPU parity: the calls that keep a pool's books against the oracle's lists, exactly; and the copies that follow from them."""
 import numpy as np
 import pytest
 import torch
@@ -141,7 +141,7 @@ def test_free_then_grow(war, size):
 def test_compact(war, size, most_copies):
     B, page, most, spare = size
     if B > 64 and most_copies > 3:
-        B = 64                                                          # (the checker moves one page at a time)
+        B = 64                                                          # (the oracle moves one page at a time)
     b = U.random_books(np.random.default_rng(9), B, page, most, spare)
     d = U.Device(war, b)
     n = min(most_copies, b.num_pages)

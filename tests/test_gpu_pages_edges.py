@@ -185,3 +185,46 @@ def test_an_empty_pool_and_a_full_one(war):
     war.war_pages_free(p, t([1, 0]))
     assert [int(x) & 0xffffffff for x in p.free.tolist()] == [0xffffffff, 1] and not p.refs.any()
     assert war.war_device_status() == 0
+
+
+def test_captured_behind_other_work(war):
+    """Calls whose predecessor in a graph is a fill, a copy, a kernel of another stream or one of the set: each waits for what it is
+    behind, and what follows waits for it."""
+    b = books()
+    b.width = 12
+    d = U.Device(war, b)
+    state = [x.clone() for x in (*d.pages, d.prefix, d.tail, d.tail_len)]
+    back = list(zip((*d.pages, d.prefix, d.tail, d.tail_len), state))
+    src, done, x, y = t([-1, -1, -1, 0]), t([0, 1, 0, 0]), torch.zeros(1 << 24, device=DEV), torch.zeros(1 << 24, device=DEV)
+    leader, shared, seen = t([-7] * 4), t([-7] * 4), t([-7] * 4)
+    fork(war, d, [-1] * 4, 4)                                                    # (one-time set-up of the device)
+    other = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        main = torch.cuda.current_stream()
+        for a, c in back:
+            a.copy_(c)
+        d.granted.zero_()
+        war.war_pages_fork(d.pages, src, 4, d.prefix, d.tail, d.tail_len, d.copies, d.n, d.word)
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            x.add_(1)
+            y.copy_(x)
+            d.prefix.add_(1)                                                     # seen by the calls behind the meeting
+        main.wait_stream(other)
+        war.war_pages_free(d.pages, done, d.tail_len)
+        war.war_pages_grow(d.pages, 3, 4, d.prefix, d.tail_len, d.granted)
+        war.war_prefix_groups(d.pages.page_table, d.prefix, d.tail_len, 4, 4, leader, shared)
+        seen.copy_(leader)
+    ok, copies = O.fork(b, src.tolist(), 4)
+    b.prefix = [v + 1 for v in b.prefix]
+    O.release(b, done.tolist())
+    want = O.grow(b, 3, 4)
+    groups = O.groups(b.rows, b.prefix, [v >= 0 for v in b.tail_len], 4, 4)
+    for _ in range(20):
+        g.replay()
+    torch.cuda.synchronize()
+    assert ok and d.listed() == copies and d.granted.tolist() == want
+    d.check(b)
+    assert seen.tolist() == groups[0] and shared.tolist() == groups[1] and float(y[-1]) == 20
+    assert war.war_device_status() == 0

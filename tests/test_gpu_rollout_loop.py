@@ -3,7 +3,7 @@ pages back, starts new ones as copies of running ones, makes room, stores a tree
 attention over their shared prefixes, picks the target's tokens, accepts and commits; now and then the pool is compacted.
 
 Checked at every step: the books against plain lists; what every request's cache holds, through its own table, bit for bit across
-forks, copies and compaction; attention against the fp64 checker on that (bounds of test_gpu_attention_shared.py); acceptance."""
+forks, copies and compaction; attention against the fp64 oracle on that (bounds of test_gpu_attention_shared.py); acceptance."""
 import numpy as np
 import pytest
 import torch

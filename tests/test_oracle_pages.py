@@ -1,4 +1,4 @@
-"""Pins of the checker for pages: hand-worked cases, and identities that any books keep."""
+"""Pins of the oracle for pages: hand-worked cases, and identities that any books keep."""
 import numpy as np
 import pytest
 
