@@ -65,11 +65,19 @@ inline SharedWorkspace war_attn_shared_layout(const war_attn_params_t* p, void* 
     return w;
 }
 
-// The attention kernels on such a plan (war_verify_attn_shared_sm100.cu, war_verify_attn_quant_many.cu).
+// The attention kernels on such a plan: war_verify_attn_shared_sm100.cu; war_verify_attn_quant_many.cu up to kQuantWideRows query rows per request
+// and kv head, above war_verify_attn_shared_quant_sm100.cu.  The latter has twice the rows in a unit, the former more of a cache in flight where
+// memory is the bound, the requests' own keys.  In turn on one GPU (us, former / latter): 4 rows, 4K to 8K own keys 504 / 645; 32 rows
+// 16 prompts of 4 338 / 347, one of 16 264 / 240; 64 rows, 8K own keys 257 / 290, 4 prompts of 4 with 32K 271 / 236; 68 and 80 rows, 8K own keys
+// 300 / 308, 304 / 312, with 4 rollouts of 12K shared 376 / 366; 128 rows 331 / 329, 721 / 637, 517 / 460; 256 rows 562 / 495, 680 / 588.
+constexpr int kQuantWideRows = 64;
 war_status_t war_attn_shared_launch(const void* q, const void* k, const void* v, const int32_t* page_table, const int32_t* parent,
                                     const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse,
                                     int* status_word, cudaStream_t s);
 war_status_t war_attn_quant_launch_shared(const void* q, const AttnQuantPools& pools, const int32_t* page_table, const int32_t* parent,
+                                          const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse,
+                                          int* status_word, cudaStream_t s);
+war_status_t war_attn_quant_launch_shared_wide(const void* q, const AttnQuantPools& pools, const int32_t* page_table, const int32_t* parent,
                                           const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse,
                                           int* status_word, cudaStream_t s);
 
@@ -84,5 +92,22 @@ __device__ __forceinline__ SharedUnit shared_unit(const uint2* units, const Shar
     x.tile_begin = c * x.part.each + min(c, x.part.more); x.tile_end = x.tile_begin + x.part.each + (c < x.part.more ? 1 : 0);
     x.part0 = x.part.part0 + (c * Hkv + x.kvh) * x.part.rows;
     return x;
+}
+
+// The loads of a unit of T tiles are K0, K1, V0, K2, V1, ..., K(T-1), V(T-2), V(T-1); ld0: loads before the unit.
+__device__ __forceinline__ uint32_t load_k(uint32_t ld0, int t) { return t == 0 ? ld0 : ld0 + 2u * t - 1u; }
+__device__ __forceinline__ uint32_t load_v(uint32_t ld0, int t, int T) { return t == T - 1 ? ld0 + 2u * T - 1u : ld0 + 2u * t + 2u; }
+
+// a number twice, as a packed pair; the sum of four packed pairs
+__device__ __forceinline__ uint64_t pair_of(float x) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float sum_of(uint64_t s0, uint64_t s1, uint64_t s2, uint64_t s3) {
+    float r;
+    asm("{\n.reg .f32 a, b;\nadd.rn.f32x2 %1, %1, %2;\nadd.rn.f32x2 %3, %3, %4;\nadd.rn.f32x2 %1, %1, %3;\nmov.b64 {a, b}, %1;\nadd.rn.f32 %0, a, b;\n}\n"
+        : "=f"(r), "+l"(s0), "+l"(s1), "+l"(s2), "+l"(s3));
+    return r;
 }
 #endif

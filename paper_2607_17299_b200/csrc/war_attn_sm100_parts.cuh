@@ -48,6 +48,15 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, BarsT* 
     return true;
 }
 
+// Has the phase completed?  (mbarrier.try_wait may hold the thread for a while, test_wait never does.)
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+
 // One arrival for a whole warp: 32 lanes arriving on one barrier queue up behind each other.
 __device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
     __syncwarp();

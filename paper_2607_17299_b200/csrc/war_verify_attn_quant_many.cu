@@ -11,8 +11,8 @@
 // Splitting the small operands keeps the tensor work of the bf16 kernel per key (sixteen products of 64 cycles a tile).  Converting the
 // cache to 16 bits on chip instead would move every element through shared memory three more times (read, written twice as
 // wide, read twice as wide by the tensor cores): 192 KB a tile, 1500 cycles, above the 1400 that HBM needs for a tile but
-// below the 3400 that this kernel takes.  (Tried for shared prefixes, whose units it also runs, with four more warps that widen tiles for the bf16
-// kernel's softmax: 645 us against 728 with 32-slot trees, but 647 against 518 where requests have long keys of their own.)
+// below the 3400 that this kernel takes.  For shared prefixes, whose units this kernel runs up to 64 rows a request, war_verify_attn_shared_quant_sm100.cu
+// does so above.
 // A tile of 128 keys is 16 KB of K and 16 KB of V, rows of 128 bytes in the 128-byte swizzle, for either memory order: one
 // tensor map (d, token, head, page) with the pool's own strides, one copy per (page, head).  The scales of a tile travel
 // with it, sixteen 4-byte asynchronous copies for K and for V, so that no softmax warp waits for global memory.

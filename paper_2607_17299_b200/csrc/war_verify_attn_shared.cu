@@ -435,8 +435,9 @@ extern "C" war_status_t war_verify_attn_shared_quant(const void* d_q, const void
     for (int i = 0; i < 3; ++i) { pools.ks[i] = p->k_strides[i]; pools.vs[i] = p->v_strides[i]; }
     pools.kv = qp->kv_type; pools.block = qp->scale_block;
     const SharedWorkspace w = war_attn_shared_layout(p, d_workspace);
-    st = launch_plan(d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len, p, kSharedQuantBlock, w, status_word, stream);
+    const bool wide = p->Hq / p->Hkv * p->N > kQuantWideRows;
+    st = launch_plan(d_prefix_len, d_num_nodes, d_parent, d_leader, d_shared_len, p, wide ? kSharedBlock : kSharedQuantBlock, w, status_word, stream);
     if (st != WAR_OK) return st;
-    st = war_attn_quant_launch_shared(d_q, pools, d_page_table, d_parent, p, w, d_out, d_lse, status_word, stream);
+    st = (wide ? war_attn_quant_launch_shared_wide : war_attn_quant_launch_shared)(d_q, pools, d_page_table, d_parent, p, w, d_out, d_lse, status_word, stream);
     return st == WAR_OK ? launch_merge(p, w, d_out, d_lse, stream) : st;
 }

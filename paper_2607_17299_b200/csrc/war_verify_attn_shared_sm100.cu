@@ -56,19 +56,8 @@ struct Bars {
 };
 static_assert(sizeof(Bars) <= 512, "barrier block");
 
-// The loads of a unit of T tiles are K0, K1, V0, K2, V1, ..., K(T-1), V(T-2), V(T-1); load n of the CTA goes into ring slot n % 5.  Its
-// barriers are number n % 8: with more barriers than loads in flight a parity tells a load's phase from any other that can be asked for.
-__device__ __forceinline__ uint32_t load_k(uint32_t ld0, int t) { return t == 0 ? ld0 : ld0 + 2u * t - 1u; }
-__device__ __forceinline__ uint32_t load_v(uint32_t ld0, int t, int T) { return t == T - 1 ? ld0 + 2u * T - 1u : ld0 + 2u * t + 2u; }
-
-// Has the phase completed?  (mbarrier.try_wait may hold the thread for a while, test_wait never does.)
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-    return ok != 0;
-}
+// Load n of the CTA (see load_k) goes into ring slot n % 5.  Its barriers are number n % 8: with more barriers than loads in flight a
+// parity tells a load's phase from any other that can be asked for.
 
 // Two elements of a softmax row: P = exp2(x * scale - m) as packed bf16, added to a pair of sums in 32 bits.  Written as one
 // block of packed 32-bit instructions: with the intrinsics the same instructions take 13 % longer (two groups, 64 columns: 1318 cycles
@@ -84,17 +73,6 @@ __device__ __forceinline__ void weights2(uint32_t x0, uint32_t x1, uint64_t scal
         "add.rn.f32x2 %1, %1, y;\n"
         "cvt.rn.bf16x2.f32 %0, b, a;\n}\n"
         : "=r"(packed), "+l"(sum2) : "r"(x0), "r"(x1), "l"(scale2), "l"(neg_m2));
-}
-__device__ __forceinline__ uint64_t pair_of(float x) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ float sum_of(uint64_t s0, uint64_t s1, uint64_t s2, uint64_t s3) {
-    float r;
-    asm("{\n.reg .f32 a, b;\nadd.rn.f32x2 %1, %1, %2;\nadd.rn.f32x2 %3, %3, %4;\nadd.rn.f32x2 %1, %1, %3;\nmov.b64 {a, b}, %1;\nadd.rn.f32 %0, a, b;\n}\n"
-        : "=f"(r), "+l"(s0), "+l"(s1), "+l"(s2), "+l"(s3));
-    return r;
 }
 
 struct KernelArgs {

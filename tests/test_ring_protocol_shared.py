@@ -162,3 +162,73 @@ def test_a_slot_is_free_only_when_both_users_are_through():
     with pytest.raises(Broken):
         for _ in range(300):
             Model(units(rng), rng, stragglers=0.02, early=True)
+
+
+class WideningModel(Model):
+    """war_verify_attn_shared_quant_sm100.cu: the producers' loads go into two slots of codes, load n with barriers n % 4; four wideners, a
+    quarter of each load apiece, wait for the codes and for the ring's slot (four of them) and bring the load into it."""
+
+    SLOTS, STAGES, STAGE_BARS = 4, 2, 4
+
+    def __init__(self, units, rng, stragglers, bars=BARS, stage_bars=STAGE_BARS):
+        self.units, self.rng, self.stragglers, self.bars, self.early, self.stage_bars = units, rng, stragglers, bars, False, stage_bars
+        self.full, self.empty = [Barrier(4) for _ in range(bars)], [Barrier(2) for _ in range(bars)]
+        self.codes_full, self.codes_empty = [Barrier(2) for _ in range(stage_bars)], [Barrier(4) for _ in range(stage_bars)]
+        self.codes = [[None] * self.STAGES for _ in range(2)]            # each producer's half of a slot
+        self.quarters = [[None] * self.SLOTS for _ in range(4)]          # each widener's quarter of a slot
+        self.flying, self.now, self.s, self.p, self.pv = [], 0, set(), set(), set()
+        actors = [self.producer(0), self.producer(1), *(self.widener(w) for w in range(4)), self.issuer(0), self.issuer(1), self.softmax(0), self.softmax(1)]
+        waits = [next(a, None) for a in actors]
+        while any(w is not None for w in waits):
+            self.now += 1
+            for x in [x for x in self.flying if x[0] <= self.now]:
+                self.flying.remove(x)
+                self.codes[x[2]][x[1] % self.STAGES] = x[1]
+                self.codes_full[x[1] % stage_bars].land()
+            ready = [i for i, w in enumerate(waits) if w is not None and w()]
+            if ready:
+                i = rng.choice(ready)
+                waits[i] = next(actors[i], None)
+            elif not self.flying:
+                raise Broken("nobody can go on")
+
+    def at_stage(self, bars, ld):
+        return lambda: bars[ld % self.stage_bars].passed((ld // self.stage_bars) & 1)
+
+    def producer(self, half):
+        for ld in range(2 * sum(T for T, _ in self.units)):
+            if ld >= self.STAGES:
+                yield self.at_stage(self.codes_empty, ld - self.STAGES)
+            self.codes_full[ld % self.stage_bars].arrive(tx=1)
+            late = self.rng.random() < self.stragglers
+            self.flying.append((self.now + self.rng.randint(1, 400 if late else 12), ld, half))
+
+    def widener(self, w):
+        for ld in range(2 * sum(T for T, _ in self.units)):
+            yield self.at_stage(self.codes_full, ld)
+            if ld >= self.SLOTS:
+                yield self.at(self.empty, ld - self.SLOTS)
+            for _ in range(self.rng.randint(0, 2)):
+                yield lambda: True
+            if any(c[ld % self.STAGES] != ld for c in self.codes):
+                raise Broken("codes are widened before they are there, or after the slot was given up")
+            self.quarters[w][ld % self.SLOTS] = ld
+            self.codes_empty[ld % self.stage_bars].arrive()
+            self.full[ld % self.bars].arrive()
+
+    def use(self, ld):
+        if any(q[ld % self.SLOTS] != ld for q in self.quarters):
+            raise Broken("a slot is used before its load is there, or after it was given up")
+
+
+def test_widened_loads_are_used_when_they_are_there():
+    rng = random.Random(4)
+    for _ in range(200):
+        WideningModel(units(rng), rng, stragglers=rng.choice([0.0, 0.02, 0.2]))
+
+
+def test_one_barrier_would_not_tell_the_codes_apart():
+    rng = random.Random(5)
+    with pytest.raises(Broken):
+        for _ in range(300):
+            WideningModel(units(rng), rng, stragglers=0.05, stage_bars=1)
