@@ -228,3 +228,26 @@ def test_captured_behind_other_work(war):
     d.check(b)
     assert seen.tolist() == groups[0] and shared.tolist() == groups[1] and float(y[-1]) == 20
     assert war.war_device_status() == 0
+
+
+def test_behind_an_event_of_another_stream(war):
+    """Not captured: the calls wait for what their stream waits for, not only for the kernel that they are behind."""
+    b = books()
+    b.width = 12
+    d = U.Device(war, b)
+    prefix, leader, shared = d.prefix.clone(), t([-7] * 4), t([-7] * 4)
+    other, x = torch.cuda.Stream(), torch.zeros(1 << 20, device=DEV)
+    for k in range(1, 21):
+        main = torch.cuda.current_stream()
+        other.wait_stream(main)
+        with torch.cuda.stream(other):
+            torch.cuda._sleep(300_000)
+            prefix.copy_(d.prefix + k)
+        x.add_(1)
+        main.wait_stream(other)
+        war.war_prefix_groups(d.pages.page_table, prefix, d.tail_len, 4, 4, leader, shared)
+        torch.cuda.synchronize()
+        want = O.groups(b.rows, [min(v + k, 4 * len(r)) for v, r in zip(b.prefix, b.rows)], [v >= 0 for v in b.tail_len], 4, 4)
+        assert (leader.tolist(), shared.tolist()) == want, k
+        leader.fill_(-7)
+    assert war.war_device_status() == 0
