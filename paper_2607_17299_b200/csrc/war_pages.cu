@@ -461,6 +461,9 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
 // ------------------------------------------------------------------------------------------------
 // The i-th highest used page goes to the i-th lowest free page while it lies above it.  With U pages in use that moves exactly the
 // used pages at or above U, so the two lists are the free pages below U, upwards, and the used ones from U on, downwards.
+// place[] says where in its list a page stands, and counts for nothing unless the list has the page there: only listed pages are written, so
+// for any other it holds what the workspace held.  That tells a held page that the map has as free, on either side of U, without a word for
+// every page of the pool.
 struct CompactShared {
     int2 warp[32];
     int used;                              // of this block's words
@@ -474,7 +477,7 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, rank = (int)cluster.block_rank();
     const int n_words = (int)((p.num_pages + 31) / 32);
-    int32_t* const place = ws;                                    // [num_pages] where a used page from U on goes
+    int32_t* const place = ws;                                    // [num_pages] a listed page's position
     int32_t* const to = ws + p.num_pages;                         // free pages below U
     int32_t* const from = to + p.num_pages;                       // used pages from U on
     const int per = (n_words + kCluster - 1) / kCluster, w0 = min(n_words, rank * per), w1 = min(n_words, w0 + per);
@@ -531,7 +534,7 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
             const int i = i0 + k * kCluster * kThreads;
-            a[k] = i < moves ? from[i] : 0; c[k] = i < done ? to[i] : a[k];
+            a[k] = i < moves ? from[i] : 0; c[k] = i < moves ? to[i] : 0;
         }
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) refs[k] = i0 + k * kCluster * kThreads < done ? p.d_refs[a[k]] : 0;
@@ -539,7 +542,7 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
         for (int k = 0; k < kDeep; ++k) {
             const int i = i0 + k * kCluster * kThreads;
             if (i >= moves) break;
-            place[a[k]] = c[k];
+            place[a[k]] = i; place[c[k]] = i;
             if (i >= done) continue;
             p.d_refs[c[k]] = refs[k];
             p.d_refs[a[k]] = 0;
@@ -559,20 +562,24 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
         int32_t* row = p.d_page_table + (size_t)b * p.max_pages_per_req;
         if (held < 0 || held > p.max_pages_per_req) { if (lane == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
         for (int j0 = lane; j0 < held; j0 += 32 * 2 * kDeep) {
-            int page[2 * kDeep], now[2 * kDeep];
+            int page[2 * kDeep], at[2 * kDeep], listed[2 * kDeep], now[2 * kDeep];
 #pragma unroll
-            for (int k = 0; k < 2 * kDeep; ++k) page[k] = j0 + k * 32 < held ? row[j0 + k * 32] : 0;
+            for (int k = 0; k < 2 * kDeep; ++k) page[k] = j0 + k * 32 < held ? row[j0 + k * 32] : -1;
+#pragma unroll
+            for (int k = 0; k < 2 * kDeep; ++k) at[k] = page[k] >= 0 && page[k] < p.num_pages ? place[page[k]] : -1;
 #pragma unroll
             for (int k = 0; k < 2 * kDeep; ++k) {
-                const bool bad = page[k] < 0 || page[k] >= p.num_pages;
-                if (bad) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
-                now[k] = !bad && page[k] >= U && j0 + k * 32 < held ? place[page[k]] : -1;
+                if (at[k] >= moves) at[k] = -1;
+                listed[k] = at[k] < 0 ? -1 : page[k] < U ? to[at[k]] : from[at[k]];
+                now[k] = at[k] < 0 || page[k] < U ? -1 : at[k] < done ? to[at[k]] : page[k];
             }
 #pragma unroll
             for (int k = 0; k < 2 * kDeep; ++k) {
-                if (j0 + k * 32 >= held || page[k] < U || page[k] >= p.num_pages) continue;
-                if (now[k] < 0 || now[k] >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);   // (a held page marked as free)
-                else row[j0 + k * 32] = now[k];
+                if (j0 + k * 32 >= held) continue;
+                // outside the pool; a free one of the list below U; none of the used ones from U on
+                const bool bad = page[k] < 0 || page[k] >= p.num_pages || (page[k] < U ? listed[k] == page[k] : listed[k] != page[k]);
+                if (bad) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+                else if (page[k] >= U) row[j0 + k * 32] = now[k];
             }
         }
     }

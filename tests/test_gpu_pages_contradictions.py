@@ -1,0 +1,93 @@
+"""Books that contradict themselves: a held page that refs does not count and the free map offers, pages outside the pool, and calls
+for no requests.  Such books are reported, no other request's entries or pages change for them, and what the call leaves has a bit
+set iff refs is 0."""
+import pytest
+import torch
+
+from oracle import pages_oracle as O
+from tests import pages_util as U
+from tests.test_gpu_pages import DEV, fork, t
+
+pytestmark = pytest.mark.gpu
+BAD_PAGE = 8
+
+
+@pytest.fixture(scope="module")
+def war():
+    from paper_2607_17299_b200 import binding
+    return binding
+
+
+def uncount(d, page):
+    """One entry that holds the page is not counted any more."""
+    d.pages.refs[page] -= 1
+    d.pages.free.copy_(torch.from_numpy(U.words(d.pages.refs.tolist())))
+
+
+def agree(d):
+    refs = d.pages.refs.tolist()
+    assert min(refs) >= 0 and d.pages.free.tolist() == U.words(refs).tolist()
+    return refs
+
+
+def compact(war, d, ws, most=8, page=4):
+    lines = torch.zeros((most, 3), dtype=torch.int32, device=DEV)
+    war.war_pages_compact(d.pages, page, ws, lines, d.n, d.word)
+    torch.cuda.synchronize()
+    return [tuple(x[:2]) for x in lines[:int(d.n)].tolist()]
+
+
+@pytest.mark.parametrize("left", [0, 1, 2, 3, -1, 0x7FFFFFFF])
+def test_compaction_of_a_page_that_is_marked_free(war, left):
+    """Whatever the workspace held before, the entry stays as it is."""
+    d = U.Device(war, O.Books(4, 3, [[0], [3]], [4, 4], [[1], [2]], [1, 1]))
+    uncount(d, 3)
+    ws = war.new_compact_workspace(d.pages)
+    ws.view(torch.int32).fill_(left)
+    assert compact(war, d, ws) == [] and int(d.word) == 1
+    assert war.war_device_status() == BAD_PAGE
+    assert d.pages.page_table.tolist() == [[0, -1, -1], [3, -1, -1]] and agree(d) == [1, 0, 0, 0]
+
+
+def test_compaction_after_another_one_with_the_same_workspace(war):
+    d = U.Device(war, O.Books(6, 2, [[0], [5], [3]], [4, 4, 4], [[1], [2], [3]], [1, 1, 1]))
+    ws = war.new_compact_workspace(d.pages)
+    assert compact(war, d, ws) == [(5, 1), (3, 2)] and war.war_device_status() == 0
+    d = U.Device(war, O.Books(6, 2, [[0], [5], [3]], [4, 4, 4], [[1], [2], [3]], [1, 1, 1]))
+    uncount(d, 5)
+    assert compact(war, d, ws) == [(3, 1)] and war.war_device_status() == BAD_PAGE
+    assert d.pages.page_table[:, 0].tolist() == [0, 5, 1] and agree(d) == [1, 1, 0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("left", [0, 1, -1])
+@pytest.mark.parametrize("most", [0, 1, 8])
+def test_compaction_onto_a_page_that_is_held(war, left, most):
+    """Below the pages in use, the free map gives the page away; its holder is reported, moved or not."""
+    d = U.Device(war, O.Books(6, 2, [[0], [5], [3]], [4, 4, 4], [[1], [2], [3]], [1, 1, 1]))
+    uncount(d, 0)
+    ws = war.new_compact_workspace(d.pages)
+    ws.view(torch.int32).fill_(left)
+    assert compact(war, d, ws, most) == [(5, 0), (3, 1)][:most] and war.war_device_status() == BAD_PAGE
+    assert d.pages.page_table[:, 0].tolist() == [0, 5 if most < 1 else 0, 3 if most < 2 else 1]
+    agree(d)
+
+
+@pytest.mark.parametrize("left", [0, -1])
+def test_compaction_of_many_pages_with_a_few_uncounted(war, left):
+    """Both sides of the pages in use, words of all blocks, against the counted entries alone."""
+    n = 3000
+    place = torch.randperm(n, generator=torch.Generator().manual_seed(3)).tolist()
+    rows = [place[40 * i:40 * i + 40] for i in range(45)]
+    lost = [(3, 7), (11, 0), (44, 39), (20, 20), (29, 1)]
+    d = U.Device(war, O.Books(n, 50, rows, [160] * 45, [[0]] * 45, [1] * 45))
+    for i, j in lost:
+        uncount(d, rows[i][j])
+    ws = war.new_compact_workspace(d.pages)
+    ws.view(torch.int32).fill_(left)
+    counted = O.Books(n, 50, [[p for j, p in enumerate(r) if (i, j) not in lost] for i, r in enumerate(rows)], [160] * 45, [[0]] * 45, [1] * 45)
+    copies, top = O.compact(counted, 700, 4)
+    assert compact(war, d, ws, 700) == [c[:2] for c in copies] and int(d.word) == top
+    assert war.war_device_status() == BAD_PAGE and agree(d) == counted.refs()
+    for i, r in enumerate(d.pages.page_table.tolist()):
+        assert [p for j, p in enumerate(r[:40]) if (i, j) not in lost] == counted.rows[i], i
+        assert all(r[j] == rows[i][j] for k, j in lost if k == i), i
