@@ -1,6 +1,7 @@
 """Books that contradict themselves: a held page that refs does not count and the free map offers, pages outside the pool, and calls
 for no requests.  Such books are reported, no other request's entries or pages change for them, and what the call leaves has a bit
 set iff refs is 0."""
+import numpy as np
 import pytest
 import torch
 
@@ -91,3 +92,91 @@ def test_compaction_of_many_pages_with_a_few_uncounted(war, left):
     for i, r in enumerate(d.pages.page_table.tolist()):
         assert [p for j, p in enumerate(r[:40]) if (i, j) not in lost] == counted.rows[i], i
         assert all(r[j] == rows[i][j] for k, j in lost if k == i), i
+
+
+def books():
+    return O.Books(40, 6, [[3, 4, 5], [3, 4, 9], [20, 21], []], [10, 11, 8, 0], [[1], [2], [3], [4]], [1, 1, 1, -1])
+
+
+def test_fork_of_a_page_that_is_not_counted(war):
+    """The copies count, and the page is not given out any more."""
+    d = U.Device(war, books())
+    uncount(d, 20)
+    fork(war, d, [-1, -1, -1, 2], 4)
+    assert war.war_device_status() == BAD_PAGE and int(d.word) == 1 and int(d.n) == 0
+    assert d.pages.page_table[3].tolist() == [20, 21, -1, -1, -1, -1]
+    refs = agree(d)
+    assert refs[20] == 1 and refs[21] == 2
+    war.war_pages_grow(d.pages, 16, 4, d.prefix, d.tail_len, d.granted)
+    table = d.pages.page_table.tolist()
+    assert d.granted.tolist() == [0, 0, 1, 1] and [r.count(20) for r in table] == [0, 0, 1, 1]      # (26 and 27 positions: too many for a row)
+    assert war.war_device_status() == BAD_PAGE
+
+
+def test_fork_in_place_of_a_page_that_is_not_counted(war):
+    d = U.Device(war, books())
+    uncount(d, 20)
+    fork(war, d, [-1, -1, 0, -1], 4)
+    assert war.war_device_status() == BAD_PAGE and int(d.word) == 1 and d.listed() == [(5, 0, 2)]
+    assert d.pages.page_table[2].tolist() == [3, 4, 0, -1, -1, -1]
+    refs = agree(d)
+    assert [refs[x] for x in (0, 3, 4, 20, 21)] == [1, 3, 3, 0, 0]
+
+
+def test_fork_in_place_of_two_entries_of_which_one_is_counted(war):
+    d = U.Device(war, books())
+    uncount(d, 3)
+    fork(war, d, [2, 2, -1, -1], 4)
+    assert war.war_device_status() == BAD_PAGE
+    refs = agree(d)
+    assert [refs[x] for x in (3, 4, 5, 9, 20, 21)] == [0, 0, 0, 0, 3, 3]
+
+
+def test_fork_that_gives_out_a_page_of_its_source(war):
+    """The lowest free page is one that the source holds: it counts for both."""
+    d = U.Device(war, O.Books(8, 4, [[0, 1], []], [6, 0], [[1], [2]], [1, -1]))
+    uncount(d, 0)
+    fork(war, d, [-1, 0], 4)
+    assert war.war_device_status() == BAD_PAGE and d.listed() == [(1, 0, 2)]
+    assert d.pages.page_table[1].tolist() == [0, 0, -1, -1]
+    assert agree(d) == [2, 1, 0, 0, 0, 0, 0, 0]
+
+
+def test_fork_that_gives_out_a_page_of_what_is_replaced(war):
+    d = U.Device(war, O.Books(8, 4, [[0], [2, 3]], [4, 6], [[1], [2]], [1, 1]))
+    uncount(d, 0)
+    fork(war, d, [1, -1], 4)
+    assert war.war_device_status() == BAD_PAGE and d.listed() == [(3, 0, 2)]
+    assert d.pages.page_table.tolist() == [[2, 0, -1, -1], [2, 3, -1, -1]] and agree(d) == [1, 0, 2, 1, 0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_forks_of_books_that_count_too_little(war, seed):
+    """refs goes by the changes alone, whatever the order of the blocks: entries afterwards minus those that were not counted, or 0."""
+    rng = np.random.default_rng(seed)
+    B, page = int(rng.choice([5, 40, 300])), 4
+    b = U.random_books(rng, B, page, 60, 3 * B, room=6)
+    live = [i for i in range(B) if b.tail_len[i] >= 0]
+    src = [int(rng.choice(live)) if rng.random() < 0.6 else -1 for _ in range(B)]
+    d = U.Device(war, b)
+    free, lost = b.free(), {}
+    for i in rng.permutation(live)[:4].tolist():
+        full = b.rows[i][:b.prefix[i] // page]
+        full = [p for p in full if p > free[B]]                                   # (what is given out is below)
+        if full:
+            p = int(rng.choice(full))
+            for _ in range(int(rng.integers(1, b.refs()[p] + 1)) if p not in lost else 0):
+                uncount(d, p)
+                lost[p] = lost.get(p, 0) + 1
+    zero = [p for p in lost if int(d.pages.refs[p]) == 0]
+    touched = {p for i in range(B) for p in b.rows[i] if (src[i] >= 0 and src[i] != i) or i in [s for k, s in enumerate(src) if s != k]}
+    before = b.refs()
+    ok, copies = O.fork(b, src, page)
+    fork(war, d, src, page)
+    assert ok and int(d.word) == 1 and d.listed() == copies
+    after = b.refs()
+    assert agree(d) == [max(0, n - lost.get(p, 0)) for p, n in enumerate(after)]
+    status = war.war_device_status()
+    assert status in (0, BAD_PAGE)
+    if any(p in touched and before[p] != after[p] for p in zero):
+        assert status == BAD_PAGE
