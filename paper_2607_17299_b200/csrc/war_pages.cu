@@ -253,6 +253,7 @@ pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, 
 // hold.  Asking for the counts of the pages that gain holders, too, costs 256 resampled requests 31.0 -> 34.5 us.
 constexpr int kDeep = 4, kForkDeep = 8;   // entries that a thread asks for at once
 constexpr int kForkTile = 16384;          // entries of a tile
+constexpr int kNoPage = 0x7fffffff;       // a source's partly filled page that lies outside the pool: its copies get none
 struct ForkShared {
     ScanScratch scan;
     FreeRound round;
@@ -311,8 +312,8 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
             if (src >= 0 && prefix_len[src] % page_size != 0) {
                 last = p.d_page_table[(size_t)src * width + s.full[src]];
                 const bool bad = last < 0 || last >= p.num_pages;
-                if (bad) { if (rank == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); last = 0; }
-                fresh = bad || !(s.src[src] >= 0 && s.first[src] == b && p.d_refs[last] == 1);
+                if (bad) { if (rank == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); last = kNoPage; }
+                fresh = !bad && !(s.src[src] >= 0 && s.first[src] == b && p.d_refs[last] == 1);
             }
             s.last[b] = last;
             if (src >= 0) atomicMax(&s.columns, max(s.held[b], s.full[src] + (last >= 0)));
@@ -443,7 +444,7 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
                 if (src < 0) continue;
                 int now = -1;
                 if (col < s.full[src]) now = s.entries[(src << wide) + c];
-                else if (col == s.full[src] && s.last[b] >= 0) now = s.fresh[b] < -1 ? ~(s.fresh[b] + 1) : s.last[b];
+                else if (col == s.full[src] && s.last[b] >= 0) now = s.fresh[b] < -1 ? ~(s.fresh[b] + 1) : s.last[b] == kNoPage ? -1 : s.last[b];
                 else if (col >= s.held[b]) continue;              // (nothing stood there)
                 p.d_page_table[(size_t)b * width + col] = now;
             }

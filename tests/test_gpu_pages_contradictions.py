@@ -180,3 +180,33 @@ def test_forks_of_books_that_count_too_little(war, seed):
     assert status in (0, BAD_PAGE)
     if any(p in touched and before[p] != after[p] for p in zero):
         assert status == BAD_PAGE
+
+
+@pytest.mark.parametrize("page", [40, -3, 0x7FFFFFFF, -2147483648])
+@pytest.mark.parametrize("replaced", [False, True])
+def test_fork_of_a_partly_filled_page_outside_the_pool(war, page, replaced):
+    """No copy of another page's rows, and no fresh page for it: the entry is none."""
+    d = U.Device(war, books())
+    d.pages.page_table[0, 2] = page
+    d.pages.refs[5] = 0
+    d.pages.free.copy_(torch.from_numpy(U.words(d.pages.refs.tolist())))
+    fork(war, d, [2 if replaced else -1, -1, 0, 0], 4)
+    assert war.war_device_status() == BAD_PAGE and int(d.word) == 1 and d.listed() == []
+    first = [20, 21, -1] if replaced else [3, 4, page]
+    assert [r[:3] for r in d.pages.page_table.tolist()] == [first, [3, 4, 9], [3, 4, -1], [3, 4, -1]]
+    assert d.pages.held.tolist() == [2 if replaced else 3, 3, 3, 3] and d.prefix.tolist() == [8 if replaced else 10, 11, 10, 10]
+    refs = agree(d)
+    assert [refs[x] for x in (0, 3, 4, 9, 20, 21)] == ([0, 3, 3, 1, 1, 1] if replaced else [0, 4, 4, 1, 0, 0])
+
+
+def test_a_fork_and_its_copies_leave_the_first_page_alone(war):
+    d = U.Device(war, books())
+    d.pages.page_table[0, 2] = 99
+    k, v = (torch.randn((40, 2, 4, 128), device=DEV).to(torch.bfloat16) for _ in range(2))
+    want = k.clone(), v.clone()
+    fork(war, d, [-1, -1, 1, 0], 4)                                              # (request 2: a sound one behind it)
+    war.war_pages_copy(d.copies, d.n, k, v)
+    assert war.war_device_status() == BAD_PAGE and d.listed() == [(9, 0, 3)]
+    for x, y in zip((k, v), want):
+        y[0, :, :3] = y[9, :, :3]
+        assert torch.equal(x, y)
