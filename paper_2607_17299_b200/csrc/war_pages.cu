@@ -443,8 +443,10 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
                 }
                 if (src < 0) continue;
                 int now = -1;
-                if (col < s.full[src]) now = s.entries[(src << wide) + c];
-                else if (col == s.full[src] && s.last[b] >= 0) now = s.fresh[b] < -1 ? ~(s.fresh[b] + 1) : s.last[b] == kNoPage ? -1 : s.last[b];
+                if (col < s.full[src]) {
+                    now = s.entries[(src << wide) + c];           // (one outside the pool stays what it is)
+                    if (now < 0 || now >= p.num_pages) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+                } else if (col == s.full[src] && s.last[b] >= 0) now = s.fresh[b] < -1 ? ~(s.fresh[b] + 1) : s.last[b] == kNoPage ? -1 : s.last[b];
                 else if (col >= s.held[b]) continue;              // (nothing stood there)
                 p.d_page_table[(size_t)b * width + col] = now;
             }

@@ -199,6 +199,19 @@ def test_fork_of_a_partly_filled_page_outside_the_pool(war, page, replaced):
     assert [refs[x] for x in (0, 3, 4, 9, 20, 21)] == ([0, 3, 3, 1, 1, 1] if replaced else [0, 4, 4, 1, 0, 0])
 
 
+@pytest.mark.parametrize("page", [40, -3])
+@pytest.mark.parametrize("src", [[-1, -1, -1, 0], [2, -1, -1, 0], [2, -1, 0, -1]])
+def test_fork_of_a_full_page_outside_the_pool(war, page, src):
+    """The entry is copied as it is and reported, and counts nowhere."""
+    d = U.Device(war, books())
+    d.pages.page_table[0, 1] = page
+    uncount(d, 4)
+    fork(war, d, src, 4)
+    assert war.war_device_status() == BAD_PAGE and int(d.word) == 1
+    taker = src.index(0)
+    assert d.pages.page_table[taker, :2].tolist() == [3, page] and agree(d)[4] == 1
+
+
 def test_a_fork_and_its_copies_leave_the_first_page_alone(war):
     d = U.Device(war, books())
     d.pages.page_table[0, 2] = 99
