@@ -805,9 +805,8 @@ extern "C" war_status_t war_pages_fork(const war_pages_t* p, const int32_t* d_sr
                                        int32_t* d_tail_len, int32_t* d_copies, int32_t* d_n_copies, int32_t* d_ok, war_stream_t stream) {
     war_status_t st = check_pages(p);
     if (st != WAR_OK) return st;
-    if (P < 1 || P > kMaxTail) return WAR_ERR_INVALID_ARG;
-    if (p->B == 0) return WAR_OK;
-    if (!d_src || !d_prefix_len || !d_tail || !d_tail_len || !d_copies || !d_n_copies || !d_ok) return WAR_ERR_INVALID_ARG;
+    if (P < 1 || P > kMaxTail || !d_n_copies || !d_ok) return WAR_ERR_INVALID_ARG;
+    if (p->B > 0 && (!d_src || !d_prefix_len || !d_tail || !d_tail_len || !d_copies)) return WAR_ERR_INVALID_ARG;   // (without requests both words are written all the same)
     int* status_word = war_status_word();
     if (!status_word) return WAR_ERR_CUDA;
     int sms;

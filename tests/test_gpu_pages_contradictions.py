@@ -223,3 +223,15 @@ def test_a_fork_and_its_copies_leave_the_first_page_alone(war):
     for x, y in zip((k, v), want):
         y[0, :, :3] = y[9, :, :3]
         assert torch.equal(x, y)
+
+
+def test_a_fork_of_no_requests_leaves_no_copies(war):
+    """What follows does not apply an earlier list again."""
+    pages = war.new_pages(40, 0, 5, DEV)
+    none, copies, n, ok = t([]), t([[1, 2, 4], [3, 4, 4]]), t([2]), t([-7])
+    war.war_pages_fork(pages, none, 4, none, torch.zeros((0, 8), dtype=torch.int32, device=DEV), none, copies, n, ok)
+    assert int(n) == 0 and int(ok) == 1
+    k, v = (torch.randn((40, 2, 4, 128), device=DEV).to(torch.bfloat16) for _ in range(2))
+    want = k.clone(), v.clone()
+    war.war_pages_copy(copies, n, k, v)
+    assert torch.equal(k, want[0]) and torch.equal(v, want[1]) and war.war_device_status() == 0
