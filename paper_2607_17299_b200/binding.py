@@ -886,6 +886,8 @@ def war_pages_copy(d_copies: torch.Tensor, d_n_copies: torch.Tensor, k_pool: tor
     """Applies a list of copies (war_pages_fork, war_pages_compact) to one layer's cache: bf16, or 8-bit with its scales."""
     q = _copy_params(_layout(k_pool), _layout(v_pool), _layout(k_scale), _layout(v_scale))
     lines = _copy_list(d_copies, 0)
+    if d_n_copies.numel() != 1:
+        raise ValueError("d_n_copies is one number")
     at, _ = _addresses(torch.int32, d_copies, d_n_copies)
     code = _lib.war_pages_copy(at[0], at[1], lines, _address(k_pool), _address(v_pool), _address(k_scale), _address(v_scale), C.byref(q),
                                _stream_of(k_pool, v_pool, k_scale, v_scale))
