@@ -438,7 +438,8 @@ war_status_t war_rope_frequencies(const war_rope_freq_params_t* params, float* h
 /* ------------------------------------------------------------------------------------------------
  * Verification attention over a cache held in 8 bits: war_verify_attn with K[c,:] = kscale * kcode[c,:] and
  * V[c,:] = vscale * vcode[c,:], the scales those of c's block of scale_block tokens and kv head (see war_rope_store; here they
- * need not be powers of two).  Half the bytes of the bf16 cache, and the codes go to the tensor cores as they are: q and the
+ * need not be powers of two).  Half the bytes of the bf16 cache, and the codes go to the tensor cores as they are (war_verify_attn_shared_quant
+ * differs above 64 query rows, see there): q and the
  * softmax weights are each split into two 8-bit parts whose products are summed in 32 bits,
  * so no precision of the bf16 queries is lost (elements below 2^-9 of a row's largest are held to 2^-17 of it).  A weight
  * times its V scale, w = p * vscale, is held to 2^-7.8 of itself or, the small ones, to 2^-18.6 of the largest w among the
@@ -585,6 +586,9 @@ war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d_n_copies, 
  * count; members that are no leaders are looked at first, so a leader that they leave alone is a request for itself.
  * kernel must be 0; Hkv <= 65535, B * N * Hq < 2^29.  Three launches.  Pages of the shared prefix are taken from one table: tables that differ there
  * give the results of that one.
+ * Precision: war_verify_attn's and, for the 8-bit cache, war_verify_attn_quant's up to 64 query rows per request and kv head ((Hq / Hkv) * N).
+ * Above, codes are widened to halves on chip, which keeps all of them; q is kept as halves that hold elements above 2^-29 of a row's
+ * largest exactly; and w = p * vscale is rounded once, to 2^-11 of itself or, the small ones, to 2^-32 of the row's largest w (V scales as there).
  * ------------------------------------------------------------------------------------------------ */
 war_status_t war_prefix_groups(const int32_t* d_page_table, const int32_t* d_prefix_len, const int32_t* d_tail_len, int32_t B,
                                int32_t page_size, int32_t max_pages_per_req, int32_t min_shared, int32_t* d_leader, int32_t* d_shared_len,
