@@ -63,6 +63,9 @@ static_assert(sizeof(Bars) <= 640, "barrier block");
 
 // Load n of the CTA (see load_k) has codes in slot n % 2 and halves in slot n % 4 of the ring; its barriers are numbers n % 4 and n % 8, as in
 // war_verify_attn_shared_sm100.cu.
+// Scales are written without a wait for their ring.  Those of tile t + 1 come behind load K(t + 1), number 2t + 1 of its unit, for which the wideners
+// are through with load 2t - 1 and so the issuers with load 2t - 5 and all before it, V(t - 4) among them: the softmax warps are past tile t - 4.
+// A unit's first scales come behind the last load of the unit before, which says as much for the tile four back.  Five tiles would do.
 __device__ __forceinline__ uint4 ld_shared16(uint32_t at) {
     uint4 x;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
@@ -180,7 +183,7 @@ attn_shared_quant_kernel(const __grid_constant__ CUtensorMap k_map, const __grid
     if (warp == kWarpLoad0 || warp == kWarpLoad1) {
         // ------------------------------------------------------------------ producers: both make every load, half of its pages each
         // (one lane issues one copy, and a warp's copies go out one after the other, about 60 ns each.  A warp for K and one for V
-        // would not do here: with five slots the one could get two rounds ahead of the other, and parities would mislead it.)
+        // would not do here: with two slots the one could get a round of barriers ahead of the other, and parities would mislead it.)
         const int half = warp == kWarpLoad1;
         const int piece = 2 * lane + half;                          // this lane's page of a tile
         uint32_t ld = 0, tile0 = 0;
