@@ -7,8 +7,8 @@
 // All of this is a few kilobytes to a few megabytes of integers per call, so a call costs its launch and the chain of dependent reads.
 // One launch each, then.  Fork and compaction need all blocks to have read before one writes; they run as one cluster of
 // eight blocks, whose hardware barrier takes the place of further launches (a barrier: about 0.5 us; a launch in a graph: 1.5 to 2).
-// Measured, a launch by itself, cold: 1024 requests with 0.5 million pages: free 8.6 us, grow 9.6; 256 requests resampled: fork 32;
-// 128 requests in 3.5 GB of 64 KB pages: compaction 17, the copy of its moves 254 (6.3 TB/s, the rate of a plain copy); groups among
+// Measured, a launch by itself, cold: 1024 requests with 0.5 million pages: free 8.6 us, grow 9.6; 256 requests resampled: fork 38;
+// 128 requests in 3.5 GB of 64 KB pages: compaction 19, the copy of its moves 254 (6.3 TB/s, the rate of a plain copy); groups among
 // 512 requests of up to 73 000 tokens 15.
 #include <cooperative_groups.h>
 #include <mutex>
@@ -238,7 +238,7 @@ pages_grow_kernel(war_pages_t p, int N, const int32_t* __restrict__ prefix_len, 
     for (int b = tid; b < B; b += kThreads) {
         const int need = s.upto[b + 1] - s.upto[b];
         const bool ok = s.held[b] >= 0 && (need == 0 || s.upto[b + 1] <= served);
-        if (granted) granted[b] = ok;
+        granted[b] = ok;
         if (ok && need > 0) p.d_held[b] = s.held[b] + need;
     }
 }
@@ -487,9 +487,9 @@ pages_fork_kernel(war_pages_t p, const int32_t* __restrict__ d_src, int P, int32
 // ------------------------------------------------------------------------------------------------
 // The i-th highest used page goes to the i-th lowest free page while it lies above it.  With U pages in use that moves exactly the
 // used pages at or above U, so the two lists are the free pages below U, upwards, and the used ones from U on, downwards.
-// place[] says where in its list a page stands, and counts for nothing unless the list has the page there: only listed pages are written, so
-// for any other it holds what the workspace held.  That tells a held page that the map has as free, on either side of U, without a word for
-// every page of the pool.
+// The map as it was is kept: a table's entry that it has as free is not counted in refs, whichever side of U its page is on, and place[] holds for it
+// what the workspace held.  (A word for 32 pages, mostly out of L1: 18.8 us where 17.6 without the look, 3.5 GB pool;
+// to look the page up in its list instead costs two dependent reads an entry, 24.6.)
 struct CompactShared {
     int2 warp[32];
     int used;                              // of this block's words
@@ -503,9 +503,10 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, rank = (int)cluster.block_rank();
     const int n_words = (int)((p.num_pages + 31) / 32);
-    int32_t* const place = ws;                                    // [num_pages] a listed page's position
-    int32_t* const to = ws + p.num_pages;                         // free pages below U
-    int32_t* const from = to + p.num_pages;                       // used pages from U on
+    int32_t* const place = ws;                                    // [num_pages] where a used page from U on goes
+    int32_t* const to = ws + p.num_pages;                         // free pages below U; as many as used ones from U on, at most half of all
+    int32_t* const from = to + p.num_pages / 2;                   // used pages from U on
+    uint32_t* const was = (uint32_t*)(ws + 2 * p.num_pages);      // the map before the moves
     const int per = (n_words + kCluster - 1) / kCluster, w0 = min(n_words, rank * per), w1 = min(n_words, w0 + per);
     auto valid = [&](int w) -> uint32_t {                         // pages of a word that exist
         const long long left = p.num_pages - (long long)w * 32;
@@ -515,7 +516,8 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
     const bool once = w1 - w0 <= kThreads;                        // a word a thread: it is read and summed up once
     const uint32_t mine = w0 + tid < w1 ? p.d_free[w0 + tid] : 0u;
     int used = w0 + tid < w1 ? __popc(~mine & valid(w0 + tid)) : 0;
-    for (int w = w0 + tid + kThreads; w < w1; w += kThreads) used += __popc(~p.d_free[w] & valid(w));
+    if (w0 + tid < w1) was[w0 + tid] = mine;
+    for (int w = w0 + tid + kThreads; w < w1; w += kThreads) { const uint32_t f = p.d_free[w]; was[w] = f; used += __popc(~f & valid(w)); }
     int2 total;
     block_scan2(make_int2(used, 0), s.warp, &total);
     if (tid == 0) s.used = total.x;
@@ -560,7 +562,7 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
             const int i = i0 + k * kCluster * kThreads;
-            a[k] = i < moves ? from[i] : 0; c[k] = i < moves ? to[i] : 0;
+            a[k] = i < moves ? from[i] : 0; c[k] = i < done ? to[i] : a[k];
         }
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) refs[k] = i0 + k * kCluster * kThreads < done ? p.d_refs[a[k]] : 0;
@@ -568,7 +570,7 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
         for (int k = 0; k < kDeep; ++k) {
             const int i = i0 + k * kCluster * kThreads;
             if (i >= moves) break;
-            place[a[k]] = i; place[c[k]] = i;
+            place[a[k]] = c[k];
             if (i >= done) continue;
             p.d_refs[c[k]] = refs[k];
             p.d_refs[a[k]] = 0;
@@ -588,23 +590,20 @@ pages_compact_kernel(war_pages_t p, int32_t* ws, int max_copies, int32_t* copies
         int32_t* row = p.d_page_table + (size_t)b * p.max_pages_per_req;
         if (held < 0 || held > p.max_pages_per_req) { if (lane == 0) war_set_device_status(status_word, WAR_ERR_BAD_PAGE); continue; }
         for (int j0 = lane; j0 < held; j0 += 32 * 2 * kDeep) {
-            int page[2 * kDeep], at[2 * kDeep], listed[2 * kDeep], now[2 * kDeep];
+            int page[2 * kDeep], now[2 * kDeep];
+            bool bad[2 * kDeep];
 #pragma unroll
-            for (int k = 0; k < 2 * kDeep; ++k) page[k] = j0 + k * 32 < held ? row[j0 + k * 32] : -1;
-#pragma unroll
-            for (int k = 0; k < 2 * kDeep; ++k) at[k] = page[k] >= 0 && page[k] < p.num_pages ? place[page[k]] : -1;
+            for (int k = 0; k < 2 * kDeep; ++k) page[k] = j0 + k * 32 < held ? row[j0 + k * 32] : 0;
 #pragma unroll
             for (int k = 0; k < 2 * kDeep; ++k) {
-                if (at[k] >= moves) at[k] = -1;
-                listed[k] = at[k] < 0 ? -1 : page[k] < U ? to[at[k]] : from[at[k]];
-                now[k] = at[k] < 0 || page[k] < U ? -1 : at[k] < done ? to[at[k]] : page[k];
+                bad[k] = page[k] < 0 || page[k] >= p.num_pages;
+                now[k] = !bad[k] && page[k] >= U ? place[page[k]] : page[k];
+                bad[k] = bad[k] || (was[page[k] >> 5] >> (page[k] & 31) & 1u);
             }
 #pragma unroll
             for (int k = 0; k < 2 * kDeep; ++k) {
                 if (j0 + k * 32 >= held) continue;
-                // outside the pool; a free one of the list below U; none of the used ones from U on
-                const bool bad = page[k] < 0 || page[k] >= p.num_pages || (page[k] < U ? listed[k] == page[k] : listed[k] != page[k]);
-                if (bad) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
+                if (bad[k]) war_set_device_status(status_word, WAR_ERR_BAD_PAGE);
                 else if (page[k] >= U) row[j0 + k * 32] = now[k];
             }
         }
@@ -701,7 +700,7 @@ struct CopyArgs {
     long long ks[3], vs[3];                // strides (page, head, token) in bytes
     const int32_t *copies, *n_copies;
     long long num_pages;
-    int max_copies, Hkv, page_size, row_bytes, block;
+    int max_copies, Hkv, page_size, block;
 };
 
 // A warp per (copy, K or V, head): rows of 256 or 128 bytes, 512 bytes a warp's instruction, up to eight of them in flight.
@@ -868,7 +867,7 @@ extern "C" war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d
     a.k = (uint8_t*)d_kpool; a.v = (uint8_t*)d_vpool; a.kscale = d_kscale; a.vscale = d_vscale;
     for (int i = 0; i < 3; ++i) { a.ks[i] = q->kpool_strides[i] * size; a.vs[i] = q->vpool_strides[i] * size; }
     a.copies = d_copies; a.n_copies = d_n_copies; a.num_pages = q->num_pages; a.max_copies = max_copies;
-    a.Hkv = q->Hkv; a.page_size = q->page_size; a.row_bytes = 128 * size; a.block = quant ? q->scale_block : 0;
+    a.Hkv = q->Hkv; a.page_size = q->page_size; a.block = quant ? q->scale_block : 0;
     const long long blocks = ((long long)max_copies * 2 * q->Hkv + kCopyWarps - 1) / kCopyWarps;
     const int grid = (int)(blocks < sms * 8ll ? blocks : sms * 8ll);
     return war_launch_behind(quant ? pages_copy_kernel<8> : pages_copy_kernel<16>, grid, kCopyWarps * 32, 0, 1, stream, a, status_word);
