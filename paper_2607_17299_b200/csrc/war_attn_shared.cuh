@@ -5,7 +5,7 @@
 // visible to all) or what a request has for itself (its rows; keys behind the shared ones, its tree among them).  Parts are cut into
 // units as in war_attn_plan.cuh: (part, kv head, row block, chunk of 128-key tiles).  Rows of a shared part are the (slot, query head
 // of the group) pairs of its members one behind the other, so that row blocks are full whatever the trees' sizes are.  A row block has
-// 256 rows with the bf16 kernel and 128 with the 8-bit one.
+// 256 rows, and 128 with the 8-bit kernel up to kQuantWideRows.
 #pragma once
 #include <cuda_runtime.h>
 #include "war_attn_plan.cuh"
@@ -69,7 +69,9 @@ inline SharedWorkspace war_attn_shared_layout(const war_attn_params_t* p, void* 
 // and kv head, above war_verify_attn_shared_quant_sm100.cu.  The latter has twice the rows in a unit, the former more of a cache in flight where
 // memory is the bound, the requests' own keys.  In turn on one GPU (us, former / latter): 4 rows, 4K to 8K own keys 504 / 645; 32 rows
 // 16 prompts of 4 338 / 347, one of 16 264 / 240; 64 rows, 8K own keys 257 / 290, 4 prompts of 4 with 32K 271 / 236; 68 and 80 rows, 8K own keys
-// 300 / 308, 304 / 312, with 4 rollouts of 12K shared 376 / 366; 128 rows 331 / 329, 721 / 637, 517 / 460; 256 rows 562 / 495, 680 / 588.
+// 300 / 308, 304 / 312, with 4 rollouts of 12K shared 376 / 366; 128 rows 331 / 329, 721 / 637, 517 / 460; 256 rows 562 / 495, 680 / 588.  The rule sees a
+// request's rows, which the host knows, and not the lengths, which it does not: with shared keys alone the latter can be ahead at 32 and 64 rows
+// (264 / 240, 271 / 236), with long own keys the former still at 68 and 80 (300 / 308, 304 / 312).
 constexpr int kQuantWideRows = 64;
 war_status_t war_attn_shared_launch(const void* q, const void* k, const void* v, const int32_t* page_table, const int32_t* parent,
                                     const war_attn_params_t* p, const SharedWorkspace& w, void* out, float* lse,

@@ -98,7 +98,7 @@ __device__ __forceinline__ void tmem_zero8(uint32_t taddr) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%1], {%0, %0, %0, %0, %0, %0, %0, %0};" ::"r"(0), "r"(taddr) : "memory");
 }
 
-// kFused, kShared: see attn_sm100_kernel.
+// kFused: see attn_sm100_kernel.  kShared: units of war_verify_attn_shared.cu, drawn one by one; partial results go to its merge.
 template <bool kFused, bool kShared = false>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_quant_many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const QuantKernelArgs a) {

@@ -3,7 +3,8 @@
 // With the keys of a row split into any parts, part c giving m_c = max x, l_c = sum exp2(x - m_c), O_c = sum exp2(x - m_c) v, the whole is
 //     m = max m_c,   l = sum l_c exp2(m_c - m),   out = sum O_c exp2(m_c - m) / l,   lse = (m + log2 l) ln 2.
 // So the prefix of a group is one part whose rows are those of all members, read once, and what each member has for itself is
-// another.  The attention kernels are those of war_verify_attn and war_verify_attn_quant; only their units come from here.
+// another.  Their units come from here; the kernels are war_verify_attn_shared_sm100.cu (bf16 cache), war_verify_attn_quant_many.cu and
+// war_verify_attn_shared_quant_sm100.cu (8-bit cache).
 #include <cuda_bf16.h>
 #include <math_constants.h>
 #include <mutex>
@@ -74,6 +75,8 @@ constexpr int kMinChunkCost = 4;          // tiles of one row block
 // 6 in place of 36 is 2 to 25 % slower, 100 from 3 % faster to 29 % slower; a search over 32 chunk costs by an estimate of the time was no
 // better; shared and own parts in turn instead of by length: 818 us against 728 with 256 requests.)  With little work C is what makes a unit
 // for every CTA, if that is less.  Units are sorted, the longest first; the CTAs draw them one by one.  Cold: 13 us for 32 requests, 23 for 256.
+// A part's place is found by comparing it with all others, and a member's rows by a walk over the requests before it, so the time grows with the square
+// of the requests (trees of 8 slots): 75 us for 1024 in groups of eight (91 in one group), 223 for 2048, 760 for 4096 (1270 in pairs, 970 in one group).
 __global__ void __launch_bounds__(kPlanThreads)                    // (a quarter of the threads for small batches: barriers are cheaper)
 attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ num_nodes, const int32_t* __restrict__ parent,
                         const int32_t* __restrict__ leader, const int32_t* __restrict__ shared_len, int B, int N, int Hkv, int G,
@@ -245,7 +248,7 @@ attn_shared_plan_kernel(const int32_t* __restrict__ prefix_len, const int32_t* _
         x.pad = 0;
         w.parts[e] = x;
     }
-    if (tid == 0) { w.counters[0] = 0; w.counters[1] = units; w.counters[3] = 0; }
+    if (tid == 0) { w.counters[0] = 0; w.counters[1] = units; }
     __syncthreads();
     // ---- unit table: (chunk, kv head, row block), a thread each ----
     for (int u = tid; u < units; u += n_threads) {

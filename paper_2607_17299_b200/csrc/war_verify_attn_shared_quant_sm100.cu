@@ -4,10 +4,11 @@
 // Every code of both types is a half, so K and V lose nothing.  Q is scaled by a power of two per row (its largest element into [2^14, 2^15)) and
 // kept as halves: exact for elements above 2^-29 of the row's largest.  Scales stay outside of the products: K's goes to S, p * (V's
 // scale) is rounded to a half (2^-11 of itself, or 2^-32 of the row's largest), with the row's reference as in war_attn_quant.cuh.
-// What bounds it: the softmax, as there, and shared memory: a tile with two row blocks moves 352 KB (operands 256, codes in 32, out of their
-// slot and in again 64), 2750 cycles at 128 bytes each.  4 prompts of 16K to 32K tokens with 7 rollouts of 32 slots and 4 requests alone, 32 + 8 heads,
-// e4m3: 637 us the call (codes as they are: 721; each for itself 649; bf16 cache 530).  Conversions are not the bound (e5m2, widened by moving bytes, takes
-// the same), nor is the number of slots for codes (four of them, three for halves: 709 against 656).
+// What it costs: 4 prompts of 16K to 32K tokens with 7 rollouts of 32 slots and 4 requests alone, 32 + 8 heads, 637 us the call with e4m3 and as much
+// with e5m2 (codes as they are: 721; each for itself 649; bf16 cache 530).  No one unit is the bound: a tile with two row blocks moves 352 KB through
+// shared memory (operands 256, codes in 32, out of their slot and in again 64), 2750 cycles at 128 bytes each, which is 250 to 290 us of the call;
+// the tensor pipe is 40 % busy, issue slots 51 %.  The rest is the chain of codes, wideners, products and softmax, which has not been taken apart.
+// Conversions are not it (e5m2 is widened by moving bytes), nor are the slots for codes (four of them, three for halves: 709 against 656).
 // Warp roles:  warps 8 and 11   producers: TMA copies of codes into two slots of 16 KB; the first one also brings the scales
 //              warps 12-15      wideners: 16 KB of codes -> a 32 KB slot of the ring, rows of V past the part's last key zeroed
 //              warps 9 and 10   MMA issuers, warps 0-3 and 4-7 softmax groups: as there
