@@ -525,7 +525,9 @@ war_status_t war_commit_quant(const int32_t* d_ids, const int32_t* d_accept_len,
  * int32 [n, 3] = (from, to, rows) is given to war_pages_copy once per layer.  Results do not depend on timing: pages are given
  * out from the lowest free one up, to the requests in order.  B <= 4096, num_pages <= 2^30, B * max_pages_per_req < 2^31.  One launch each; nothing is allocated.
  * Books that contradict themselves (a page outside the pool, more entries than refs counts, held outside [0, max_pages_per_req]) record
- * WAR_ERR_BAD_PAGE; such entries are left out.
+ * WAR_ERR_BAD_PAGE where a call meets them; such entries are left out: they change no count (copies of an entry that is not counted are), refs stays at 0 or
+ * above, and bits that were set iff refs is 0 stay so.  The bits are believed: a held page that refs does not count is free to grow and fork, and compaction, which
+ * reports its holder, may move another page onto it.
  *
  * war_pages_grow: room for the next step.  A running request (d_tail_len NULL, or tail_len[b] >= 0) gets pages for positions below
  *   prefix_len[b] + N.  It is served iff the pool has all pages wanted by the requests up to and with it.
@@ -535,9 +537,10 @@ war_status_t war_commit_quant(const int32_t* d_ids, const int32_t* d_accept_len,
  *   stay.  All copies are made at once, so requests may swap.  Its prefix_len, tail window and tail_len are those of s (see war_commit); the
  *   full pages of the prefix are shared; the page that is partly filled (prefix_len % page_size rows) becomes a fresh one and a line of
  *   d_copies, except that the lowest request that takes an s which is itself replaced gets s's page, if nobody else holds it.
+ *   Full pages outside the pool are copied as they are, for a partly filled one the entry is -1 and nothing is copied.
  *   What b held before is given back; entries behind the new ones are -1; pages of s behind its prefix (its tree's) are not shared:
  *   war_pages_grow follows.  d_copies has room for B lines, in the order of the requests; d_n_copies int32.  *d_ok = 1; or 0 and nothing is changed
- *   where the pool has too few free pages (those given back by the call itself do not count).  A source that is not running, is
+ *   where the pool has too few free pages (those given back by the call itself do not count), d_n_copies is 0 then; both are written without requests, too.  A source that is not running, is
  *   no request or holds fewer pages than its prefix: WAR_ERR_INVALID_ARG, and b stays as it is.
  * war_pages_free: requests with done[b] != 0 give their pages back (shared ones stay with their other holders): held = 0, their entries -1,
  *   tail_len = -1 where d_tail_len is given.
@@ -546,7 +549,7 @@ war_status_t war_commit_quant(const int32_t* d_ids, const int32_t* d_accept_len,
  *   *d_top: no page at or above it is in use.  d_workspace: war_pages_compact_workspace_bytes(num_pages), 4-byte aligned, any contents.
  * war_pages_copy: rows [0, rows) of page `from` to page `to` for every line, K and V, all heads, and the scales of the blocks that hold
  *   them.  A page that is written stands on one line only.  *d_n_copies lines, at most max_copies.  Pools by strides: unit stride
- *   along d, the others multiples of 16 bytes.  Bad page ids are skipped (WAR_ERR_BAD_PAGE).
+ *   along d, the others multiples of 16 bytes; at most 32 blocks with scales to a page.  Bad page ids are skipped (WAR_ERR_BAD_PAGE).
  * ------------------------------------------------------------------------------------------------ */
 typedef struct {
     int32_t* d_refs; uint32_t* d_free; int32_t* d_page_table; int32_t* d_held;
@@ -586,6 +589,9 @@ war_status_t war_pages_copy(const int32_t* d_copies, const int32_t* d_n_copies, 
  * count; members that are no leaders are looked at first, so a leader that they leave alone is a request for itself.
  * kernel must be 0; Hkv <= 65535, B * N * Hq < 2^29.  Three launches.  Pages of the shared prefix are taken from one table: tables that differ there
  * give the results of that one.
+ * When to call it: it reads a group's prefix once and pays with two more launches and partial results to merge.  It wins where the prefix is most
+ * of what requests read (rollouts of a few slots behind thousands of shared tokens: half the time and less); with 32-slot trees, which are bound by
+ * the products, 2 to 8 % are left; it loses where nobody or only pairs with long own keys share.  Calls of some 40 us are within a few us either way.
  * Precision: war_verify_attn's and, for the 8-bit cache, war_verify_attn_quant's up to 64 query rows per request and kv head ((Hq / Hkv) * N).
  * Above, codes are widened to halves on chip, which keeps all of them; q is kept as halves that hold elements above 2^-29 of a row's
  * largest exactly; and w = p * vscale is rounded once, to 2^-11 of itself or, the small ones, to 2^-32 of the row's largest w (V scales as there).
